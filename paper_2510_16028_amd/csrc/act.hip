@@ -30,29 +30,6 @@ constexpr double kTwoRsqrtPiUp = 0x1.20dd750429b6ep+0;   // 2/sqrt(pi) rounded u
 constexpr double kBetaUp = 0x1.9884533d43651p-1, kBetaLo = 0x1.9884533d43650p-1;   // sqrt(2/pi)
 constexpr double kCubicUp = 0x1.6e4e26d4801f8p-5, kCubicLo = 0x1.6e4e26d4801f7p-5; // 0.044715
 
-// exp(-s) for s >= 0 with relative error below 2^-40 (covered, with the few
-// roundings around it, by the guard factor): s = k ln2 + r, |r| <= ln2/2, degree-11
-// Taylor polynomial of exp(-r) (remainder 0.35^12/12! < 1e-14), scaled by 2^-k.
-__device__ __forceinline__ double exp_neg(double s) {
-    if (s > 745.0) return 0x1p-1074;                       // never report exactly 0
-    const double kf = rint(s * 0x1.71547652b82fep+0);      // s / ln 2
-    const double r = fma(-kf, 0x1.62e42fefa39efp-1, s) - kf * 0x1.abc9e3b39803fp-56;   // s - k ln2
-    const double x = -r;
-    double p = 1.0 / 39916800.0;
-    p = fma(p, x, 1.0 / 3628800.0);
-    p = fma(p, x, 1.0 / 362880.0);
-    p = fma(p, x, 1.0 / 40320.0);
-    p = fma(p, x, 1.0 / 5040.0);
-    p = fma(p, x, 1.0 / 720.0);
-    p = fma(p, x, 1.0 / 120.0);
-    p = fma(p, x, 1.0 / 24.0);
-    p = fma(p, x, 1.0 / 6.0);
-    p = fma(p, x, 0.5);
-    p = fma(p, x, 1.0);
-    p = fma(p, x, 1.0);
-    return ldexp(p, -(int)kf);
-}
-
 template <int KIND>
 __device__ __forceinline__ float act_one(float x, float y, const ActConsts& k) {
     const double ay = fabs((double)y);
@@ -307,9 +284,7 @@ static int act_setup(int kind, const tao_fp_model* model, tao::ActConsts* out, d
     k.et_f = widen(2.0 * u + u * u);
     const double inv1mu = widen(1.0 / (1.0 - u));
     k.fresh2 = widen(u * (1.0 + inv1mu));
-    const double c1 = widen(md.c_exp * u / (1.0 - md.c_exp * u));
-    const double om = widen((c1 + u) * inv1mu);
-    k.silu_f = widen(om * inv1mu + u);
+    k.silu_f = silu_factor(md);
     k.a_f = widen(kTwoRsqrtPiUp * (1.0 + 4.0 * u));
     k.g7 = widen(7.0 * u / (1.0 - 7.0 * u));
     k.c_tanh_u = md.c_tanh * u;

@@ -40,6 +40,29 @@ __device__ __forceinline__ float up32g(double v, double mul = kUpMul, double sub
     return f;
 }
 
+// exp(-s) for s >= 0 with relative error below 2^-40 (covered, with the few
+// roundings around it, by the guard factor): s = k ln2 + r, |r| <= ln2/2, degree-11
+// Taylor polynomial of exp(-r) (remainder 0.35^12/12! < 1e-14), scaled by 2^-k.
+__device__ __forceinline__ double exp_neg(double s) {
+    if (s > 745.0) return 0x1p-1074;                       // never report exactly 0
+    const double kf = rint(s * 0x1.71547652b82fep+0);      // s / ln 2
+    const double r = fma(-kf, 0x1.62e42fefa39efp-1, s) - kf * 0x1.abc9e3b39803fp-56;   // s - k ln2
+    const double x = -r;
+    double p = 1.0 / 39916800.0;
+    p = fma(p, x, 1.0 / 3628800.0);
+    p = fma(p, x, 1.0 / 362880.0);
+    p = fma(p, x, 1.0 / 40320.0);
+    p = fma(p, x, 1.0 / 5040.0);
+    p = fma(p, x, 1.0 / 720.0);
+    p = fma(p, x, 1.0 / 120.0);
+    p = fma(p, x, 1.0 / 24.0);
+    p = fma(p, x, 1.0 / 6.0);
+    p = fma(p, x, 0.5);
+    p = fma(p, x, 1.0);
+    p = fma(p, x, 1.0);
+    return ldexp(p, -(int)kf);
+}
+
 // Reductions over the 64 lanes, the result in every lane: four exchanges inside rows of 16 lanes (quads, halves, rows: data-parallel
 // moves), then rows and halves of the wavefront swapped -- register moves throughout, where a shuffle through LDS takes some hundred
 // cycles a step (LayerNorm of 512 x 768 with its check: see rowops.hip).  Each step combines what two groups of lanes hold in

@@ -57,6 +57,13 @@ int resolve_model(const tao_fp_model* m, tao_fp_model* out);
 double gamma_up(long k, const tao_fp_model& m);            // NaN when undefined
 inline double widen(double v) { return v * (1.0 + 0x1p-49); }   // for v >= 0
 
+// SiLU's and the sigmoid's relative error: w/(1-u) + u with w = (c_exp u/(1-c_exp u) + u)/(1-u), upper.
+inline double silu_factor(const tao_fp_model& m) {
+    const double u = m.u, inv1mu = widen(1.0 / (1.0 - u));
+    const double om = widen((widen(m.c_exp * u / (1.0 - m.c_exp * u)) + u) * inv1mu);
+    return widen(om * inv1mu + u);
+}
+
 // Shape checks of a 2-D convolution (channels-last input [batch][H][W][C], filters [Cout][R][S][C]) and the
 // shape of its implicit patch-matrix product: M = batch OH OW rows, K = R S C columns.
 inline int conv_geometry(long batch, long H, long W, long C, long Cout, long R, long S,

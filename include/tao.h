@@ -11,9 +11,10 @@
  * check of Sec. 5.4.
  *
  * Conventions for every entry point
- *  - All tensor pointers are DEVICE pointers to binary32 data owned by the
- *    caller; row-major; leading dimensions are in elements.  `tau` buffers are
- *    written, everything else is read only.  Nothing is retained after return.
+ *  - All tensor pointers are DEVICE pointers to binary32 data (8-bit whole
+ *    numbers where int8_t is written) owned by the caller; row-major; leading
+ *    dimensions are in elements.  `tau` buffers (and `y`, `q`, `scale` of the
+ *    operators that are re-executed) are written, everything else is read only.  Nothing is retained after return.
  *  - `stream` is the caller's hipStream_t passed as void* (NULL = the null
  *    stream).  All work is enqueued asynchronously on it; no entry point
  *    allocates device memory and none synchronises, except the two device self
@@ -245,6 +246,43 @@ int tao_bound_check_linear_in_epilogue(long M, long N, long K, long batch);
 int tao_selftest_matrix_core_bf16(unsigned *report, long cases, void *ws, size_t ws_bytes, void *stream);
 size_t tao_selftest_workspace_bytes(long cases);
 
+/* Matrix product in 8-bit whole numbers with a scale for each token (row of A) and each channel (row of W), as quantised
+ * layers compute it, re-executed and bounded in one call:
+ *     S = sum_k A[b][i][k] W[b][j][k]                            (exact: |S| <= K 2^14 < 2^31),
+ *     y[b][i][j]   = fl(fl(fl(fl(S) scale_a[b][i]) scale_w[b][j]) + bias[j])        (the addition only with a bias),
+ *     tau[b][i][j] = Gamma(d) |v|                                                   without a bias, v = S scale_a scale_w,
+ *                  = Gamma(d) |v| + u (|v + bias| + Gamma(d) |v|)                   with one,
+ *     d = 2, or 3 where |S| > 1/u (the conversion of S to binary32 then rounds too).
+ * The sum being exact, y is the same bit for bit whatever order forms it, and tau covers every execution that
+ * accumulates in 32-bit whole numbers and applies the two scales in either order, or as one product, in binary32.
+ * TAO_FLAG_UNDERFLOW_TERMS adds (|S| + |scale_a| + |scale_w| + 1) 2^-149 for scales and products that underflow.
+ * exact <= tau <= exact (1 + 1e-6); tau is NaN where a scale or the bias is not finite, +inf beyond the binary32 range.
+ * A: [batch][M][K] with row stride lda and batch stride strideA; W: [batch][N][K] (row j = weights of output j), ldw, strideW
+ * (0 shares one W and one scale_w across the batch); any strides and addresses (rows of whole 16-byte units on
+ * 16-byte addresses are read fastest).  scale_a: [batch][M], scale_w: [N] with strideW == 0, else [batch][N]; contiguous.
+ * bias: [N] or NULL, shared across the batch.  y, tau: [batch][M][N], ldy, strideY; either may be NULL (not stored).
+ * TAO_ERR_K_RANGE for K > TAO_INT8_MAX_K; TAO_ERR_SHAPE also for M, N or batch >= 2^31, M N batch >= 2^36 and overlapping
+ * outputs.  M, N or batch equal to 0 is a no-op; K == 0 gives S = 0. */
+#define TAO_INT8_MAX_K 131071
+int tao_bound_linear_int8(const int8_t *A, const float *scale_a, const int8_t *W, const float *scale_w, const float *bias,
+                          float *y, float *tau, long M, long N, long K, long lda, long ldw, long ldy,
+                          long batch, long strideA, long strideW, long strideY, const tao_fp_model *model, void *stream);
+/* The same operator checked on the spot (Sec. 5.4 leaf check, Sec. 5.3 profile): *out receives exactly what
+ * tao_check_and_profile(claimed, y, tau, ...) returns for the y and tau of tao_bound_linear_int8, neither of which is
+ * stored.  y_ref: the verifier's own output to check against instead of y, or NULL.  y_ref, claimed: laid out like y.
+ * ws / ws_bytes: DEVICE scratch of at least tao_check_workspace_bytes(M * N * batch), 256-byte aligned.  Errors as
+ * for the two calls. */
+int tao_bound_check_linear_int8(const int8_t *A, const float *scale_a, const int8_t *W, const float *scale_w, const float *bias,
+                                const float *y_ref, const float *claimed, long M, long N, long K, long lda, long ldw, long ldy,
+                                long batch, long strideA, long strideW, long strideY, double alpha, double eps_rel,
+                                const tao_fp_model *model, tao_profile *out, void *ws, size_t ws_bytes, void *stream);
+/* The 8-bit operand of the product from binary32 activations: per row, with m = max |x|,
+ *     scale[r] = fl(m / 127),   q[r][c] = round(fl(x[r][c] / scale[r])) to the nearest whole number, ties to even, in [-127, 127].
+ * A row whose scale comes out as 0 (zeros; values below 127 2^-150) has q = 0; a row that is not finite has scale NaN and
+ * q = 0, so that its products are NaN, which no check admits.  Every step is one correctly rounded operation: the result is the same bit for
+ * bit in any implementation.  x: [rows][cols], row stride ld; q: row stride ldq; scale: [rows]. */
+int tao_quantize_rows(const float *x, int8_t *q, float *scale, long rows, long cols, long ld, long ldq, void *stream);
+
 /* 2-D convolution bound without a stored patch matrix (Sec. 3.1: conv is a
  * reduction with gamma_k of the output element; Conv2D of the operator list,
  * App. A.3):
@@ -347,6 +385,37 @@ int tao_bound_groupnorm(const float *x, const float *y_ref, const float *gamma, 
                         double eps, float *tau, long batch, long channels, long positions, long groups,
                         const tao_fp_model *model, void *ws, size_t ws_bytes, void *stream);
 size_t tao_groupnorm_workspace_bytes(long batch, long channels, long positions, long groups);
+
+/* GroupNorm with an activation on channels-last features x[batch][positions][channels] (the layout of tao_bound_conv2d;
+ * positions = product of the spatial extents), re-executed and bounded in one call.  Every (sample, group) is a LayerNorm over
+ * its channels/groups consecutive channels times all positions (n elements); with mu, r = 1/sqrt(var + eps), d = x - mu and
+ * E_p of tao_bound_norm's LAYERNORM chain,
+ *     p = d r gamma + beta,   E = E_p + u (|p| + E_p)                 (the last rounding, over every canonical execution),
+ *   act TAO_ACT_EXACT  y = p,                 tau = E                  (no activation)
+ *       TAO_ACT_RELU   y = max(p, 0),         tau = max(0, min(E, p + E))
+ *       TAO_ACT_SILU   y = s(p) = p/(1 + exp(-p)),  B = min(|s'(p)| E + E^2/4, 1.1 E),   tau = B + f/(1 - f) (|s(p)| + B),
+ *                      f the relative error of tao_bound_act's SILU (|s''| <= 1/2 and |s'| < 1.1 everywhere).
+ * y is the formula in binary64, rounded once to binary32; no re-executed output is needed for tau.  tau is at or above its formula's value and
+ * within 1e-6 of it (for RELU within 1e-6 E).  A group whose bound is not finite gets NaN, as in tao_bound_norm.
+ * x: pixel stride ldx >= channels; y, tau: pixel stride ldy; samples follow each other; either of y, tau may be NULL (not stored).  gamma, beta:
+ * [channels] or NULL.  16-byte vectors are used where channels, ldx and ldy are multiples of 4 and the tensors 16-byte aligned.
+ * ws / ws_bytes: DEVICE scratch of tao_groupnorm_act_workspace_bytes(...), 256-byte aligned, contents irrelevant before and
+ * garbage after; calls that share ws must be ordered on one stream.
+ * TAO_ERR_KIND for another act; TAO_ERR_SHAPE when channels is not a multiple of groups, a group has 2^31 elements or more, the
+ * tensor 2^36 or more, or the batch exceeds about 16 million samples; TAO_ERR_K_RANGE as for tao_bound_norm's LAYERNORM. */
+int tao_bound_groupnorm_act(int act, const float *x, const float *gamma, const float *beta, double eps, float *y, float *tau,
+                            long batch, long positions, long channels, long groups, long ldx, long ldy,
+                            const tao_fp_model *model, void *ws, size_t ws_bytes, void *stream);
+size_t tao_groupnorm_act_workspace_bytes(long batch, long positions, long channels, long groups);
+/* The same operator checked on the spot: *out receives what tao_check_and_profile(claimed, y, tau, ...) returns for the y and
+ * tau of tao_bound_groupnorm_act, neither of which is stored.  y_ref: the verifier's own output to check against instead of y, or NULL.
+ * y_ref, claimed: laid out like y (pixel stride ldy).  ws / ws_bytes: DEVICE scratch of
+ * tao_bound_check_groupnorm_act_workspace_bytes(...), 256-byte aligned. */
+int tao_bound_check_groupnorm_act(int act, const float *x, const float *gamma, const float *beta, double eps, const float *y_ref,
+                                  const float *claimed, long batch, long positions, long channels, long groups, long ldx, long ldy,
+                                  double alpha, double eps_rel, const tao_fp_model *model, tao_profile *out,
+                                  void *ws, size_t ws_bytes, void *stream);
+size_t tao_bound_check_groupnorm_act_workspace_bytes(long batch, long positions, long channels, long groups);
 
 /* Element-wise operators (App. A.3), flat length n.  y_ref is the verifier's
  * binary32 output and is always required.

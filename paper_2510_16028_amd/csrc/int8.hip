@@ -128,14 +128,16 @@ struct Int8Check {
     __device__ __forceinline__ void put(const Int8Args& p, long i, int cols, bool vec, intx4 S, float sa, floatv4 sw, floatv4 b, const Ahead& a) {
         floatv4 r;
         if (y_ref) r = quad_load(y_ref, i, cols, vec);
-        unsigned int bin[4];
+        unsigned int bin[4], out = 0;
         bool ok = true;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             float ye, te;
+            bool outside;
             const bool accurate = int8_output(S[e], sa, sw[e], b[e], BIAS, p, ye, te);
             if (!y_ref) r[e] = ye;
-            ok &= e >= cols || (accurate && quick_settled(a.c[e], r[e], te * q.alpha, q, known, bin[e]));
+            ok &= e >= cols || (quick_decided(a.c[e], r[e], te * q.alpha, q, known, bin[e], outside) && accurate);
+            out += e < cols && outside;
         }
         const int rep = threadIdx.x & (R - 1);
         if (ok) {
@@ -144,6 +146,7 @@ struct Int8Check {
                 if (e >= cols) continue;
                 if (bin[e] == 0) ++zeros; else atomicAdd(&hist[bin[e] * R + rep], 1u);
             }
+            acc.violations += out;
             return;
         }
 #pragma unroll 1
@@ -159,126 +162,34 @@ struct Int8Check {
     __device__ __forceinline__ void finish() { if (zeros) atomicAdd(&hist[threadIdx.x & (R - 1)], zeros); }
 };
 
-// ---- few rows: a workgroup of 16 wavefronts takes all of up to 16 MT rows of A with 16 NT rows of W; the wavefronts share out the
-// reduction in chunks of 64 columns and add their sums in LDS, in whole numbers, so in any order.  Operands go from memory to
-// registers in the layout of v_mfma_i32_16x16x64_i8 (lane: row lane % 16, columns 16 (lane / 16) on); the order of the columns inside
-// a chunk does not matter, as both operands have the same.
-constexpr int kInt8Threads = kCheckThreads;
-template <int MT, int NT>
-struct Int8Tile {
-    static constexpr int ROWS = 16 * MT, COLS = 16 * NT;
-    __align__(16) int sums[ROWS * COLS];
-};
-template <int MT, int NT>
-__device__ __forceinline__ void int8_sums(const Int8Args& p, Int8Tile<MT, NT>& t, long z, long m0, long n0) {
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-    constexpr int WAVES = kInt8Threads / kWave;
-    for (int i = tid; i < t.ROWS * t.COLS; i += kInt8Threads) t.sums[i] = 0;
-    __syncthreads();
-    const signed char* a[MT];
-    const signed char* w[NT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) a[i] = p.A + z * p.strideA + min(m0 + i * 16 + (lane & 15), p.M - 1) * p.lda;
-#pragma unroll
-    for (int j = 0; j < NT; ++j) w[j] = p.W + z * p.strideW + min(n0 + j * 16 + (lane & 15), p.N - 1) * p.ldw;
-    intx4 acc[MT][NT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = intx4{0, 0, 0, 0};
-    for (long c = wave; c * 64 < p.K; c += WAVES) {
-        const long k = c * 64 + (lane >> 4) * 16;
-        intx4 av[MT], wv[NT];
-#pragma unroll
-        for (int i = 0; i < MT; ++i) av[i] = row16(a[i], k, p.K);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) wv[j] = row16(w[j], k, p.K);
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(av[i], wv[j], acc[i][j], 0, 0, 0);
-    }
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) atomicAdd(&t.sums[(i * 16 + (lane >> 4) * 4 + v) * t.COLS + j * 16 + (lane & 15)], acc[i][j][v]);
-    __syncthreads();
-}
-template <int MT, int NT, class Sink>
-__device__ __forceinline__ void int8_few_body(const Int8Args& p, Sink& sink, Int8Tile<MT, NT>& t) {
-    const long tm = (p.M + t.ROWS - 1) / t.ROWS, tn = (p.N + t.COLS - 1) / t.COLS, tiles = tm * tn * p.batch;
-    for (long at = blockIdx.x; at < tiles; at += gridDim.x) {
-        const long z = at / (tm * tn), in = at - z * (tm * tn), m0 = in % tm * t.ROWS, n0 = in / tm * t.COLS;
-        int8_sums(p, t, z, m0, n0);
-        const float* sa = p.sa + z * p.M;
-        const float* sw = p.sw + (p.strideW ? z * p.N : 0);
-        for (int e = threadIdx.x; e < t.ROWS * t.COLS / 4; e += kInt8Threads) {
-            const int row = e / (t.COLS / 4), col = e % (t.COLS / 4) * 4;
-            const long m = m0 + row, n = n0 + col, left = p.N - n;
-            if (m >= p.M || left <= 0) continue;
-            const int cols = left < 4 ? (int)left : 4;
-            const bool vec = p.vec && cols == 4;
-            const long i = z * p.strideY + m * p.ldy + n;
-            const auto ahead = sink.request(i, cols, vec);
-            floatv4 w4, b4 = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                w4[c] = sw[min(n + c, p.N - 1)];
-                if (p.bias) b4[c] = p.bias[min(n + c, p.N - 1)];
-            }
-            const intx4 S = *reinterpret_cast<const intx4*>(&t.sums[row * t.COLS + col]);
-            if (p.bias) sink.template put<true>(p, i, cols, vec, S, sa[m], w4, b4, ahead);
-            else        sink.template put<false>(p, i, cols, vec, S, sa[m], w4, b4, ahead);
-        }
-        __syncthreads();
-    }
-}
-template <int MT, int NT>
-__global__ __launch_bounds__(kInt8Threads) void int8_few(Int8Args p) {
-    __shared__ Int8Tile<MT, NT> t;
-    Int8Store sink;
-    int8_few_body(p, sink, t);
-}
-template <int MT, int NT>
-__global__ __launch_bounds__(kInt8Threads) void int8_few_check(Int8Args p, const float* y_ref, const float* claimed, double alpha, double eps_rel, float quick, PassOut pass) {
-    __shared__ Int8Tile<MT, NT> t;
-    __shared__ unsigned int hist[kBins * kReplicas];
-    __shared__ unsigned int red[kRedWords];
-    __shared__ unsigned int largest;
-    for (int i = threadIdx.x; i < kBins * kReplicas; i += kInt8Threads) hist[i] = 0;
-    if (threadIdx.x == 0) largest = 0;
-    Int8Check<kReplicas> sink(y_ref, claimed, alpha, eps_rel, quick, hist, &largest);
-    int8_few_body(p, sink, t);
-    sink.finish();
-    __syncthreads();
-    finish_pass(hist, sink.acc, red, pass);
-}
-
-// ---- many rows: a workgroup of 8 wavefronts takes BM x BN outputs, 128 columns of the reduction a stage, two stages in LDS: one is
-// multiplied by v_mfma_i32_32x32x32_i8 while the next is on its way.  A stage holds rows of 128 bytes, whose 16-byte units lie at
-// place unit ^ (row & 7): the eight rows that a read of a fragment touches at a time then lie in different banks.
-// A wavefront takes WM x WN outputs, so that a fragment read from LDS serves WN / 32 or WM / 32 instructions.
+// ---- the product: a workgroup takes BM x BN outputs and walks the reduction in slabs of KB columns, of which STAGES lie in LDS: one is
+// multiplied by v_mfma_i32_32x32x32_i8 while the next ones are on their way.  A slab holds rows of KB bytes, whose 16-byte units are
+// permuted by the row (unit ^ row & 7, or unit ^ row / 2 & 3 for rows of four units): the eight rows that a read of a fragment touches at
+// a time then lie in different banks.  A wavefront takes WM x WN outputs, so that a fragment serves WN / 32 or WM / 32 instructions, and reads
+// the fragments of one step while it multiplies those of the one before, across the slabs' borders too: the barrier of a slab stands before
+// its last step, when all its fragments are in registers and the slab behind it has landed.
+// GROUPS: where there are fewer tiles than compute units, several groups of wavefronts of a workgroup share out the reduction, each with
+// stages of its own, and their sums are added at the end.
 // DIRECT: rows of whole units on 16-byte addresses go from memory to LDS without a stop in registers (global_load_lds_dwordx4: lane i's 16 bytes
 // land at the wavefront's place + 16 i; an address in scalar registers and a 32-bit offset, as 64-bit addresses per lane stall the SIMD next
-// to matrix instructions).  Otherwise they are read from any address into registers while the previous stage is multiplied, then written to LDS.
+// to matrix instructions).  Otherwise they are read from any address into registers while a slab is multiplied, then written to LDS.
 typedef int intx16 __attribute__((ext_vector_type(16)));
-constexpr int kSlabK = 128;
 static __device__ __align__(16) const int zero_unit[4] = {0, 0, 0, 0};
 
-template <int BM_, int BN_, int WM_, int WN_>
+template <int BM_, int BN_, int WM_, int WN_, int KB_, int STAGES_, int GROUPS_ = 1>
 struct Int8Shape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, RM = WM / 32, RN = WN / 32;
-    static constexpr int WAVES = (BM / WM) * (BN / WN), THREADS = WAVES * kWave;
-    static constexpr int NA = BM / 8 / WAVES, NW = BN / 8 / WAVES;           // pieces of 8 rows that a wavefront copies
-    static constexpr int STAGE = (BM + BN) * kSlabK;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KB = KB_, STAGES = STAGES_, GROUPS = GROUPS_, RM = WM / 32, RN = WN / 32;
+    static constexpr int WAVES = (BM / WM) * (BN / WN), THREADS = WAVES * GROUPS * kWave;      // of a group, of the workgroup
+    static constexpr int UNITS = KB / 16, STEPS = KB / 32, PIECE = kWave / UNITS;      // units of a row, matrix steps of a slab, rows that a wavefront copies at a time
+    static constexpr int NA = BM / PIECE / WAVES, NW = BN / PIECE / WAVES;
+    static constexpr int STAGE = (BM + BN) * KB, LDS = STAGES * STAGE * GROUPS;
     static constexpr int SCALES = (BM + 2 * BN) * 4;                         // of the tile's rows and columns, and the bias
+    static_assert(NA * PIECE * WAVES == BM && NW * PIECE * WAVES == BN && (UNITS == 4 || UNITS == 8), "whole pieces");
 };
 
 // Tiles in the order in which workgroups take them: the eight dies (workgroup modulo 8) have consecutive shares, inside which four
 // tile rows go along together, so that what one die reads at a time shares rows of A and W in its L2.
-struct Int8Grid { unsigned tm, tn, batch, tiles, share; };
+struct Int8Grid { unsigned tm, tn, tiles, share; };
 __device__ __forceinline__ bool locate(const Int8Grid& g, unsigned t, unsigned& m, unsigned& n, unsigned& z) {
     unsigned at = (t & 7) * g.share + (t >> 3);
     if (at >= g.tiles) return false;
@@ -289,46 +200,53 @@ __device__ __forceinline__ bool locate(const Int8Grid& g, unsigned t, unsigned& 
     return true;
 }
 
+// s_waitcnt: at most n copies from memory on their way, and no access to LDS
+__device__ __forceinline__ constexpr int at_most(int n) { return 0x0070 | (n & 15) | (n >> 4 << 14); }
 template <class SH, bool DIRECT>
 struct Int8Walk {
     const Int8Args& p;
-    char* lds;
-    int lane, wave;
+    char* lds;                                               // the group's stages
+    int lane, wave, group;                                   // (wavefront of the group)
     // of the tile: operand rows of this lane's pieces
     const signed char* A; const signed char* W;              // first rows of the tile (scalar)
     unsigned offA[SH::NA], offW[SH::NW];                     // DIRECT: byte offsets of this lane's unit from there
     long rowA[SH::NA], rowW[SH::NW];                         // otherwise the rows' offsets
     int unit;                                                // this lane's unit of a row
     intx4 held[DIRECT ? 1 : SH::NA + SH::NW];
+    struct Fragments { intx4 a[SH::RM], w[SH::RN]; };
 
-    __device__ __forceinline__ Int8Walk(const Int8Args& p_, char* lds_) : p(p_), lds(lds_) {
+    static __device__ __forceinline__ int turn(int row) { return SH::UNITS == 8 ? row & 7 : row >> 1 & 3; }
+    __device__ __forceinline__ Int8Walk(const Int8Args& p_, char* lds_) : p(p_) {
         const int tid = threadIdx.x;
         lane = tid & (kWave - 1);
         wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-        unit = (lane & 7) ^ (lane >> 3);                     // (row & 7 is lane / 8 in every piece)
+        group = wave / SH::WAVES;
+        wave -= group * SH::WAVES;
+        lds = lds_ + group * SH::STAGES * SH::STAGE;
+        unit = (lane % SH::UNITS) ^ turn(lane / SH::UNITS);  // (pieces begin at multiples of eight rows)
     }
     __device__ __forceinline__ void start(long z, long m0, long n0) {
         A = p.A + z * p.strideA + m0 * p.lda;
         W = p.W + z * p.strideW + n0 * p.ldw;
 #pragma unroll
         for (int i = 0; i < SH::NA; ++i) {
-            const long r = min((long)((wave + i * SH::WAVES) * 8 + (lane >> 3)), p.M - 1 - m0);       // (rows beyond the last repeat it)
+            const long r = min((long)((wave + i * SH::WAVES) * SH::PIECE + lane / SH::UNITS), p.M - 1 - m0);       // (rows beyond the last repeat it)
             if (DIRECT) offA[i] = (unsigned)(r * p.lda) + unit * 16; else rowA[i] = r * p.lda;
         }
 #pragma unroll
         for (int i = 0; i < SH::NW; ++i) {
-            const long r = min((long)((wave + i * SH::WAVES) * 8 + (lane >> 3)), p.N - 1 - n0);
+            const long r = min((long)((wave + i * SH::WAVES) * SH::PIECE + lane / SH::UNITS), p.N - 1 - n0);
             if (DIRECT) offW[i] = (unsigned)(r * p.ldw) + unit * 16; else rowW[i] = r * p.ldw;
         }
     }
     __device__ __forceinline__ unsigned place(int stage, int piece) const {
         return (unsigned)(size_t)(__attribute__((address_space(3))) char*)lds + (unsigned)(stage * SH::STAGE + piece * 1024);
     }
-    // columns k .. k + 127 into stage `stage`; units from column K on become 0
-    __device__ __forceinline__ void request(int stage, long k) {
+    // columns k .. k + KB - 1 into stage `stage` (DIRECT) or into registers; units from column K on become 0
+    __device__ __forceinline__ void request(int stage, int k) {
         if constexpr (DIRECT) {
             // (written as assembly: the compiler would wait for these copies before every barrier; the waits are the explicit ones in the loop)
-            if (k + kSlabK <= p.K) {
+            if (k + SH::KB <= p.K) {
                 const signed char* a = A + k;
                 const signed char* w = W + k;
 #pragma unroll
@@ -336,7 +254,7 @@ struct Int8Walk {
                     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(place(stage, wave + i * SH::WAVES)), "v"(offA[i]), "s"(a) : "memory");
 #pragma unroll
                 for (int i = 0; i < SH::NW; ++i)
-                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(place(stage, SH::BM / 8 + wave + i * SH::WAVES)), "v"(offW[i]), "s"(w) : "memory");
+                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(place(stage, SH::BM / SH::PIECE + wave + i * SH::WAVES)), "v"(offW[i]), "s"(w) : "memory");
             } else {
                 const bool in = k + unit * 16 < p.K;         // (K is a whole number of units)
                 const char* zero = reinterpret_cast<const char*>(zero_unit);
@@ -347,7 +265,7 @@ struct Int8Walk {
 #pragma unroll
                 for (int i = 0; i < SH::NW; ++i)
                     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-                                 :: "s"(place(stage, SH::BM / 8 + wave + i * SH::WAVES)), "v"(in ? reinterpret_cast<const char*>(W + k) + offW[i] : zero) : "memory");
+                                 :: "s"(place(stage, SH::BM / SH::PIECE + wave + i * SH::WAVES)), "v"(in ? reinterpret_cast<const char*>(W + k) + offW[i] : zero) : "memory");
             }
         } else {
 #pragma unroll
@@ -356,46 +274,83 @@ struct Int8Walk {
             for (int i = 0; i < SH::NW; ++i) held[SH::NA + i] = row16(W + rowW[i], k + unit * 16, p.K);
         }
     }
-    // DIRECT: what was requested has landed (of this wavefront); otherwise it is written
-    __device__ __forceinline__ void commit(int stage) {
-        if constexpr (DIRECT) {
-            __builtin_amdgcn_s_waitcnt(0x0F70);              // vmcnt(0)
-        } else {
+    __device__ __forceinline__ void write(int stage) const {
 #pragma unroll
-            for (int i = 0; i < SH::NA; ++i) *reinterpret_cast<intx4*>(lds + stage * SH::STAGE + (wave + i * SH::WAVES) * 1024 + lane * 16) = held[i];
+        for (int i = 0; i < SH::NA; ++i) *reinterpret_cast<intx4*>(lds + stage * SH::STAGE + (wave + i * SH::WAVES) * 1024 + lane * 16) = held[i];
 #pragma unroll
-            for (int i = 0; i < SH::NW; ++i)
-                *reinterpret_cast<intx4*>(lds + stage * SH::STAGE + (SH::BM / 8 + wave + i * SH::WAVES) * 1024 + lane * 16) = held[SH::NA + i];
-        }
+        for (int i = 0; i < SH::NW; ++i)
+            *reinterpret_cast<intx4*>(lds + stage * SH::STAGE + (SH::BM / SH::PIECE + wave + i * SH::WAVES) * 1024 + lane * 16) = held[SH::NA + i];
     }
-    __device__ __forceinline__ void multiply(int stage, intx16 (&acc)[SH::RM][SH::RN]) const {
+    __device__ __forceinline__ void read(Fragments& f, int stage, int step) const {
         constexpr int WC = SH::BN / SH::WN;
-        const char* a = lds + stage * SH::STAGE + ((wave / WC) * SH::WM + (lane & 31)) * kSlabK;
-        const char* w = lds + stage * SH::STAGE + (SH::BM + (wave % WC) * SH::WN + (lane & 31)) * kSlabK;
+        const int row = lane & 31, at = row * SH::KB + ((2 * step + (lane >> 5)) ^ turn(row)) * 16;
+        const char* a = lds + stage * SH::STAGE + (wave / WC) * SH::WM * SH::KB + at;
+        const char* w = lds + stage * SH::STAGE + (SH::BM + (wave % WC) * SH::WN) * SH::KB + at;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int at = ((2 * s + (lane >> 5)) ^ (lane & 7)) * 16;
-            intx4 av[SH::RM], wv[SH::RN];
+        for (int i = 0; i < SH::RM; ++i) f.a[i] = *reinterpret_cast<const intx4*>(a + i * 32 * SH::KB);
 #pragma unroll
-            for (int i = 0; i < SH::RM; ++i) av[i] = *reinterpret_cast<const intx4*>(a + i * 32 * kSlabK + at);
+        for (int j = 0; j < SH::RN; ++j) f.w[j] = *reinterpret_cast<const intx4*>(w + j * 32 * SH::KB);
+    }
+    static __device__ __forceinline__ void multiply(const Fragments& f, intx16 (&acc)[SH::RM][SH::RN]) {
 #pragma unroll
-            for (int j = 0; j < SH::RN; ++j) wv[j] = *reinterpret_cast<const intx4*>(w + j * 32 * kSlabK + at);
+        for (int i = 0; i < SH::RM; ++i)
 #pragma unroll
-            for (int i = 0; i < SH::RM; ++i)
+            for (int j = 0; j < SH::RN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f.a[i], f.w[j], acc[i][j], 0, 0, 0);
+    }
+    // all of this wavefront's copies but those of the newest SLABS slabs have landed, and its reads of LDS have ended: behind a barrier everybody's
+    template <int SLABS>
+    static __device__ __forceinline__ void landed() { __builtin_amdgcn_s_waitcnt(at_most(SLABS * (SH::NA + SH::NW))); }
+    // the group's share of the reduction: `slabs` slabs (the same number for every group, which meet at the barriers; beyond K all is 0)
+    __device__ __forceinline__ void sums(intx16 (&acc)[SH::RM][SH::RN], int slabs) {
+        constexpr int S = SH::STAGES;
+        const int k0 = group * slabs * SH::KB;
+        if constexpr (DIRECT) {
 #pragma unroll
-                for (int j = 0; j < SH::RN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(av[i], wv[j], acc[i][j], 0, 0, 0);
+            for (int s = 0; s < S; ++s) if (s < slabs) request(s, k0 + s * SH::KB);
+            if (slabs >= S) landed<S - 1>(); else landed<0>();
+        } else {
+            request(0, k0);
+            write(0);
+        }
+        __syncthreads();
+        Fragments f[2];
+        read(f[0], 0, 0);
+        int stage = 0;
+        for (int g = 0; g < slabs; ++g) {
+            const int next = stage + 1 == S ? 0 : stage + 1;
+            if (!DIRECT && g + 1 < slabs) request(next, k0 + (g + 1) * SH::KB);
+#pragma unroll
+            for (int s = 0; s + 1 < SH::STEPS; ++s) {
+                read(f[(s + 1) & 1], stage, s + 1);
+                multiply(f[s & 1], acc);
+            }
+            __builtin_amdgcn_s_waitcnt(at_most(63));         // (on either way: else the last step would wait for the next slab's fragments)
+            if (g + 1 < slabs) {
+                if constexpr (DIRECT) {
+                    if (g + S <= slabs) landed<S - 2>(); else landed<0>();
+                } else {
+                    write(next);
+                }
+                __syncthreads();                             // the next slab is whole; of this one all fragments are in registers
+                if (DIRECT && g + S < slabs) request(stage, k0 + (g + S) * SH::KB);
+                read(f[0], next, 0);
+            }
+            multiply(f[1], acc);
+            stage = next;
         }
     }
 };
 // The sums of a tile by way of LDS (the stages' memory, a half of the rows at a time where that is what fits) to threads that have four
 // neighbouring columns each, so that outputs and claims move as vectors; claims are requested AHEAD rows of a thread before they are needed.
-template <class SH, bool BIAS, class Sink>
-__device__ __forceinline__ void int8_outputs(const Int8Args& p, const intx16 (&acc)[SH::RM][SH::RN], int lane, int wave, long z, long m0, long n0,
+template <class SH, bool BIAS, class Walk, class Sink>
+__device__ __forceinline__ void int8_outputs(const Int8Args& p, const intx16 (&acc)[SH::RM][SH::RN], const Walk& walk, long z, long m0, long n0,
                                              char* lds, const float* scales, Sink& sink) {
-    constexpr int WC = SH::BN / SH::WN, PARTS = SH::BM * SH::BN * 4 / (2 * SH::STAGE), RP = SH::RM / PARTS, BAND = SH::WM / PARTS;
-    constexpr int QUADS = SH::BN / 4, STEP = SH::THREADS / QUADS, TRIPS = SH::BM / PARTS / STEP, AHEAD = Sink::AHEAD;
-    static_assert(PARTS * 2 * SH::STAGE == SH::BM * SH::BN * 4, "a part of the tile fills the stages");
-    int* sums = reinterpret_cast<int*>(lds);
+    const int lane = walk.lane, wave = walk.wave;
+    constexpr int WC = SH::BN / SH::WN, PARTS = (SH::BM * SH::BN * 4 + SH::STAGES * SH::STAGE - 1) / (SH::STAGES * SH::STAGE), RP = SH::RM / PARTS, BAND = SH::WM / PARTS;
+    constexpr int QUADS = SH::BN / 4, STEP = SH::THREADS / QUADS, ROWS = SH::BM / PARTS, TRIPS = (ROWS + STEP - 1) / STEP, AHEAD = Sink::AHEAD;
+    static_assert(SH::RM % PARTS == 0 && STEP > 0, "whole blocks a part, whole rows a trip");
+    const int* sums = reinterpret_cast<const int*>(lds);     // [group][row][column], a group's in its own stages
+    int* mine = reinterpret_cast<int*>(walk.lds);
     const int col = threadIdx.x % QUADS * 4, row0 = threadIdx.x / QUADS;
     const long left = p.N - n0 - col;
     const int cols = (int)max(min(left, 4L), 0L);
@@ -413,33 +368,36 @@ __device__ __forceinline__ void int8_outputs(const Int8Args& p, const intx16 (&a
             for (int j = 0; j < SH::RN; ++j)
 #pragma unroll
                 for (int v = 0; v < 16; ++v)
-                    sums[((wave / WC) * BAND + i * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) * SH::BN + (wave % WC) * SH::WN + j * 32 + (lane & 31)] = acc[part * RP + i][j][v];
+                    mine[((wave / WC) * BAND + i * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) * SH::BN + (wave % WC) * SH::WN + j * 32 + (lane & 31)] = acc[part * RP + i][j][v];
         __syncthreads();
         typename Sink::Ahead ahead[AHEAD];
         auto ask = [&](int trip) __attribute__((always_inline)) {
             const int row = row_of(row0 + trip * STEP);
-            const bool inside = trip < TRIPS && m0 + row < p.M;
+            const bool inside = row0 + trip * STEP < ROWS && m0 + row < p.M;
             return sink.request(inside ? base + row * p.ldy : 0, inside ? cols : 0, inside && vec);
         };
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a) ahead[a] = ask(a);
 #pragma unroll Sink::UNROLL
         for (int trip = 0; trip < TRIPS; ++trip) {
-            const typename Sink::Ahead mine = ahead[0];
+            const typename Sink::Ahead claims = ahead[0];
 #pragma unroll
             for (int a = 0; a + 1 < AHEAD; ++a) ahead[a] = ahead[a + 1];
             ahead[AHEAD - 1] = ask(trip + AHEAD);
             const int r = row0 + trip * STEP, row = row_of(r);
-            if (m0 + row >= p.M || cols == 0) continue;
-            sink.template put<BIAS>(p, base + row * p.ldy, cols, vec, *reinterpret_cast<const intx4*>(sums + r * SH::BN + col), scales[row], sw, b, mine);
+            if (r >= ROWS || m0 + row >= p.M || cols == 0) continue;
+            intx4 S = *reinterpret_cast<const intx4*>(sums + r * SH::BN + col);
+#pragma unroll
+            for (int g = 1; g < SH::GROUPS; ++g) S += *reinterpret_cast<const intx4*>(sums + g * (SH::STAGES * SH::STAGE / 4) + r * SH::BN + col);
+            sink.template put<BIAS>(p, base + row * p.ldy, cols, vec, S, scales[row], sw, b, claims);
         }
     }
 }
 template <class SH, bool DIRECT, class Sink>
 __device__ __forceinline__ void int8_tiles_body(const Int8Args& p, const Int8Grid& grid, Sink& sink, char* lds) {
     Int8Walk<SH, DIRECT> walk(p, lds);
-    float* scales = reinterpret_cast<float*>(lds + 2 * SH::STAGE);           // [BM], [BN], bias [BN]
-    const int slabs = (int)((p.K + kSlabK - 1) / kSlabK);
+    float* scales = reinterpret_cast<float*>(lds + SH::LDS);              // [BM], [BN], bias [BN]
+    const int slabs = (int)((p.K + SH::KB * SH::GROUPS - 1) / (SH::KB * SH::GROUPS));
     for (unsigned t = blockIdx.x; (t >> 3) < grid.share; t += gridDim.x) {
         unsigned tm, tn, z;
         if (!locate(grid, t, tm, tn, z)) continue;
@@ -452,23 +410,15 @@ __device__ __forceinline__ void int8_tiles_body(const Int8Args& p, const Int8Gri
             for (int j = 0; j < SH::RN; ++j)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[i][j][v] = 0;
-        if (slabs > 0) walk.request(0, 0);
         for (int i = threadIdx.x; i < SH::BM; i += SH::THREADS) scales[i] = p.sa[z * p.M + min(m0 + i, p.M - 1)];
         for (int i = threadIdx.x; i < SH::BN; i += SH::THREADS) {
             const long n = min(n0 + i, p.N - 1);
             scales[SH::BM + i] = p.sw[(p.strideW ? z * p.N : 0) + n];
             scales[SH::BM + SH::BN + i] = p.bias ? p.bias[n] : 0.f;
         }
-        for (int g = 0; g < slabs; ++g) {
-            if (DIRECT || g == 0) walk.commit(g & 1);
-            __syncthreads();                                 // stage g is whole, and nobody reads the other one any more
-            if (g + 1 < slabs) walk.request((g + 1) & 1, (long)(g + 1) * kSlabK);
-            walk.multiply(g & 1, acc);
-            if (!DIRECT && g + 1 < slabs) walk.commit((g + 1) & 1);
-        }
-        if (slabs == 0) __syncthreads();                     // (the scales are in place)
-        if (p.bias) int8_outputs<SH, true>(p, acc, walk.lane, walk.wave, z, m0, n0, lds, scales, sink);
-        else        int8_outputs<SH, false>(p, acc, walk.lane, walk.wave, z, m0, n0, lds, scales, sink);
+        if (slabs > 0) walk.sums(acc, slabs); else __syncthreads();          // (the scales are in place behind a barrier)
+        if (p.bias) int8_outputs<SH, true>(p, acc, walk, z, m0, n0, lds, scales, sink);
+        else        int8_outputs<SH, false>(p, acc, walk, z, m0, n0, lds, scales, sink);
         __syncthreads();                                     // (the scales and the stages are the next tile's)
     }
 }
@@ -483,7 +433,7 @@ template <class SH, bool DIRECT>
 __global__ __launch_bounds__(SH::THREADS) void int8_tiles_check(Int8Args p, Int8Grid grid, const float* y_ref, const float* claimed, double alpha, double eps_rel,
                                                                 float quick, CheckWorkspace w) {
     extern __shared__ __align__(16) char lds[];
-    unsigned int* hist = reinterpret_cast<unsigned int*>(lds + 2 * SH::STAGE + SH::SCALES);
+    unsigned int* hist = reinterpret_cast<unsigned int*>(lds + SH::LDS + SH::SCALES);
     unsigned int* rest = hist + kBins * kTileReplicas;       // largest error, three counters of every wavefront
     const int tid = threadIdx.x, wave = tid / kWave;
     for (int i = tid; i < kBins * kTileReplicas; i += SH::THREADS) hist[i] = 0;
@@ -498,18 +448,23 @@ __global__ __launch_bounds__(SH::THREADS) void int8_tiles_check(Int8Args p, Int8
     if (tid == 0) {
         unsigned long long vs = 0, qs = 0;
         unsigned int ms = 0;
-        for (int i = 0; i < SH::WAVES; ++i) { vs += rest[4 + i * 3]; qs += rest[4 + i * 3 + 1]; ms = max(ms, rest[4 + i * 3 + 2]); }
+        for (int i = 0; i < SH::THREADS / kWave; ++i) { vs += rest[4 + i * 3]; qs += rest[4 + i * 3 + 1]; ms = max(ms, rest[4 + i * 3 + 2]); }
         BlockStats& o = w.stats[blockIdx.x];
         o.violations = vs; o.nans = qs; o.max_bits = ms;
     }
     flush_histogram<kTileReplicas>(hist, w.hist + (size_t)blockIdx.x * kBins, w.coarse + blockIdx.x * kGroups);
 }
 template <class SH> constexpr int tile_lds(bool check) {
-    return 2 * SH::STAGE + SH::SCALES + (check ? kBins * kTileReplicas * 4 + (4 + 3 * SH::WAVES) * 4 : 0);
+    return SH::LDS + SH::SCALES + (check ? kBins * kTileReplicas * 4 + (4 + 3 * SH::THREADS / kWave) * 4 : 0);
 }
-typedef Int8Shape<256, 256, 128, 64> Int8Wide;
-typedef Int8Shape<128, 128, 64, 32> Int8Mid;
-static_assert(Int8Wide::THREADS == 512 && Int8Mid::THREADS == 512 && tile_lds<Int8Wide>(true) <= 160 * 1024, "one workgroup a compute unit");
+typedef Int8Shape<32, 32, 32, 32, 128, 2, 8> Int8Tiny;                       // 136 KB of LDS
+typedef Int8Shape<32, 64, 32, 32, 128, 3, 4> Int8Flat;                       // 144 KB; 96 where the check's histogram has to fit
+typedef Int8Shape<32, 64, 32, 32, 128, 2, 4> Int8FlatCheck;
+typedef Int8Shape<64, 64, 32, 32, 128, 2, 2> Int8Small;                      // 64 KB: two workgroups a compute unit
+typedef Int8Shape<128, 128, 64, 32, 128, 2> Int8Mid;                         // 64 KB
+typedef Int8Shape<256, 256, 128, 64, 128, 2> Int8Wide;                       // 128 KB
+static_assert(tile_lds<Int8Tiny>(true) <= 160 * 1024 && tile_lds<Int8FlatCheck>(true) <= 160 * 1024 && tile_lds<Int8Flat>(false) <= 160 * 1024 &&
+              tile_lds<Int8Wide>(true) <= 160 * 1024, "a compute unit's LDS");
 
 // ---- quantisation of rows: scale = fl(max|x| / 127), q = round(fl(x / scale)), ties to even.  A row that is not finite has scale NaN
 // and q = 0 (so the product is NaN, which no check admits); a row of zeros, or one so small that its scale rounds to 0, scale 0 and q = 0.
@@ -574,34 +529,39 @@ static int int8_setup(const int8_t* A, const float* scale_a, const int8_t* W, co
     return TAO_OK;
 }
 
-// Which kernel: `few` where the rows are few or the outputs too few to give every compute unit a tile of 128 x 128; of the tiles the large ones
-// where there are enough of them.
-enum { kFewTiny, kFewTall, kFewSquare, kMidTiles, kWideTiles };
+// Which tiles: the smallest ones that one round of the compute units takes, their groups sharing out the reduction; 64 x 64 from there on, 128 x 128
+// from three quarters of a round of those on, 256 x 256 where its whole rounds are less than those of 128 x 128 (a tile of four times the size in about
+// 3.5 times the time).  Measured on 256 units, us, output and bound stored: 64 x 4096 x 4096 (M x K x N) 32 x 32 6.6, 32 x 64 7.8, 64 x 64 10.2, 128 x 128 20.8;
+// 8 x 4096 x 12288 13.8, 11.1, 13.6, 22.8; 128 x 4096 x 4096 11.4, 8.3, 10.5, 22.1; 64 x 4096 x 12288 19.0, 16.1, 14.6, 24.1; 512 x 4096 x 4096 43.5, 30.1,
+// 18.0, 24.0; 1536 x 4096 x 4096 64 x 64 51.0, 128 x 128 39.8, 256 x 256 60.9; 4096 x 4096 x 4096 128 x 128 91, 256 x 256 80;
+// 2048 x 4096 x 12288 132, 141; 8192 x 8192 x 8192 637, 542.
+enum { kTinyTiles, kFlatTiles, kSmallTiles, kMidTiles, kWideTiles };
 static int int8_kind(const Int8Args& p) {
     auto tiles = [&](long bm, long bn) { return (double)((p.M + bm - 1) / bm) * (double)((p.N + bn - 1) / bn) * (double)p.batch; };
-    if (p.M <= 16) return kFewTiny;
-    if (p.M <= 64) return kFewTall;
-    const int cus = device_cus();
-    if (tiles(256, 256) >= cus / 2) return kWideTiles;
-    if (tiles(128, 128) >= cus / 2) return kMidTiles;
-    return tiles(64, 64) >= cus / 2 ? kFewSquare : kFewTall;
+    const double cus = device_cus();
+    if (tiles(32, 32) <= cus) return kTinyTiles;
+    if (tiles(32, 64) <= cus) return kFlatTiles;
+    if (tiles(128, 128) < 0.75 * cus) return kSmallTiles;
+    return std::ceil(tiles(256, 256) / cus) * 3.5 < tiles(128, 128) / cus ? kWideTiles : kMidTiles;
 }
 template <class SH> static bool int8_grid(const Int8Args& p, Int8Grid* g) {
     const long tm = (p.M + SH::BM - 1) / SH::BM, tn = (p.N + SH::BN - 1) / SH::BN;
     const __int128 tiles = (__int128)tm * tn * p.batch;
     if (tiles >= (1L << 31) - 8) return false;
-    g->tm = (unsigned)tm; g->tn = (unsigned)tn; g->batch = (unsigned)p.batch; g->tiles = (unsigned)tiles; g->share = (unsigned)((tiles + 7) / 8);
+    g->tm = (unsigned)tm; g->tn = (unsigned)tn; g->tiles = (unsigned)tiles; g->share = (unsigned)((tiles + 7) / 8);
     return true;
 }
 // (a lane's offset inside the tile has 32 bits)
 static bool int8_direct(const Int8Args& p, int rows) {
     return p.K % 16 == 0 && p.lda % 16 == 0 && p.ldw % 16 == 0 && p.strideA % 16 == 0 && p.strideW % 16 == 0 && aligned(p.A, 16) && aligned(p.W, 16) &&
-           (p.lda + kSlabK) * rows < (1L << 31) && (p.ldw + kSlabK) * rows < (1L << 31);
+           (p.lda + 128) * rows < (1L << 31) && (p.ldw + 128) * rows < (1L << 31);
 }
 template <class K> static hipError_t allow_lds(K kernel, int bytes) {
     return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
-template <class SH> static int int8_launch_tiles(const Int8Args& p, const Int8Grid& g, hipStream_t st) {
+template <class SH> static int int8_launch_tiles(const Int8Args& p, hipStream_t st) {
+    Int8Grid g;
+    if (!int8_grid<SH>(p, &g)) return TAO_ERR_SHAPE;
     static OncePerDevice once;
     const hipError_t e = once.run([] {
         const hipError_t e = allow_lds(int8_tiles<SH, true>, tile_lds<SH>(false));
@@ -609,21 +569,27 @@ template <class SH> static int int8_launch_tiles(const Int8Args& p, const Int8Gr
     });
     if (e != hipSuccess) { g_last_hip_error = (int)e; return TAO_ERR_LAUNCH; }
     const dim3 grid(g.share * 8 < (1u << 22) ? g.share * 8 : 1u << 22), blk(SH::THREADS);
-    if (int8_direct(p, SH::BM)) hipLaunchKernelGGL((int8_tiles<SH, true>), grid, blk, tile_lds<SH>(false), st, p, g);
-    else                        hipLaunchKernelGGL((int8_tiles<SH, false>), grid, blk, tile_lds<SH>(false), st, p, g);
+    if (int8_direct(p, SH::BM > SH::BN ? SH::BM : SH::BN)) hipLaunchKernelGGL((int8_tiles<SH, true>), grid, blk, tile_lds<SH>(false), st, p, g);
+    else hipLaunchKernelGGL((int8_tiles<SH, false>), grid, blk, tile_lds<SH>(false), st, p, g);
     return launch_status();
 }
-template <class SH> static int int8_launch_check(const Int8Args& p, const Int8Grid& g, int nblocks, const float* y_ref, const float* claimed, double alpha, double eps_rel,
-                                                 float quick, const CheckWorkspace& w, hipStream_t st) {
+struct Int8CheckArgs { const float* y_ref; const float* claimed; double alpha, eps_rel; float quick; CheckWorkspace w; long n; tao_profile* out; };
+template <class SH> static int int8_launch_check(const Int8Args& p, const Int8CheckArgs& c, hipStream_t st) {
+    Int8Grid g;
+    if (!int8_grid<SH>(p, &g)) return TAO_ERR_SHAPE;
     static OncePerDevice once;
     const hipError_t e = once.run([] {
         const hipError_t e = allow_lds(int8_tiles_check<SH, true>, tile_lds<SH>(true));
         return e != hipSuccess ? e : allow_lds(int8_tiles_check<SH, false>, tile_lds<SH>(true));
     });
     if (e != hipSuccess) { g_last_hip_error = (int)e; return TAO_ERR_LAUNCH; }
+    const int nblocks = g.share == 0 ? 1 : g.share * 8 < kMaxCheckBlocks ? (int)g.share * 8 : kMaxCheckBlocks;
     const dim3 grid(nblocks), blk(SH::THREADS);
-    if (int8_direct(p, SH::BM)) hipLaunchKernelGGL((int8_tiles_check<SH, true>), grid, blk, tile_lds<SH>(true), st, p, g, y_ref, claimed, alpha, eps_rel, quick, w);
-    else                        hipLaunchKernelGGL((int8_tiles_check<SH, false>), grid, blk, tile_lds<SH>(true), st, p, g, y_ref, claimed, alpha, eps_rel, quick, w);
+    if (int8_direct(p, SH::BM > SH::BN ? SH::BM : SH::BN))
+        hipLaunchKernelGGL((int8_tiles_check<SH, true>), grid, blk, tile_lds<SH>(true), st, p, g, c.y_ref, c.claimed, c.alpha, c.eps_rel, c.quick, c.w);
+    else
+        hipLaunchKernelGGL((int8_tiles_check<SH, false>), grid, blk, tile_lds<SH>(true), st, p, g, c.y_ref, c.claimed, c.alpha, c.eps_rel, c.quick, c.w);
+    launch_profile_reduce(c.w, nblocks, (unsigned long long)c.n, c.out, st);
     return launch_status();
 }
 
@@ -656,18 +622,13 @@ int tao_bound_linear_int8(const int8_t* A, const float* scale_a, const int8_t* W
     p.y = y; p.tau = tau;
     p.vec = p.vec && aligned(y, 16) && aligned(tau, 16);
     hipStream_t st = (hipStream_t)stream;
-    int kind = int8_kind(p);
-    Int8Grid g;
-    if (kind == kWideTiles && int8_grid<Int8Wide>(p, &g)) return int8_launch_tiles<Int8Wide>(p, g, st);
-    if (kind == kMidTiles && int8_grid<Int8Mid>(p, &g)) return int8_launch_tiles<Int8Mid>(p, g, st);
-    auto few = [&](auto kernel, long rows, long cols) {
-        const __int128 tiles = (__int128)((M + rows - 1) / rows) * ((N + cols - 1) / cols) * batch;
-        hipLaunchKernelGGL(kernel, dim3(tiles < (1 << 20) ? (unsigned)tiles : 1u << 20), dim3(kInt8Threads), 0, st, p);
-    };
-    if (kind == kFewTiny)      few(int8_few<1, 1>, 16, 16);
-    else if (kind == kFewTall) few(int8_few<4, 1>, 64, 16);
-    else                       few(int8_few<4, 4>, 64, 64);
-    return launch_status();
+    switch (int8_kind(p)) {
+        case kTinyTiles:  return int8_launch_tiles<Int8Tiny>(p, st);
+        case kFlatTiles:  return int8_launch_tiles<Int8Flat>(p, st);
+        case kSmallTiles: return int8_launch_tiles<Int8Small>(p, st);
+        case kMidTiles:   return int8_launch_tiles<Int8Mid>(p, st);
+        default:          return int8_launch_tiles<Int8Wide>(p, st);
+    }
 }
 
 int tao_bound_check_linear_int8(const int8_t* A, const float* scale_a, const int8_t* W, const float* scale_w, const float* bias,
@@ -689,27 +650,14 @@ int tao_bound_check_linear_int8(const int8_t* A, const float* scale_a, const int
     p.vec = p.vec && aligned(claimed, 16) && aligned(y_ref, 16);
     tao_fp_model md;
     resolve_model(model, &md);                               // (validated above)
-    const float quick = quick_alpha(alpha, md);
-    int kind = int8_kind(p), nblocks = 1;
-    Int8Grid g;
-    if ((kind == kWideTiles && int8_grid<Int8Wide>(p, &g)) || (kind == kMidTiles && int8_grid<Int8Mid>(p, &g))) {
-        nblocks = g.share * 8 < kMaxCheckBlocks ? g.share * 8 : kMaxCheckBlocks;
-        const int rc = kind == kWideTiles ? int8_launch_check<Int8Wide>(p, g, nblocks, y_ref, claimed, alpha, eps_rel, quick, w, st)
-                                          : int8_launch_check<Int8Mid>(p, g, nblocks, y_ref, claimed, alpha, eps_rel, quick, w, st);
-        if (rc != TAO_OK) return rc;
-        launch_profile_reduce(w, nblocks, (unsigned long long)n, out, st);
-        return launch_status();
+    const Int8CheckArgs c{y_ref, claimed, alpha, eps_rel, quick_alpha(alpha, md), w, n, out};
+    switch (int8_kind(p)) {
+        case kTinyTiles:  return int8_launch_check<Int8Tiny>(p, c, st);
+        case kFlatTiles:  return int8_launch_check<Int8FlatCheck>(p, c, st);
+        case kSmallTiles: return int8_launch_check<Int8Small>(p, c, st);
+        case kMidTiles:   return int8_launch_check<Int8Mid>(p, c, st);
+        default:          return int8_launch_check<Int8Wide>(p, c, st);
     }
-    auto few = [&](auto kernel, long rows, long cols) {
-        const long tiles = n > 0 ? ((M + rows - 1) / rows) * ((N + cols - 1) / cols) * batch : 1;
-        nblocks = (int)(tiles < kMaxCheckBlocks ? tiles : kMaxCheckBlocks);
-        hipLaunchKernelGGL(kernel, dim3(nblocks), dim3(kInt8Threads), 0, st, p, y_ref, claimed, alpha, eps_rel, quick, pass_out(w, nblocks, n, out));
-    };
-    if (kind == kFewTiny)      few(int8_few_check<1, 1>, 16, 16);
-    else if (kind == kFewTall) few(int8_few_check<4, 1>, 64, 16);
-    else                       few(int8_few_check<4, 4>, 64, 64);
-    launch_finish(w, nblocks, n, out, st);
-    return launch_status();
 }
 
 }  // extern "C"

@@ -21,33 +21,50 @@ struct Int8Args {
     long M, N, K, lda, ldw, ldy, batch, strideA, strideW, strideY;
     double g2, g3, u, uflow;                    // Gamma(2), Gamma(3), unit roundoff; 2^-149 or 0
     int vec;                                    // rows of outputs and claims are on 16-byte addresses
-    int limit;                                  // whole numbers of larger magnitude round in the conversion
-    float c2, c3, cu, least;                    // the bound in binary32 (int8_output), for |v| from `least` on
+    unsigned limit;                             // whole numbers of larger magnitude (beyond_limit) round in the conversion
+    float flimit;                               // ... binary32 ones below it do not
+    float c2, c3, cu, least;                    // the bound in binary32 (int8_quad), for |v| from `least` on
 };
+
+__device__ __forceinline__ bool beyond_limit(int S, const Int8Args& p) { return (unsigned)S + p.limit > 2u * p.limit; }     // |S| > limit
 
 // The bound of one sum in binary64.  Binary64 holds S sa exactly to a rounding of 2^-53, far inside the margin of the final upper
 // rounding; the sum with the bias may cancel, but its rounding is relative to terms that the bound itself carries.
 __device__ __forceinline__ float int8_bound(int S, float sa, float sw, float b, bool has_bias, const Int8Args& p) {
     const double s = (double)S, v = s * (double)sa * (double)sw;
-    double e = (abs(S) > p.limit ? p.g3 : p.g2) * fabs(v);
+    double e = (beyond_limit(S, p) ? p.g3 : p.g2) * fabs(v);
     if (has_bias) e = fma(p.u, fabs(v + (double)b) + e, e);
     e = fma(p.uflow, fabs(s) + fabs((double)sa) + fabs((double)sw) + 1.0, e);
     return up32g(e);
 }
-// Output and bound of one sum.  The bound takes binary32 where that is accurate enough (eight binary64 instructions and three
+// Outputs and bounds of four sums of a row.  The bound takes binary32 where that is accurate enough (eight binary64 instructions and three
 // conversions less).  With h = 2^-24: v32, of three roundings, is within 3h of v (a product with S is exact where it is subnormal, so only the
 // last can underflow: |v32| >= least excludes it).
 //   Without a bias, e32 = fl(|v32| c) with c >= Gamma (1 + 4.2 h), its successor at most, lies in [1, 1 + 10.4 h] Gamma|v|.
 //   With one, y32 = fl(v32 + b) is within h|y32| + 3h|v| of v + b, and 3h u|v| <= 1.5 h Gamma|v|; with c >= Gamma (1 + 6.8 h) and
 //   cu >= u (1 + 3.2 h), fma(cu, |y32| + e32, e32) lies in [1, 1 + 15.4 h] tau.
-// 15.4 h = 9.2e-7; what is left out is of the order h^2.  A NaN, an infinity, a small or zero v go the binary64 way.
-// Returns whether binary32 was enough; otherwise tau is left to int8_bound.
-__device__ __forceinline__ bool int8_output(int S, float sa, float sw, float b, bool has_bias, const Int8Args& p, float& y, float& tau) {
-    const float v = ((float)S * sa) * sw;
-    y = has_bias ? v + b : v;
-    const float e = fabsf(v) * (abs(S) > p.limit ? p.c3 : p.c2);
-    tau = has_bias ? fmaf(p.cu, fabsf(y) + e, e) : e;
-    return fabsf(v) >= p.least && fmaxf(fabsf(y), fabsf(v)) <= 0x1p120f;
+// 15.4 h = 9.2e-7; what is left out is of the order h^2.  Returns whether that holds for all four (a NaN has a NaN for its bound either way)
+// and they are no larger than 2^90 (alpha times a bound is then an ordinary number); otherwise the bounds are left to int8_bound.
+template <bool BIAS>
+__device__ __forceinline__ bool int8_quad(const Int8Args& p, intx4 S, float sa, floatv4 sw, floatv4 b, floatv4& y, floatv4& tau) {
+    float f[4], v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { f[e] = (float)S[e]; v[e] = (f[e] * sa) * sw[e]; y[e] = BIAS ? v[e] + b[e] : v[e]; }
+    auto most = [](float a, float c, float d, float g) { return fmaxf(fmaxf(fabsf(a), fabsf(c)), fmaxf(fabsf(d), fabsf(g))); };
+    auto least = [](float a, float c, float d, float g) { return fminf(fminf(fabsf(a), fabsf(c)), fminf(fabsf(d), fabsf(g))); };
+    floatv4 c = {p.c2, p.c2, p.c2, p.c2};
+    if (!(most(f[0], f[1], f[2], f[3]) < p.flimit)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = beyond_limit(S[e], p) ? p.c3 : p.c2;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float t = fabsf(v[e]) * c[e];
+        tau[e] = BIAS ? fmaf(p.cu, fabsf(y[e]) + t, t) : t;
+    }
+    bool ok = least(v[0], v[1], v[2], v[3]) >= p.least && most(v[0], v[1], v[2], v[3]) <= 0x1p90f;
+    if (BIAS) ok = ok && most(y[0], y[1], y[2], y[3]) <= 0x1p90f;
+    return ok;
 }
 
 // 16 bytes of a row from column k on; columns from K on read as 0 (nothing beyond the row's K columns is touched).
@@ -94,14 +111,7 @@ struct Int8Store {
     template <bool BIAS>
     __device__ __forceinline__ void put(const Int8Args& p, long i, int cols, bool vec, intx4 S, float sa, floatv4 sw, floatv4 b, const Ahead&) {
         floatv4 y, t;
-        bool ok = true;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float ye, te;
-            ok &= int8_output(S[e], sa, sw[e], b[e], BIAS, p, ye, te);
-            y[e] = ye; t[e] = te;
-        }
-        if (!ok) {
+        if (!int8_quad<BIAS>(p, S, sa, sw, b, y, t)) {
 #pragma unroll 1
             for (int e = 0; e < 4; ++e) t[e] = int8_bound(S[e], sa, sw[e], b[e], BIAS, p);
         }
@@ -109,16 +119,36 @@ struct Int8Store {
         if (p.tau) quad_store(p.tau, i, cols, vec, t);
     }
 };
-// (R copies of every bin; errors of 0, which most claims have, are counted in a register: the lanes of a wavefront would queue for one word of LDS)
-template <int R>
+// The histogram of a workgroup: all bins once, and those of errors from 2^-32 to 1, where claims of binary32 outputs mostly fall, four times more:
+// a wavefront's errors of one or two steps share a few bins, and lanes that add to one word of LDS queue for it (4096 x 4096 outputs one
+// step off: 151 -> TBD us with the copies).  Errors of 0 are counted in a register.
+struct Int8Bins {
+    static constexpr unsigned NEAR = 760, NEARS = 256, COPIES = 4;
+    static constexpr int WORDS = kBins + NEARS * COPIES;
+    static __device__ __forceinline__ void add(unsigned int* hist, unsigned bin) {
+        const unsigned near = bin - NEAR;
+        atomicAdd(&hist[near < NEARS ? kBins + near * COPIES + (threadIdx.x & (COPIES - 1)) : bin], 1u);
+    }
+    static __device__ __forceinline__ unsigned int total(const unsigned int* hist, unsigned bin) {
+        unsigned int c = hist[bin];
+        const unsigned near = bin - NEAR;
+        if (near < NEARS) {
+#pragma unroll
+            for (unsigned i = 0; i < COPIES; ++i) c += hist[kBins + near * COPIES + i];
+        }
+        return c;
+    }
+};
+// WIDE: the first claims, whose errors no other one's tells the size of, are checked side by side, for kernels that have the registers.
+template <bool WIDE>
 struct Int8Check {
     const float* y_ref; const float* claimed; double alpha, eps_rel;
-    unsigned int* hist; unsigned int* largest; QuickCheck q;
-    ThreadAcc acc; unsigned int zeros = 0, known = 0;
-    static constexpr int AHEAD = 6, UNROLL = 1;
+    unsigned int* hist; unsigned int* largest; QuickCheck q; bool ordinary;
+    ThreadAcc acc; unsigned int zeros = 0;
+    static constexpr int AHEAD = 4, UNROLL = 1;
     struct Ahead { floatv4 c; };
     __device__ __forceinline__ Int8Check(const float* y_ref_, const float* claimed_, double alpha_, double eps_rel_, float quick, unsigned int* hist_, unsigned int* largest_)
-        : y_ref(y_ref_), claimed(claimed_), alpha(alpha_), eps_rel(eps_rel_), hist(hist_), largest(largest_), q(quick, eps_rel_) {}
+        : y_ref(y_ref_), claimed(claimed_), alpha(alpha_), eps_rel(eps_rel_), hist(hist_), largest(largest_), q(quick, eps_rel_) { ordinary = q.eps < INFINITY && q.alpha > 0.f; }
     __device__ __forceinline__ Ahead request(long i, int cols, bool vec) const {
         Ahead a;
         a.c = quad_load(claimed, i, cols, vec);
@@ -126,40 +156,55 @@ struct Int8Check {
     }
     template <bool BIAS>
     __device__ __forceinline__ void put(const Int8Args& p, long i, int cols, bool vec, intx4 S, float sa, floatv4 sw, floatv4 b, const Ahead& a) {
-        floatv4 r;
-        if (y_ref) r = quad_load(y_ref, i, cols, vec);
-        unsigned int bin[4], out = 0;
-        bool ok = true;
+        floatv4 y, t;
+        const bool accurate = int8_quad<BIAS>(p, S, sa, sw, b, y, t);
+        // four claims equal to their outputs, within bounds that are ordinary numbers: errors of 0
+        bool same = accurate && !y_ref && cols == 4 && ordinary;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float ye, te;
-            bool outside;
-            const bool accurate = int8_output(S[e], sa, sw[e], b[e], BIAS, p, ye, te);
-            if (!y_ref) r[e] = ye;
-            ok &= e >= cols || (quick_decided(a.c[e], r[e], te * q.alpha, q, known, bin[e], outside) && accurate);
-            out += e < cols && outside;
-        }
-        const int rep = threadIdx.x & (R - 1);
-        if (ok) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (e >= cols) continue;
-                if (bin[e] == 0) ++zeros; else atomicAdd(&hist[bin[e] * R + rep], 1u);
-            }
-            acc.violations += out;
+        for (int e = 0; e < 4; ++e) same &= a.c[e] == y[e];
+        if (same) {
+            zeros += 4;
             return;
         }
+        if (y_ref) y = quad_load(y_ref, i, cols, vec);
+        const unsigned int known = newest(largest);
+        bool ok = accurate && cols == 4 && ordinary;
+        if (y_ref) ok = ok && fmaxf(fmaxf(fabsf(y[0]), fabsf(y[1])), fmaxf(fabsf(y[2]), fabsf(y[3]))) <= 0x1p100f;
+        if (settle(a.c, y, t, known, ok)) return;
+        if (WIDE && known == 0 && accurate && cols == 4) {
+            const float c4[4] = {a.c[0], a.c[1], a.c[2], a.c[3]}, y4[4] = {y[0], y[1], y[2], y[3]}, t4[4] = {t[0], t[1], t[2], t[3]};
+            check_four<1>(c4, y4, t4, alpha, eps_rel, hist, 0, acc);
+        } else {
 #pragma unroll 1
-        for (int e = 0; e < 4; ++e) {
-            float ye, te;
-            if (!int8_output(S[e], sa, sw[e], b[e], BIAS, p, ye, te)) te = int8_bound(S[e], sa, sw[e], b[e], BIAS, p);
-            if (e < cols) check_one<R>(a.c[e], r[e], te, alpha, eps_rel, hist, rep, acc);
+            for (int e = 0; e < cols; ++e) check_one<1>(a.c[e], y[e], accurate ? t[e] : int8_bound(S[e], sa, sw[e], b[e], BIAS, p), alpha, eps_rel, hist, 0, acc);
         }
         if (acc.max_bits > known) atomicMax(largest, acc.max_bits);
-        known = max(newest(largest), acc.max_bits);
+    }
+    // Quick settlement (tao_check.hpp) of four claims at once, also of those that leave their bounds.  `at`, alpha tau to within 2^-17, decides a comparison that
+    // d misses by more than 2^-13 of it; the error's estimate a bin that it is 16 steps inside of (of 0 and of the smallest ones, whose bin has no
+    // lower edge, too).  What is no number, or too large, has an estimate beyond any error that occurs.
+    __device__ __forceinline__ bool settle(floatv4 c, floatv4 r, floatv4 t, unsigned int known, bool ok) {
+        unsigned int bits[4], lowest = ~0u, highest = 0u, out = 0;
+        float clear = INFINITY;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float d = fabsf(c[e] - r[e]), at = t[e] * q.alpha;
+            bits[e] = max(__float_as_uint(d * __builtin_amdgcn_rcpf(fabsf(r[e]) + q.eps)), 64u) + 16u;
+            lowest = min(lowest, bits[e] & 0xfffffu);
+            highest = max(highest, bits[e]);
+            clear = fminf(clear, fmaf(at, -0x1p-13f, fabsf(d - at)));
+            out += d > at;
+        }
+        if (!(ok && lowest >= 32u && highest <= known && clear > 0x1p-90f)) return false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (bits[e] == 80u) ++zeros; else Int8Bins::add(hist, bits[e] >> 20);
+        }
+        acc.violations += out;
+        return true;
     }
     // (before the histogram is read, with a barrier behind)
-    __device__ __forceinline__ void finish() { if (zeros) atomicAdd(&hist[threadIdx.x & (R - 1)], zeros); }
+    __device__ __forceinline__ void finish() { if (zeros) atomicAdd(&hist[0], zeros); }
 };
 
 // ---- the product: a workgroup takes BM x BN outputs and walks the reduction in slabs of KB columns, of which STAGES lie in LDS: one is
@@ -184,6 +229,7 @@ struct Int8Shape {
     static constexpr int NA = BM / PIECE / WAVES, NW = BN / PIECE / WAVES;
     static constexpr int STAGE = (BM + BN) * KB, LDS = STAGES * STAGE * GROUPS;
     static constexpr int SCALES = (BM + 2 * BN) * 4;                         // of the tile's rows and columns, and the bias
+    static constexpr bool TWO = LDS <= 64 * 1024;                            // two workgroups a compute unit
     static_assert(NA * PIECE * WAVES == BM && NW * PIECE * WAVES == BN && (UNITS == 4 || UNITS == 8), "whole pieces");
 };
 
@@ -340,59 +386,74 @@ struct Int8Walk {
         }
     }
 };
-// The sums of a tile by way of LDS (the stages' memory, a half of the rows at a time where that is what fits) to threads that have four
-// neighbouring columns each, so that outputs and claims move as vectors; claims are requested AHEAD rows of a thread before they are needed.
-template <class SH, bool BIAS, class Walk, class Sink>
-__device__ __forceinline__ void int8_outputs(const Int8Args& p, const intx16 (&acc)[SH::RM][SH::RN], const Walk& walk, long z, long m0, long n0,
-                                             char* lds, const float* scales, Sink& sink) {
-    const int lane = walk.lane, wave = walk.wave;
-    constexpr int WC = SH::BN / SH::WN, PARTS = (SH::BM * SH::BN * 4 + SH::STAGES * SH::STAGE - 1) / (SH::STAGES * SH::STAGE), RP = SH::RM / PARTS, BAND = SH::WM / PARTS;
-    constexpr int QUADS = SH::BN / 4, STEP = SH::THREADS / QUADS, ROWS = SH::BM / PARTS, TRIPS = (ROWS + STEP - 1) / STEP, AHEAD = Sink::AHEAD;
+// The sums of a tile go by way of LDS (the stages' memory, a half of the rows at a time where that is what fits) to threads that have four
+// neighbouring columns each, so that outputs and claims move as vectors.  Claims are requested AHEAD rows of a thread before they are needed,
+// the first ones with the tile's first slabs.
+template <class SH, class Sink>
+struct Int8Outputs {
+    static constexpr int WC = SH::BN / SH::WN, PARTS = (SH::BM * SH::BN * 4 + SH::STAGES * SH::STAGE - 1) / (SH::STAGES * SH::STAGE), RP = SH::RM / PARTS, BAND = SH::WM / PARTS;
+    static constexpr int QUADS = SH::BN / 4, STEP = SH::THREADS / QUADS, ROWS = SH::BM / PARTS, TRIPS = (ROWS + STEP - 1) / STEP, AHEAD = Sink::AHEAD;
     static_assert(SH::RM % PARTS == 0 && STEP > 0, "whole blocks a part, whole rows a trip");
-    const int* sums = reinterpret_cast<const int*>(lds);     // [group][row][column], a group's in its own stages
-    int* mine = reinterpret_cast<int*>(walk.lds);
-    const int col = threadIdx.x % QUADS * 4, row0 = threadIdx.x / QUADS;
-    const long left = p.N - n0 - col;
-    const int cols = (int)max(min(left, 4L), 0L);
-    const bool vec = p.vec && cols == 4;
-    const floatv4 sw = *reinterpret_cast<const floatv4*>(scales + SH::BM + col), b = *reinterpret_cast<const floatv4*>(scales + SH::BM + SH::BN + col);
-    const long base = z * p.strideY + m0 * p.ldy + n0 + col;
+    const Int8Args& p;
+    Sink& sink;
+    int col, row0, cols, rows;                               // this thread's columns (how many exist) and first row; rows of the tile that exist
+    bool vec;
+    long base;
+    typename Sink::Ahead ahead[AHEAD];
+
+    // row of the tile that row r of part `part` is: every wavefront's rows fall into PARTS bands
+    static __device__ __forceinline__ int row_of(int part, int r) { return r / BAND * SH::WM + part * BAND + r % BAND; }
+    __device__ __forceinline__ typename Sink::Ahead ask(int part, int trip) const {
+        const int r = row0 + trip * STEP, row = row_of(part, r);
+        const bool inside = r < ROWS && row < rows;
+        return sink.request(inside ? base + row * p.ldy : 0, inside ? cols : 0, inside && vec);
+    }
+    __device__ __forceinline__ Int8Outputs(const Int8Args& p_, Sink& sink_, long z, long m0, long n0) : p(p_), sink(sink_) {
+        col = threadIdx.x % QUADS * 4; row0 = threadIdx.x / QUADS;
+        cols = (int)max(min(p.N - n0 - col, 4L), 0L);
+        rows = (int)min(p.M - m0, (long)SH::BM);
+        vec = p.vec && cols == 4;
+        base = z * p.strideY + m0 * p.ldy + n0 + col;
 #pragma unroll
-    for (int part = 0; part < PARTS; ++part) {
-        // row of the tile that row r of the part is: every wavefront's rows fall into PARTS bands
-        auto row_of = [&](int r) __attribute__((always_inline)) { return r / BAND * SH::WM + part * BAND + r % BAND; };
-        __syncthreads();                                     // (nobody reads what lies there any more)
+        for (int a = 0; a < AHEAD; ++a) ahead[a] = ask(0, a);
+    }
+    template <bool BIAS, class Walk>
+    __device__ __forceinline__ void put(const intx16 (&acc)[SH::RM][SH::RN], const Walk& walk, const char* lds, const float* scales) {
+        const int lane = walk.lane, wave = walk.wave;
+        const int* sums = reinterpret_cast<const int*>(lds);  // [group][row][column], a group's in its own stages
+        int* mine = reinterpret_cast<int*>(walk.lds);
+        const floatv4 sw = *reinterpret_cast<const floatv4*>(scales + SH::BM + col), b = *reinterpret_cast<const floatv4*>(scales + SH::BM + SH::BN + col);
 #pragma unroll
-        for (int i = 0; i < RP; ++i)
+        for (int part = 0; part < PARTS; ++part) {
+            __syncthreads();                                 // (nobody reads what lies there any more)
 #pragma unroll
-            for (int j = 0; j < SH::RN; ++j)
+            for (int i = 0; i < RP; ++i)
 #pragma unroll
-                for (int v = 0; v < 16; ++v)
-                    mine[((wave / WC) * BAND + i * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) * SH::BN + (wave % WC) * SH::WN + j * 32 + (lane & 31)] = acc[part * RP + i][j][v];
-        __syncthreads();
-        typename Sink::Ahead ahead[AHEAD];
-        auto ask = [&](int trip) __attribute__((always_inline)) {
-            const int row = row_of(row0 + trip * STEP);
-            const bool inside = row0 + trip * STEP < ROWS && m0 + row < p.M;
-            return sink.request(inside ? base + row * p.ldy : 0, inside ? cols : 0, inside && vec);
-        };
+                for (int j = 0; j < SH::RN; ++j)
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) ahead[a] = ask(a);
+                    for (int v = 0; v < 16; ++v)
+                        mine[((wave / WC) * BAND + i * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) * SH::BN + (wave % WC) * SH::WN + j * 32 + (lane & 31)] = acc[part * RP + i][j][v];
+            if (part > 0) {
+#pragma unroll
+                for (int a = 0; a < AHEAD; ++a) ahead[a] = ask(part, a);
+            }
+            __syncthreads();
 #pragma unroll Sink::UNROLL
-        for (int trip = 0; trip < TRIPS; ++trip) {
-            const typename Sink::Ahead claims = ahead[0];
+            for (int trip = 0; trip < TRIPS; ++trip) {
+                const typename Sink::Ahead claims = ahead[0];
 #pragma unroll
-            for (int a = 0; a + 1 < AHEAD; ++a) ahead[a] = ahead[a + 1];
-            ahead[AHEAD - 1] = ask(trip + AHEAD);
-            const int r = row0 + trip * STEP, row = row_of(r);
-            if (r >= ROWS || m0 + row >= p.M || cols == 0) continue;
-            intx4 S = *reinterpret_cast<const intx4*>(sums + r * SH::BN + col);
+                for (int a = 0; a + 1 < AHEAD; ++a) ahead[a] = ahead[a + 1];
+                ahead[AHEAD - 1] = ask(part, trip + AHEAD);
+                const int r = row0 + trip * STEP, row = row_of(part, r);
+                if (r >= ROWS || row >= rows || cols == 0) continue;
+                intx4 S = *reinterpret_cast<const intx4*>(sums + r * SH::BN + col);
 #pragma unroll
-            for (int g = 1; g < SH::GROUPS; ++g) S += *reinterpret_cast<const intx4*>(sums + g * (SH::STAGES * SH::STAGE / 4) + r * SH::BN + col);
-            sink.template put<BIAS>(p, base + row * p.ldy, cols, vec, S, scales[row], sw, b, claims);
+                for (int g = 1; g < SH::GROUPS; ++g) S += *reinterpret_cast<const intx4*>(sums + g * (SH::STAGES * SH::STAGE / 4) + r * SH::BN + col);
+                sink.template put<BIAS>(p, base + row * p.ldy, cols, vec, S, scales[row], sw, b, claims);
+            }
         }
     }
-}
+};
 template <class SH, bool DIRECT, class Sink>
 __device__ __forceinline__ void int8_tiles_body(const Int8Args& p, const Int8Grid& grid, Sink& sink, char* lds) {
     Int8Walk<SH, DIRECT> walk(p, lds);
@@ -403,6 +464,7 @@ __device__ __forceinline__ void int8_tiles_body(const Int8Args& p, const Int8Gri
         if (!locate(grid, t, tm, tn, z)) continue;
         const long m0 = (long)tm * SH::BM, n0 = (long)tn * SH::BN;
         walk.start(z, m0, n0);
+        Int8Outputs<SH, Sink> outputs(p, sink, z, m0, n0);
         intx16 acc[SH::RM][SH::RN];
 #pragma unroll
         for (int i = 0; i < SH::RM; ++i)
@@ -417,8 +479,8 @@ __device__ __forceinline__ void int8_tiles_body(const Int8Args& p, const Int8Gri
             scales[SH::BM + SH::BN + i] = p.bias ? p.bias[n] : 0.f;
         }
         if (slabs > 0) walk.sums(acc, slabs); else __syncthreads();          // (the scales are in place behind a barrier)
-        if (p.bias) int8_outputs<SH, true>(p, acc, walk, z, m0, n0, lds, scales, sink);
-        else        int8_outputs<SH, false>(p, acc, walk, z, m0, n0, lds, scales, sink);
+        if (p.bias) outputs.template put<true>(acc, walk, lds, scales);
+        else        outputs.template put<false>(acc, walk, lds, scales);
         __syncthreads();                                     // (the scales and the stages are the next tile's)
     }
 }
@@ -428,43 +490,68 @@ __global__ __launch_bounds__(SH::THREADS) void int8_tiles(Int8Args p, Int8Grid g
     Int8Store sink;
     int8_tiles_body<SH, DIRECT>(p, grid, sink, lds);
 }
-constexpr int kTileReplicas = 2;
+// More workgroups than partial results: several add to one of them, which the launch before has cleared (whole numbers, so in any order).
+__global__ __launch_bounds__(kCheckThreads) void clear_partials(CheckWorkspace w) {
+    const int tid = threadIdx.x;
+    for (int i = tid; i < kBins; i += kCheckThreads) w.hist[(size_t)blockIdx.x * kBins + i] = 0;
+    if (tid < kGroups) w.coarse[blockIdx.x * kGroups + tid] = 0;
+    if (tid == 0) { BlockStats& o = w.stats[blockIdx.x]; o.violations = 0; o.nans = 0; o.max_bits = 0; }
+}
 template <class SH, bool DIRECT>
-__global__ __launch_bounds__(SH::THREADS) void int8_tiles_check(Int8Args p, Int8Grid grid, const float* y_ref, const float* claimed, double alpha, double eps_rel,
+__global__ __launch_bounds__(SH::THREADS, SH::TWO ? SH::THREADS * 2 / (4 * kWave) : 1) void int8_tiles_check(Int8Args p, Int8Grid grid, const float* y_ref, const float* claimed, double alpha, double eps_rel,
                                                                 float quick, CheckWorkspace w) {
     extern __shared__ __align__(16) char lds[];
     unsigned int* hist = reinterpret_cast<unsigned int*>(lds + SH::LDS + SH::SCALES);
-    unsigned int* rest = hist + kBins * kTileReplicas;       // largest error, three counters of every wavefront
+    unsigned int* rest = hist + Int8Bins::WORDS;       // largest error, three counters of every wavefront
     const int tid = threadIdx.x, wave = tid / kWave;
-    for (int i = tid; i < kBins * kTileReplicas; i += SH::THREADS) hist[i] = 0;
+    for (int i = tid; i < Int8Bins::WORDS; i += SH::THREADS) hist[i] = 0;
     if (tid == 0) rest[0] = 0;
     __syncthreads();
-    Int8Check<kTileReplicas> sink(y_ref, claimed, alpha, eps_rel, quick, hist, rest);
+    Int8Check<!SH::TWO && SH::BN < 256> sink(y_ref, claimed, alpha, eps_rel, quick, hist, rest);
     int8_tiles_body<SH, DIRECT>(p, grid, sink, lds);
     sink.finish();
     const unsigned int v = wave_sum(sink.acc.violations), q = wave_sum(sink.acc.nans), m = wave_max(sink.acc.max_bits);
     if ((tid & (kWave - 1)) == 0) { rest[4 + wave * 3] = v; rest[4 + wave * 3 + 1] = q; rest[4 + wave * 3 + 2] = m; }
     __syncthreads();
+    const int slot = blockIdx.x % kMaxCheckBlocks;
+    const bool shared = gridDim.x > kMaxCheckBlocks;
     if (tid == 0) {
         unsigned long long vs = 0, qs = 0;
         unsigned int ms = 0;
         for (int i = 0; i < SH::THREADS / kWave; ++i) { vs += rest[4 + i * 3]; qs += rest[4 + i * 3 + 1]; ms = max(ms, rest[4 + i * 3 + 2]); }
-        BlockStats& o = w.stats[blockIdx.x];
-        o.violations = vs; o.nans = qs; o.max_bits = ms;
+        BlockStats& o = w.stats[slot];
+        if (shared) {
+            if (vs) atomicAdd(&o.violations, vs);
+            if (qs) atomicAdd(&o.nans, qs);
+            if (ms) atomicMax(&o.max_bits, ms);
+        } else {
+            o.violations = vs; o.nans = qs; o.max_bits = ms;
+        }
     }
-    flush_histogram<kTileReplicas>(hist, w.hist + (size_t)blockIdx.x * kBins, w.coarse + blockIdx.x * kGroups);
+    unsigned int* bins = w.hist + (size_t)slot * kBins;
+    unsigned int* coarse = w.coarse + slot * kGroups;
+    for (int b = tid; b < kBins; b += SH::THREADS) {         // (a wavefront covers a group of 64 bins)
+        const unsigned int c = Int8Bins::total(hist, b), g = wave_sum(c);
+        const bool first = (tid & (kWave - 1)) == 0;
+        if (shared) {
+            if (c) atomicAdd(&bins[b], c);
+            if (first && g) atomicAdd(&coarse[b / kBinsPerReduceBlock], g);
+        } else {
+            bins[b] = c;
+            if (first) coarse[b / kBinsPerReduceBlock] = g;
+        }
+    }
 }
 template <class SH> constexpr int tile_lds(bool check) {
-    return SH::LDS + SH::SCALES + (check ? kBins * kTileReplicas * 4 + (4 + 3 * SH::THREADS / kWave) * 4 : 0);
+    return SH::LDS + SH::SCALES + (check ? Int8Bins::WORDS * 4 + (4 + 3 * SH::THREADS / kWave) * 4 : 0);
 }
 typedef Int8Shape<32, 32, 32, 32, 128, 2, 8> Int8Tiny;                       // 136 KB of LDS
-typedef Int8Shape<32, 64, 32, 32, 128, 3, 4> Int8Flat;                       // 144 KB; 96 where the check's histogram has to fit
-typedef Int8Shape<32, 64, 32, 32, 128, 2, 4> Int8FlatCheck;
+typedef Int8Shape<32, 64, 32, 32, 128, 3, 4> Int8Flat;                       // 144 KB
 typedef Int8Shape<64, 64, 32, 32, 128, 2, 2> Int8Small;                      // 64 KB: two workgroups a compute unit
 typedef Int8Shape<128, 128, 64, 32, 128, 2> Int8Mid;                         // 64 KB
 typedef Int8Shape<256, 256, 128, 64, 128, 2> Int8Wide;                       // 128 KB
-static_assert(tile_lds<Int8Tiny>(true) <= 160 * 1024 && tile_lds<Int8FlatCheck>(true) <= 160 * 1024 && tile_lds<Int8Flat>(false) <= 160 * 1024 &&
-              tile_lds<Int8Wide>(true) <= 160 * 1024, "a compute unit's LDS");
+static_assert(tile_lds<Int8Tiny>(true) <= 160 * 1024 && tile_lds<Int8Flat>(true) <= 160 * 1024 &&
+              tile_lds<Int8Wide>(true) <= 160 * 1024 && tile_lds<Int8Small>(true) <= 80 * 1024 && tile_lds<Int8Mid>(true) <= 80 * 1024, "a compute unit's LDS");
 
 // ---- quantisation of rows: scale = fl(max|x| / 127), q = round(fl(x / scale)), ties to even.  A row that is not finite has scale NaN
 // and q = 0 (so the product is NaN, which no check admits); a row of zeros, or one so small that its scale rounds to 0, scale 0 and q = 0.
@@ -518,7 +605,8 @@ static int int8_setup(const int8_t* A, const float* scale_a, const int8_t* W, co
     p.batch = batch; p.strideA = strideA; p.strideW = strideW; p.strideY = strideY;
     p.g2 = gamma_up(2, md); p.g3 = gamma_up(3, md); p.u = md.u;
     if (!(p.g2 == p.g2) || !(p.g3 == p.g3)) return TAO_ERR_K_RANGE;
-    p.limit = 1.0 / md.u >= 2147483647.0 ? 2147483647 : (int)std::floor(1.0 / md.u);
+    p.limit = 1.0 / md.u >= 2147483647.0 ? 2147483647u : (unsigned)std::floor(1.0 / md.u);
+    p.flimit = (float)p.limit > 0x1p24f ? 0x1p24f : (float)p.limit;      // (those below 2^24 are the whole numbers themselves)
     p.vec = ldy % 4 == 0 && strideY % 4 == 0;                // (and the tensors' addresses, below)
     p.uflow = (md.flags & TAO_FLAG_UNDERFLOW_TERMS) ? 0x1p-149 : 0.0;
     auto up = [](double v) { const float f = (float)v; return (double)f < v ? std::nextafterf(f, INFINITY) : f; };
@@ -583,13 +671,15 @@ template <class SH> static int int8_launch_check(const Int8Args& p, const Int8Ch
         return e != hipSuccess ? e : allow_lds(int8_tiles_check<SH, false>, tile_lds<SH>(true));
     });
     if (e != hipSuccess) { g_last_hip_error = (int)e; return TAO_ERR_LAUNCH; }
-    const int nblocks = g.share == 0 ? 1 : g.share * 8 < kMaxCheckBlocks ? (int)g.share * 8 : kMaxCheckBlocks;
+    const long places = SH::TWO ? 2 * kMaxCheckBlocks : kMaxCheckBlocks;
+    const int nblocks = g.share == 0 ? 1 : (int)((long)g.share * 8 < places ? g.share * 8 : places), partials = nblocks < kMaxCheckBlocks ? nblocks : kMaxCheckBlocks;
     const dim3 grid(nblocks), blk(SH::THREADS);
+    if (nblocks > kMaxCheckBlocks) hipLaunchKernelGGL(clear_partials, dim3(kMaxCheckBlocks), dim3(kCheckThreads), 0, st, c.w);
     if (int8_direct(p, SH::BM > SH::BN ? SH::BM : SH::BN))
         hipLaunchKernelGGL((int8_tiles_check<SH, true>), grid, blk, tile_lds<SH>(true), st, p, g, c.y_ref, c.claimed, c.alpha, c.eps_rel, c.quick, c.w);
     else
         hipLaunchKernelGGL((int8_tiles_check<SH, false>), grid, blk, tile_lds<SH>(true), st, p, g, c.y_ref, c.claimed, c.alpha, c.eps_rel, c.quick, c.w);
-    launch_profile_reduce(c.w, nblocks, (unsigned long long)c.n, c.out, st);
+    launch_profile_reduce(c.w, partials, (unsigned long long)c.n, c.out, st);
     return launch_status();
 }
 
@@ -653,7 +743,7 @@ int tao_bound_check_linear_int8(const int8_t* A, const float* scale_a, const int
     const Int8CheckArgs c{y_ref, claimed, alpha, eps_rel, quick_alpha(alpha, md), w, n, out};
     switch (int8_kind(p)) {
         case kTinyTiles:  return int8_launch_check<Int8Tiny>(p, c, st);
-        case kFlatTiles:  return int8_launch_check<Int8FlatCheck>(p, c, st);
+        case kFlatTiles:  return int8_launch_check<Int8Flat>(p, c, st);
         case kSmallTiles: return int8_launch_check<Int8Small>(p, c, st);
         case kMidTiles:   return int8_launch_check<Int8Mid>(p, c, st);
         default:          return int8_launch_check<Int8Wide>(p, c, st);

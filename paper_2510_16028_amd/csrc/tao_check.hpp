@@ -126,19 +126,6 @@ __device__ __forceinline__ bool quick_settled(float c, float r, float at, const 
     const float lhs = zero ? 0.f : fmaf(d, 1.f + 0x1p-16f, 0x1p-90f);     // (a bound near the subnormal range settles nothing)
     return lhs <= at && at <= 0x1p120f && den <= 0x1p100f && (zero || ((t & 0xfffffu) >= 32u && t <= known));
 }
-// The same for claims that may well leave their bounds: settled too where d is clearly beyond alpha tau (a violation, `outside`).  at as above and
-// in [(1 - 2^-17) alpha tau, (1 + 2^-18) alpha tau]; q.alpha times a binary32 tau is.
-__device__ __forceinline__ bool quick_decided(float c, float r, float at, const QuickCheck& q, unsigned known, unsigned& bin, bool& outside) {
-    const float d = fabsf(c - r);
-    const float den = fabsf(r) + q.eps;
-    const unsigned bits = __float_as_uint(d * __builtin_amdgcn_rcpf(den));
-    bin = bits >> 20;
-    const bool zero = d == 0.f;                              // exactly: c == r
-    const unsigned t = bits + 16u;
-    const bool inside = (zero ? 0.f : fmaf(d, 1.f + 0x1p-16f, 0x1p-90f)) <= at;
-    outside = d * (1.f - 0x1p-14f) > at && at >= 0x1p-90f;
-    return (inside | outside) && at <= 0x1p120f && d <= 0x1p100f && den <= 0x1p100f && (zero || ((t & 0xfffffu) >= 32u && t <= known));
-}
 typedef float floatv4 __attribute__((ext_vector_type(4)));      // (indexed by a variable it stays in registers)
 // Four elements: settled together or checked exactly, with tau(i) the binary32 bound of element i.  largest: the
 // workgroup's largest exactly computed error (LDS), known: this thread's copy, no newer than it needs to be.  WIDE: the

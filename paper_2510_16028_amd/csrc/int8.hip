@@ -120,8 +120,7 @@ struct Int8Store {
     }
 };
 // The histogram of a workgroup: all bins once, and those of errors from 2^-32 to 1, where claims of binary32 outputs mostly fall, four times more:
-// a wavefront's errors of one or two steps share a few bins, and lanes that add to one word of LDS queue for it (4096 x 4096 outputs one
-// step off: 151 -> TBD us with the copies).  Errors of 0 are counted in a register.
+// a wavefront's errors of one or two steps share a few bins, and lanes that add to one word of LDS queue for it.  Errors of 0 are counted in a register.
 struct Int8Bins {
     static constexpr unsigned NEAR = 760, NEARS = 256, COPIES = 4;
     static constexpr int WORDS = kBins + NEARS * COPIES;
@@ -139,13 +138,14 @@ struct Int8Bins {
         return c;
     }
 };
-// WIDE: the first claims, whose errors no other one's tells the size of, are checked side by side, for kernels that have the registers.
-template <bool WIDE>
+// ROOM: the kernel has registers to spare (one workgroup a compute unit): two rows under way, and claims that are not settled are checked without a loop,
+// the first ones, whose errors no other one's tells the size of, side by side.
+template <bool ROOM>
 struct Int8Check {
     const float* y_ref; const float* claimed; double alpha, eps_rel;
     unsigned int* hist; unsigned int* largest; QuickCheck q; bool ordinary;
     ThreadAcc acc; unsigned int zeros = 0;
-    static constexpr int AHEAD = 4, UNROLL = 1;
+    static constexpr int AHEAD = 4, UNROLL = ROOM ? 2 : 1;
     struct Ahead { floatv4 c; };
     __device__ __forceinline__ Int8Check(const float* y_ref_, const float* claimed_, double alpha_, double eps_rel_, float quick, unsigned int* hist_, unsigned int* largest_)
         : y_ref(y_ref_), claimed(claimed_), alpha(alpha_), eps_rel(eps_rel_), hist(hist_), largest(largest_), q(quick, eps_rel_) { ordinary = q.eps < INFINITY && q.alpha > 0.f; }
@@ -171,12 +171,23 @@ struct Int8Check {
         bool ok = accurate && cols == 4 && ordinary;
         if (y_ref) ok = ok && fmaxf(fmaxf(fabsf(y[0]), fabsf(y[1])), fmaxf(fabsf(y[2]), fabsf(y[3]))) <= 0x1p100f;
         if (settle(a.c, y, t, known, ok)) return;
-        if (WIDE && known == 0 && accurate && cols == 4) {
+        if (ROOM && known == 0 && accurate && cols == 4) {
             const float c4[4] = {a.c[0], a.c[1], a.c[2], a.c[3]}, y4[4] = {y[0], y[1], y[2], y[3]}, t4[4] = {t[0], t[1], t[2], t[3]};
             check_four<1>(c4, y4, t4, alpha, eps_rel, hist, 0, acc);
         } else {
+            auto one = [&](int e) __attribute__((always_inline)) {
+                check_one<1>(a.c[e], y[e], accurate ? t[e] : int8_bound(S[e], sa, sw[e], b[e], BIAS, p), alpha, eps_rel, hist, 0, acc);
+            };
+            if constexpr (ROOM) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (e < cols) one(e);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
 #pragma unroll 1
-            for (int e = 0; e < cols; ++e) check_one<1>(a.c[e], y[e], accurate ? t[e] : int8_bound(S[e], sa, sw[e], b[e], BIAS, p), alpha, eps_rel, hist, 0, acc);
+                for (int e = 0; e < cols; ++e) one(e);
+            }
         }
         if (acc.max_bits > known) atomicMax(largest, acc.max_bits);
     }
@@ -262,8 +273,7 @@ struct Int8Walk {
     struct Fragments { intx4 a[SH::RM], w[SH::RN]; };
 
     static __device__ __forceinline__ int turn(int row) { return SH::UNITS == 8 ? row & 7 : row >> 1 & 3; }
-    __device__ __forceinline__ Int8Walk(const Int8Args& p_, char* lds_) : p(p_) {
-        const int tid = threadIdx.x;
+    __device__ __forceinline__ Int8Walk(const Int8Args& p_, char* lds_, int tid) : p(p_) {
         lane = tid & (kWave - 1);
         wave = __builtin_amdgcn_readfirstlane(tid / kWave);
         group = wave / SH::WAVES;
@@ -408,8 +418,8 @@ struct Int8Outputs {
         const bool inside = r < ROWS && row < rows;
         return sink.request(inside ? base + row * p.ldy : 0, inside ? cols : 0, inside && vec);
     }
-    __device__ __forceinline__ Int8Outputs(const Int8Args& p_, Sink& sink_, long z, long m0, long n0) : p(p_), sink(sink_) {
-        col = threadIdx.x % QUADS * 4; row0 = threadIdx.x / QUADS;
+    __device__ __forceinline__ Int8Outputs(const Int8Args& p_, Sink& sink_, long z, long m0, long n0, int tid) : p(p_), sink(sink_) {
+        col = tid % QUADS * 4; row0 = tid / QUADS;
         cols = (int)max(min(p.N - n0 - col, 4L), 0L);
         rows = (int)min(p.M - m0, (long)SH::BM);
         vec = p.vec && cols == 4;
@@ -456,15 +466,17 @@ struct Int8Outputs {
 };
 template <class SH, bool DIRECT, class Sink>
 __device__ __forceinline__ void int8_tiles_body(const Int8Args& p, const Int8Grid& grid, Sink& sink, char* lds) {
-    Int8Walk<SH, DIRECT> walk(p, lds);
     float* scales = reinterpret_cast<float*>(lds + SH::LDS);              // [BM], [BN], bias [BN]
     const int slabs = (int)((p.K + SH::KB * SH::GROUPS - 1) / (SH::KB * SH::GROUPS));
     for (unsigned t = blockIdx.x; (t >> 3) < grid.share; t += gridDim.x) {
         unsigned tm, tn, z;
         if (!locate(grid, t, tm, tn, z)) continue;
         const long m0 = (long)tm * SH::BM, n0 = (long)tn * SH::BN;
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));                        // (what is formed of it is formed anew for every tile: kept from tile to tile it would take the registers of the sums)
+        Int8Walk<SH, DIRECT> walk(p, lds, tid);
         walk.start(z, m0, n0);
-        Int8Outputs<SH, Sink> outputs(p, sink, z, m0, n0);
+        Int8Outputs<SH, Sink> outputs(p, sink, z, m0, n0, tid);
         intx16 acc[SH::RM][SH::RN];
 #pragma unroll
         for (int i = 0; i < SH::RM; ++i)
@@ -479,6 +491,7 @@ __device__ __forceinline__ void int8_tiles_body(const Int8Args& p, const Int8Gri
             scales[SH::BM + SH::BN + i] = p.bias ? p.bias[n] : 0.f;
         }
         if (slabs > 0) walk.sums(acc, slabs); else __syncthreads();          // (the scales are in place behind a barrier)
+        asm volatile("" : "+v"(walk.lane), "+v"(outputs.col), "+v"(outputs.row0));
         if (p.bias) outputs.template put<true>(acc, walk, lds, scales);
         else        outputs.template put<false>(acc, walk, lds, scales);
         __syncthreads();                                     // (the scales and the stages are the next tile's)
@@ -497,8 +510,10 @@ __global__ __launch_bounds__(kCheckThreads) void clear_partials(CheckWorkspace w
     if (tid < kGroups) w.coarse[blockIdx.x * kGroups + tid] = 0;
     if (tid == 0) { BlockStats& o = w.stats[blockIdx.x]; o.violations = 0; o.nans = 0; o.max_bits = 0; }
 }
-template <class SH, bool DIRECT>
-__global__ __launch_bounds__(SH::THREADS, SH::TWO ? SH::THREADS * 2 / (4 * kWave) : 1) void int8_tiles_check(Int8Args p, Int8Grid grid, const float* y_ref, const float* claimed, double alpha, double eps_rel,
+// PAIR: two workgroups a compute unit, from two tiles for each on: one's checks go on under the other's products (2048 x 4096 x 12288 200 -> 180 us;
+// with one tile each the registers are worth more, 2048 x 2048 x 2048 33 us against 42, and with 288 tiles a launch less, 512 x 768 x 2304 22 against 26).
+template <class SH, bool DIRECT, bool PAIR>
+__global__ __launch_bounds__(SH::THREADS, PAIR ? SH::THREADS * 2 / (4 * kWave) : 1) void int8_tiles_check(Int8Args p, Int8Grid grid, const float* y_ref, const float* claimed, double alpha, double eps_rel,
                                                                 float quick, CheckWorkspace w) {
     extern __shared__ __align__(16) char lds[];
     unsigned int* hist = reinterpret_cast<unsigned int*>(lds + SH::LDS + SH::SCALES);
@@ -507,7 +522,7 @@ __global__ __launch_bounds__(SH::THREADS, SH::TWO ? SH::THREADS * 2 / (4 * kWave
     for (int i = tid; i < Int8Bins::WORDS; i += SH::THREADS) hist[i] = 0;
     if (tid == 0) rest[0] = 0;
     __syncthreads();
-    Int8Check<!SH::TWO && SH::BN < 256> sink(y_ref, claimed, alpha, eps_rel, quick, hist, rest);
+    Int8Check<!PAIR && SH::BN < 256> sink(y_ref, claimed, alpha, eps_rel, quick, hist, rest);
     int8_tiles_body<SH, DIRECT>(p, grid, sink, lds);
     sink.finish();
     const unsigned int v = wave_sum(sink.acc.violations), q = wave_sum(sink.acc.nans), m = wave_max(sink.acc.max_bits);
@@ -662,25 +677,31 @@ template <class SH> static int int8_launch_tiles(const Int8Args& p, hipStream_t 
     return launch_status();
 }
 struct Int8CheckArgs { const float* y_ref; const float* claimed; double alpha, eps_rel; float quick; CheckWorkspace w; long n; tao_profile* out; };
-template <class SH> static int int8_launch_check(const Int8Args& p, const Int8CheckArgs& c, hipStream_t st) {
-    Int8Grid g;
-    if (!int8_grid<SH>(p, &g)) return TAO_ERR_SHAPE;
+template <class SH, bool PAIR> static int int8_launch_check(const Int8Args& p, const Int8Grid& g, const Int8CheckArgs& c, hipStream_t st) {
     static OncePerDevice once;
     const hipError_t e = once.run([] {
-        const hipError_t e = allow_lds(int8_tiles_check<SH, true>, tile_lds<SH>(true));
-        return e != hipSuccess ? e : allow_lds(int8_tiles_check<SH, false>, tile_lds<SH>(true));
+        const hipError_t e = allow_lds(int8_tiles_check<SH, true, PAIR>, tile_lds<SH>(true));
+        return e != hipSuccess ? e : allow_lds(int8_tiles_check<SH, false, PAIR>, tile_lds<SH>(true));
     });
     if (e != hipSuccess) { g_last_hip_error = (int)e; return TAO_ERR_LAUNCH; }
-    const long places = SH::TWO ? 2 * kMaxCheckBlocks : kMaxCheckBlocks;
+    const long places = PAIR ? 2 * kMaxCheckBlocks : kMaxCheckBlocks;
     const int nblocks = g.share == 0 ? 1 : (int)((long)g.share * 8 < places ? g.share * 8 : places), partials = nblocks < kMaxCheckBlocks ? nblocks : kMaxCheckBlocks;
     const dim3 grid(nblocks), blk(SH::THREADS);
     if (nblocks > kMaxCheckBlocks) hipLaunchKernelGGL(clear_partials, dim3(kMaxCheckBlocks), dim3(kCheckThreads), 0, st, c.w);
     if (int8_direct(p, SH::BM > SH::BN ? SH::BM : SH::BN))
-        hipLaunchKernelGGL((int8_tiles_check<SH, true>), grid, blk, tile_lds<SH>(true), st, p, g, c.y_ref, c.claimed, c.alpha, c.eps_rel, c.quick, c.w);
+        hipLaunchKernelGGL((int8_tiles_check<SH, true, PAIR>), grid, blk, tile_lds<SH>(true), st, p, g, c.y_ref, c.claimed, c.alpha, c.eps_rel, c.quick, c.w);
     else
-        hipLaunchKernelGGL((int8_tiles_check<SH, false>), grid, blk, tile_lds<SH>(true), st, p, g, c.y_ref, c.claimed, c.alpha, c.eps_rel, c.quick, c.w);
+        hipLaunchKernelGGL((int8_tiles_check<SH, false, PAIR>), grid, blk, tile_lds<SH>(true), st, p, g, c.y_ref, c.claimed, c.alpha, c.eps_rel, c.quick, c.w);
     launch_profile_reduce(c.w, partials, (unsigned long long)c.n, c.out, st);
     return launch_status();
+}
+template <class SH> static int int8_launch_check(const Int8Args& p, const Int8CheckArgs& c, hipStream_t st) {
+    Int8Grid g;
+    if (!int8_grid<SH>(p, &g)) return TAO_ERR_SHAPE;
+    if constexpr (SH::TWO) {
+        if (g.tiles >= 2u * kMaxCheckBlocks) return int8_launch_check<SH, true>(p, g, c, st);
+    }
+    return int8_launch_check<SH, false>(p, g, c, st);
 }
 
 }  // namespace tao

@@ -20,7 +20,6 @@ struct Int8Args {
     float* y; float* tau;                       // [batch][M][N], either may be null
     long M, N, K, lda, ldw, ldy, batch, strideA, strideW, strideY;
     double g2, g3, u, uflow;                    // Gamma(2), Gamma(3), unit roundoff; 2^-149 or 0
-    int vec;                                    // rows of outputs and claims are on 16-byte addresses
     unsigned limit;                             // whole numbers of larger magnitude (beyond_limit) round in the conversion
     float flimit;                               // ... binary32 ones below it do not
     float c2, c3, cu, least;                    // the bound in binary32 (int8_quad), for |v| from `least` on
@@ -67,56 +66,65 @@ __device__ __forceinline__ bool int8_quad(const Int8Args& p, intx4 S, float sa, 
     return ok;
 }
 
-// 16 bytes of a row from column k on; columns from K on read as 0 (nothing beyond the row's K columns is touched).
+// 16 bytes of a row from column k on; columns from K on read as 0 (nothing beyond the row's K columns is touched): at the row's end its last
+// 16 bytes, moved down.
 __device__ __forceinline__ intx4 row16(const signed char* __restrict__ row, long k, long K) {
     intx4 r = {0, 0, 0, 0};
     if (k + 16 <= K) {
         __builtin_memcpy(&r, row + k, 16);
-    } else {
-        unsigned long long lo = 0, hi = 0;
+    } else if (k < K) {
+        unsigned long long w[2] = {0, 0};
+        if (K >= 16) {
+            __builtin_memcpy(w, row + K - 16, 16);
+            const int beyond = (int)(k + 16 - K) * 8;        // 8 .. 120
+            w[0] = beyond >= 64 ? w[1] >> (beyond - 64) : w[0] >> beyond | w[1] << (64 - beyond);
+            w[1] = beyond >= 64 ? 0 : w[1] >> beyond;
+        } else {
 #pragma unroll 1
-        for (long i = K - 1; i >= k; --i) {                  // (at most 15 bytes, the last one first)
-            hi = hi << 8 | lo >> 56;
-            lo = lo << 8 | (unsigned char)row[i];
+            for (int i = (int)K - 1; i >= 0; --i) {          // (k is 0)
+                w[1] = w[1] << 8 | w[0] >> 56;
+                w[0] = w[0] << 8 | (unsigned char)row[i];
+            }
         }
-        r = intx4{(int)(unsigned)lo, (int)(unsigned)(lo >> 32), (int)(unsigned)hi, (int)(unsigned)(hi >> 32)};
+        r = intx4{(int)(unsigned)w[0], (int)(unsigned)(w[0] >> 32), (int)(unsigned)w[1], (int)(unsigned)(w[1] >> 32)};
     }
     return r;
 }
 
-// What becomes of four neighbouring outputs of one row, from index i on (cols: how many there are; vec: as one vector): stored with
-// their bounds, or checked against the claims, which are requested ahead.
-__device__ __forceinline__ floatv4 quad_load(const float* __restrict__ src, long i, int cols, bool vec) {
+// What becomes of four neighbouring outputs of one row, from index i on (cols: how many there are): stored with their bounds, or checked
+// against the claims, which are requested ahead.  (A vector of four needs the alignment of one: rows of any stride, on any address.)
+typedef float floatv4_any __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ floatv4 quad_load(const float* __restrict__ src, long i, int cols) {
     floatv4 v = {0.f, 0.f, 0.f, 0.f};
-    if (vec) {
-        v = __builtin_nontemporal_load(reinterpret_cast<const floatv4*>(src + i));
+    if (cols == 4) {
+        v = __builtin_nontemporal_load(reinterpret_cast<const floatv4_any*>(src + i));
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) if (e < cols) v[e] = src[i + e];
+        for (int e = 0; e < 3; ++e) if (e < cols) v[e] = src[i + e];
     }
     return v;
 }
-__device__ __forceinline__ void quad_store(float* __restrict__ dst, long i, int cols, bool vec, floatv4 v) {
-    if (vec) {
-        __builtin_nontemporal_store(v, reinterpret_cast<floatv4*>(dst + i));
+__device__ __forceinline__ void quad_store(float* __restrict__ dst, long i, int cols, floatv4 v) {
+    if (cols == 4) {
+        __builtin_nontemporal_store(v, reinterpret_cast<floatv4_any*>(dst + i));
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) if (e < cols) dst[i + e] = v[e];
+        for (int e = 0; e < 3; ++e) if (e < cols) dst[i + e] = v[e];
     }
 }
 struct Int8Store {
     static constexpr int AHEAD = 1, UNROLL = 4;
     struct Ahead {};
-    __device__ __forceinline__ Ahead request(long, int, bool) const { return Ahead(); }
+    __device__ __forceinline__ Ahead request(long, int) const { return Ahead(); }
     template <bool BIAS>
-    __device__ __forceinline__ void put(const Int8Args& p, long i, int cols, bool vec, intx4 S, float sa, floatv4 sw, floatv4 b, const Ahead&) {
+    __device__ __forceinline__ void put(const Int8Args& p, long i, int cols, intx4 S, float sa, floatv4 sw, floatv4 b, const Ahead&) {
         floatv4 y, t;
         if (!int8_quad<BIAS>(p, S, sa, sw, b, y, t)) {
 #pragma unroll 1
             for (int e = 0; e < 4; ++e) t[e] = int8_bound(S[e], sa, sw[e], b[e], BIAS, p);
         }
-        if (p.y) quad_store(p.y, i, cols, vec, y);
-        if (p.tau) quad_store(p.tau, i, cols, vec, t);
+        if (p.y) quad_store(p.y, i, cols, y);
+        if (p.tau) quad_store(p.tau, i, cols, t);
     }
 };
 // The histogram of a workgroup: all bins once, and those of errors from 2^-32 to 1, where claims of binary32 outputs mostly fall, four times more:
@@ -149,13 +157,13 @@ struct Int8Check {
     struct Ahead { floatv4 c; };
     __device__ __forceinline__ Int8Check(const float* y_ref_, const float* claimed_, double alpha_, double eps_rel_, float quick, unsigned int* hist_, unsigned int* largest_)
         : y_ref(y_ref_), claimed(claimed_), alpha(alpha_), eps_rel(eps_rel_), hist(hist_), largest(largest_), q(quick, eps_rel_) { ordinary = q.eps < INFINITY && q.alpha > 0.f; }
-    __device__ __forceinline__ Ahead request(long i, int cols, bool vec) const {
+    __device__ __forceinline__ Ahead request(long i, int cols) const {
         Ahead a;
-        a.c = quad_load(claimed, i, cols, vec);
+        a.c = quad_load(claimed, i, cols);
         return a;
     }
     template <bool BIAS>
-    __device__ __forceinline__ void put(const Int8Args& p, long i, int cols, bool vec, intx4 S, float sa, floatv4 sw, floatv4 b, const Ahead& a) {
+    __device__ __forceinline__ void put(const Int8Args& p, long i, int cols, intx4 S, float sa, floatv4 sw, floatv4 b, const Ahead& a) {
         floatv4 y, t;
         const bool accurate = int8_quad<BIAS>(p, S, sa, sw, b, y, t);
         // four claims equal to their outputs, within bounds that are ordinary numbers: errors of 0
@@ -166,7 +174,7 @@ struct Int8Check {
             zeros += 4;
             return;
         }
-        if (y_ref) y = quad_load(y_ref, i, cols, vec);
+        if (y_ref) y = quad_load(y_ref, i, cols);
         const unsigned int known = newest(largest);
         bool ok = accurate && cols == 4 && ordinary;
         if (y_ref) ok = ok && fmaxf(fmaxf(fabsf(y[0]), fabsf(y[1])), fmaxf(fabsf(y[2]), fabsf(y[3]))) <= 0x1p100f;
@@ -407,7 +415,6 @@ struct Int8Outputs {
     const Int8Args& p;
     Sink& sink;
     int col, row0, cols, rows;                               // this thread's columns (how many exist) and first row; rows of the tile that exist
-    bool vec;
     long base;
     typename Sink::Ahead ahead[AHEAD];
 
@@ -416,13 +423,12 @@ struct Int8Outputs {
     __device__ __forceinline__ typename Sink::Ahead ask(int part, int trip) const {
         const int r = row0 + trip * STEP, row = row_of(part, r);
         const bool inside = r < ROWS && row < rows;
-        return sink.request(inside ? base + row * p.ldy : 0, inside ? cols : 0, inside && vec);
+        return sink.request(inside ? base + row * p.ldy : 0, inside ? cols : 0);
     }
     __device__ __forceinline__ Int8Outputs(const Int8Args& p_, Sink& sink_, long z, long m0, long n0, int tid) : p(p_), sink(sink_) {
         col = tid % QUADS * 4; row0 = tid / QUADS;
         cols = (int)max(min(p.N - n0 - col, 4L), 0L);
         rows = (int)min(p.M - m0, (long)SH::BM);
-        vec = p.vec && cols == 4;
         base = z * p.strideY + m0 * p.ldy + n0 + col;
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a) ahead[a] = ask(0, a);
@@ -459,7 +465,7 @@ struct Int8Outputs {
                 intx4 S = *reinterpret_cast<const intx4*>(sums + r * SH::BN + col);
 #pragma unroll
                 for (int g = 1; g < SH::GROUPS; ++g) S += *reinterpret_cast<const intx4*>(sums + g * (SH::STAGES * SH::STAGE / 4) + r * SH::BN + col);
-                sink.template put<BIAS>(p, base + row * p.ldy, cols, vec, S, scales[row], sw, b, claims);
+                sink.template put<BIAS>(p, base + row * p.ldy, cols, S, scales[row], sw, b, claims);
             }
         }
     }
@@ -622,7 +628,6 @@ static int int8_setup(const int8_t* A, const float* scale_a, const int8_t* W, co
     if (!(p.g2 == p.g2) || !(p.g3 == p.g3)) return TAO_ERR_K_RANGE;
     p.limit = 1.0 / md.u >= 2147483647.0 ? 2147483647u : (unsigned)std::floor(1.0 / md.u);
     p.flimit = (float)p.limit > 0x1p24f ? 0x1p24f : (float)p.limit;      // (those below 2^24 are the whole numbers themselves)
-    p.vec = ldy % 4 == 0 && strideY % 4 == 0;                // (and the tensors' addresses, below)
     p.uflow = (md.flags & TAO_FLAG_UNDERFLOW_TERMS) ? 0x1p-149 : 0.0;
     auto up = [](double v) { const float f = (float)v; return (double)f < v ? std::nextafterf(f, INFINITY) : f; };
     const double h = 0x1p-24, k = bias ? 6.8 : 4.2;
@@ -731,7 +736,6 @@ int tao_bound_linear_int8(const int8_t* A, const float* scale_a, const int8_t* W
     if (!y && !tau) return TAO_ERR_NULL;
     if (!aligned(y, 4) || !aligned(tau, 4)) return TAO_ERR_ALIGN;
     p.y = y; p.tau = tau;
-    p.vec = p.vec && aligned(y, 16) && aligned(tau, 16);
     hipStream_t st = (hipStream_t)stream;
     switch (int8_kind(p)) {
         case kTinyTiles:  return int8_launch_tiles<Int8Tiny>(p, st);
@@ -758,7 +762,6 @@ int tao_bound_check_linear_int8(const int8_t* A, const float* scale_a, const int
     if (!aligned(ws, 256) || ws_bytes < check_workspace_bytes()) return TAO_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     const CheckWorkspace w = carve_check_workspace(ws);
-    p.vec = p.vec && aligned(claimed, 16) && aligned(y_ref, 16);
     tao_fp_model md;
     resolve_model(model, &md);                               // (validated above)
     const Int8CheckArgs c{y_ref, claimed, alpha, eps_rel, quick_alpha(alpha, md), w, n, out};

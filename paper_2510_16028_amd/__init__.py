@@ -201,17 +201,18 @@ def lib():
 
 _torch_module = None
 # what every call asks torch for, looked up once with the module
-_Tensor = _float32 = _raw_stream = _current_device = None
+_Tensor = _float32 = _int8 = _uint8 = _raw_stream = _current_device = _capturing = None
 
 
 def _torch():
     # (asked once: the answer costs more than the launch of a small kernel)
-    global _torch_module, _Tensor, _float32, _raw_stream, _current_device
+    global _torch_module, _Tensor, _float32, _int8, _uint8, _raw_stream, _current_device, _capturing
     if _torch_module is None:
         import torch
         if not torch.cuda.is_available():
             raise RuntimeError("paper_2510_16028_amd needs a GPU: no CPU fallback exists")
-        _Tensor, _float32 = torch.Tensor, torch.float32
+        _Tensor, _float32, _int8, _uint8 = torch.Tensor, torch.float32, torch.int8, torch.uint8
+        _capturing = torch.cuda.is_current_stream_capturing
         _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         _torch_module = torch
     return _torch_module
@@ -871,125 +872,140 @@ def tao_calibrate_thresholds(profiles, alpha=3.0):
 INT8_MAX_K = 131071
 
 
-def _int8(t, name):
-    torch = _torch()
-    if not (isinstance(t, _Tensor) and t.is_cuda and t.dtype is torch.int8):
-        raise TypeError("%s must be an int8 CUDA tensor" % name)
-    return t
+def _wrong(t, dtype, name):
+    if not (isinstance(t, _Tensor) and t.is_cuda and t.dtype is dtype):
+        raise TypeError("%s must be %s CUDA tensor" % (name, "an int8" if dtype is _int8 else "a float32"))
+    raise ValueError("%s is on device %d, the current device is %d" % (name, t.get_device(), _current_device()))
 
 
-def _here(**tensors):
-    """The calls below enqueue on the current device's stream: every tensor has to live there."""
-    here = _current_device()
-    for name, t in tensors.items():
-        if t is not None and t.get_device() != here:
-            raise ValueError("%s is on device %d, the current device is %d" % (name, t.get_device(), here))
+def _on(t, dtype, here, name):
+    """The shape of a tensor of this type on the current device, on whose stream the calls below enqueue."""
+    if isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == here:
+        return t.shape
+    _wrong(t, dtype, name)
 
 
 def _capture_scratch(device, need):
     """_scratch, but a captured graph keeps a workspace of its own (the shared one may grow, and move, before a replay)."""
-    torch = _torch()
-    if torch.cuda.is_current_stream_capturing():
-        return torch.empty(max(int(need), 256), dtype=torch.uint8, device=device)
+    if _capturing():
+        return _torch_module.empty(max(int(need), 256), dtype=_uint8, device=device)
     return _scratch(device, need)
 
 
-def _bytes(t, name, need):
-    if t.dtype != _torch().uint8 or not t.is_contiguous() or t.numel() < need:
-        raise ValueError("%s must be a contiguous uint8 tensor of at least %d bytes" % (name, need))
+def _bytes(t, here, name, need):
+    if not isinstance(t, _Tensor) or t.dtype is not _uint8 or t.get_device() != here or t.numel() < need or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous uint8 tensor of at least %d bytes on the current device" % (name, need))
+    return t
 
 
-def _profile_and_scratch(out, ws, device, need):
-    if out is None:
-        out = new_profile_buffer(device)
-    if ws is None:
-        ws = _capture_scratch(device, need)
-    _here(out=out, ws=ws)
-    _bytes(out, "out", ctypes.sizeof(Profile))
-    _bytes(ws, "ws", need)
+_PROFILE_BYTES = ctypes.sizeof(Profile)
+
+
+def _profile_and_scratch(out, ws, like, here, need):
+    out = new_profile_buffer(like.device) if out is None else _bytes(out, here, "out", _PROFILE_BYTES)
+    ws = _capture_scratch(like.device, need) if ws is None else _bytes(ws, here, "ws", need)
     return out, ws
+
+
+def _vector(t, n, here, name):
+    """A contiguous [n] tensor, or None."""
+    if t is None:
+        return None
+    shape = _on(t, _float32, here, name)
+    if len(shape) != 1 or shape[0] != n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous [%d] tensor" % (name, n))
+    return t.data_ptr()
+
+
+def _output(t, shape, here, name):
+    """The address of a contiguous tensor of this shape."""
+    if _on(t, _float32, here, name) != shape or not t.is_contiguous():
+        raise ValueError("%s must be contiguous and of shape %s" % (name, tuple(shape)))
+    return t.data_ptr()
+
+
+def _reexecuted(y, tau, with_y, with_tau, shape, like, here):
+    """(y, tau, their addresses): made where they are asked for and not given."""
+    if not (with_y or with_tau):
+        raise ValueError("neither y nor tau is asked for")
+    if not with_y:
+        y = None
+    elif y is None:
+        y = _torch_module.empty(shape, dtype=_float32, device=like.device)
+    if not with_tau:
+        tau = None
+    elif tau is None:
+        tau = _torch_module.empty(shape, dtype=_float32, device=like.device)
+    return y, tau, None if y is None else _output(y, shape, here, "y"), None if tau is None else _output(tau, shape, here, "tau")
 
 
 def tao_quantize_rows(x, q=None, scale=None):
     """(q, scale): each row of x[..., cols] as int8 values q[..., cols] times a binary32 scale[...] = max|row| / 127."""
-    torch = _torch()
-    x = _dev(x, "x")
+    torch = _torch_module or _torch()
+    here = _current_device()
+    shape = _on(x, _float32, here, "x")
     rows, cols, ld = _rows_view(x, "x")
     if q is None:
-        q = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+        q = torch.empty(shape, dtype=_int8, device=x.device)
     if scale is None:
-        scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    _int8(q, "q"); _dev(scale, "scale")
-    if q.shape != x.shape or scale.shape != x.shape[:-1] or not scale.is_contiguous():
-        raise ValueError("q must be shaped like x, scale contiguous with one value per row")
+        scale = torch.empty(shape[:-1], dtype=_float32, device=x.device)
+    if _on(q, _int8, here, "q") != shape:
+        raise ValueError("q must be shaped like x")
     ldq = _rows_view(q, "q")[2]
-    _here(x=x, q=q, scale=scale)
-    _check(lib().tao_quantize_rows(x.data_ptr(), q.data_ptr(), scale.data_ptr(), rows, cols, ld, ldq, _stream()), "tao_quantize_rows")
+    rc = lib().tao_quantize_rows(x.data_ptr(), q.data_ptr(), _output(scale, shape[:-1], here, "scale"), rows, cols, ld, ldq, _stream())
+    _check(rc, "tao_quantize_rows")
     return q, scale
 
 
 def _int8_args(A, scale_a, W, scale_w, bias):
-    """Checked operands of the 8-bit product, the output's shape and the sizes and strides of the C call (ldy and strideY left to the caller)."""
-    A = _int8(A, "A"); W = _int8(W, "W")
-    scale_a = _dev(scale_a, "scale_a"); scale_w = _dev(scale_w, "scale_w"); bias = _dev(bias, "bias")
-    As, Ws = A.shape, W.shape
-    if len(As) not in (2, 3) or len(Ws) not in (2, 3):
+    """The current device, the output's shape, and the operands' addresses and the sizes and strides of the C call, checked."""
+    _torch_module or _torch()
+    here = _current_device()
+    As, Ws = _on(A, _int8, here, "A"), _on(W, _int8, here, "W")
+    sas, sws = _on(scale_a, _float32, here, "scale_a"), _on(scale_w, _float32, here, "scale_w")
+    Ad, Wd = len(As), len(Ws)
+    if Ad not in (2, 3) or Wd not in (2, 3):
         raise ValueError("A and W must be 2-D or 3-D")
-    At, Wt = A.stride(), W.stride()
-    for t, stride, nm in ((A, At, "A"), (W, Wt, "W")):
-        if t.shape[-1] > 1 and stride[-1] != 1 and t.numel() > 0:
-            raise ValueError("%s: last dimension must be contiguous" % nm)
-    batch = As[0] if len(As) == 3 else 1
-    M, K, N = As[-2], As[-1], Ws[-2]
+    M, K, N, batch = As[-2], As[-1], Ws[-2], As[0] if Ad == 3 else 1
     if Ws[-1] != K:
         raise ValueError("reduction sizes of A and W differ")
-    if len(Ws) == 3 and Ws[0] != batch:
+    if Wd == 3 and Ws[0] != batch:
         raise ValueError("batch sizes of A and W differ")
-    if scale_a.shape != As[:-1] or not scale_a.is_contiguous() or scale_w.shape != Ws[:-1] or not scale_w.is_contiguous():
+    if sas != As[:-1] or sws != Ws[:-1] or not scale_a.is_contiguous() or not scale_w.is_contiguous():
         raise ValueError("scale_a and scale_w must be contiguous, with one value per row of A and W")
-    if bias is not None and (bias.dim() != 1 or bias.shape[0] != N or not bias.is_contiguous()):
-        raise ValueError("bias must be a contiguous [N] tensor")
-    _here(A=A, scale_a=scale_a, W=W, scale_w=scale_w, bias=bias)
     # (a tensor without elements has no strides to speak of)
-    lda = At[-2] if M > 1 and K > 0 else max(K, 1)
-    ldw = Wt[-2] if N > 1 and K > 0 else max(K, 1)
-    sA = At[0] if len(As) == 3 and batch > 1 and A.numel() > 0 else M * lda
-    sW = 0
-    if len(Ws) == 3 and batch > 1:
-        sW = Wt[0] if W.numel() > 0 else 1               # (0 would share scale_w)
-        if sW == 0:
-            raise ValueError("a W shared by the batch is 2-D, with one scale_w")
-    return (A, scale_a, W, scale_w, bias), As[:-1] + Ws[-2:-1], (M, N, K, lda, ldw, max(N, 1), batch, sA, sW, M * max(N, 1))
-
-
-def _like_output(t, name, shape):
-    t = _dev(t, name)
-    if t is not None and (t.shape != shape or not t.is_contiguous()):
-        raise ValueError("%s must be contiguous and of shape %s" % (name, tuple(shape)))
-    return t
-
-
-def _reexecuted(y, tau, with_y, with_tau, shape, device):
-    torch = _torch()
-    if not (with_y or with_tau):
-        raise ValueError("neither y nor tau is asked for")
-    if y is None and with_y:
-        y = torch.empty(shape, dtype=torch.float32, device=device)
-    if tau is None and with_tau:
-        tau = torch.empty(shape, dtype=torch.float32, device=device)
-    y = _like_output(y, "y", shape) if with_y else None
-    tau = _like_output(tau, "tau", shape) if with_tau else None
-    _here(y=y, tau=tau)
-    return y, tau
+    lda = ldw = K or 1
+    sA, sW = M * lda, 0
+    if A.numel() > 0:
+        t = A.stride()
+        if K > 1 and t[-1] != 1:
+            raise ValueError("A: last dimension must be contiguous")
+        if M > 1:
+            lda = t[-2]
+        sA = t[0] if Ad == 3 and batch > 1 else M * lda
+    if W.numel() > 0:
+        t = W.stride()
+        if K > 1 and t[-1] != 1:
+            raise ValueError("W: last dimension must be contiguous")
+        if N > 1:
+            ldw = t[-2]
+        if Wd == 3 and batch > 1:
+            sW = t[0]
+            if sW == 0:
+                raise ValueError("a W shared by the batch is 2-D, with one scale_w")
+    elif Wd == 3 and batch > 1:
+        sW = 1                                           # (0 would share scale_w)
+    ldy = N or 1
+    return (here, As[:-1] + Ws[-2:-1], (A.data_ptr(), scale_a.data_ptr(), W.data_ptr(), scale_w.data_ptr(), _vector(bias, N, here, "bias")),
+            (M, N, K, lda, ldw, ldy, batch, sA, sW, M * ldy))
 
 
 def tao_bound_linear_int8(A, scale_a, W, scale_w, bias=None, model=None, y=None, tau=None, with_y=True, with_tau=True):
     """(y, tau) of the 8-bit product of A[..., M, K] and W[N, K] / [B, N, K] with a scale for each row of A and W: the output,
     re-executed bit for bit, and its bound (None in the place of one that is not asked for)."""
-    (A, scale_a, W, scale_w, bias), shape, dims = _int8_args(A, scale_a, W, scale_w, bias)
-    y, tau = _reexecuted(y, tau, with_y, with_tau, shape, A.device)
-    rc = lib().tao_bound_linear_int8(A.data_ptr(), scale_a.data_ptr(), W.data_ptr(), scale_w.data_ptr(), _ptr(bias), _ptr(y), _ptr(tau),
-                                     *dims, _mref(model), _stream())
+    here, shape, operands, dims = _int8_args(A, scale_a, W, scale_w, bias)
+    y, tau, yp, tp = _reexecuted(y, tau, with_y, with_tau, shape, A, here)
+    rc = (_lib or lib()).tao_bound_linear_int8(*operands, yp, tp, *dims, _mref(model), _raw_stream(here))
     _check(rc, "tao_bound_linear_int8")
     return y, tau
 
@@ -998,15 +1014,12 @@ def tao_bound_check_linear_int8(A, scale_a, W, scale_w, claimed, bias=None, y_re
                                 out=None, ws=None, readback=True):
     """The 8-bit product re-executed, bounded and checked against `claimed` in one call, nothing else stored (y_ref: check against
     this output instead of the re-executed one).  Returns the profile dict (readback=True) or the device buffer."""
-    (A, scale_a, W, scale_w, bias), shape, dims = _int8_args(A, scale_a, W, scale_w, bias)
-    if claimed is None:
-        raise TypeError("claimed must be a float32 CUDA tensor")
-    claimed = _like_output(claimed, "claimed", shape); y_ref = _like_output(y_ref, "y_ref", shape)
-    _here(claimed=claimed, y_ref=y_ref)
-    out, ws = _profile_and_scratch(out, ws, A.device, lib().tao_check_workspace_bytes(claimed.numel()))
-    rc = lib().tao_bound_check_linear_int8(A.data_ptr(), scale_a.data_ptr(), W.data_ptr(), scale_w.data_ptr(), _ptr(bias), _ptr(y_ref),
-                                           claimed.data_ptr(), *dims, float(alpha), float(eps_rel), _mref(model), out.data_ptr(),
-                                           ws.data_ptr(), ws.numel(), _stream())
+    here, shape, operands, dims = _int8_args(A, scale_a, W, scale_w, bias)
+    L = _lib or lib()
+    cp, rp = _output(claimed, shape, here, "claimed"), None if y_ref is None else _output(y_ref, shape, here, "y_ref")
+    out, ws = _profile_and_scratch(out, ws, A, here, L.tao_check_workspace_bytes(dims[0] * dims[1] * dims[6]))
+    rc = L.tao_bound_check_linear_int8(*operands, rp, cp, *dims, float(alpha), float(eps_rel), _mref(model), out.data_ptr(),
+                                       ws.data_ptr(), ws.numel(), _raw_stream(here))
     _check(rc, "tao_bound_check_linear_int8")
     return read_profile(out) if readback else out
 
@@ -1019,19 +1032,19 @@ def tao_bound_check_groupnorm_act_workspace_bytes(batch, positions, channels, gr
     return int(lib().tao_bound_check_groupnorm_act_workspace_bytes(int(batch), int(positions), int(channels), int(groups)))
 
 
-def _pixels_view(x, name):
+def _pixels_view(x, shape, name):
     """(batch, positions, channels, ld) of x[N, *spatial, C] whose pixels have one uniform stride (a slice of the channels has)."""
-    if x.dim() < 2:
+    if len(shape) < 2:
         raise ValueError("%s must be [N, *spatial, C]" % name)
-    shape, stride = x.shape, x.stride()
     batch, C = shape[0], shape[-1]
     positions = 1
     for d in shape[1:-1]:
         positions *= d
+    if x.is_contiguous() or x.numel() == 0:
+        return batch, positions, C, C or 1
+    stride = x.stride()
     if C > 1 and stride[-1] != 1:
         raise ValueError("%s: last dimension must be contiguous" % name)
-    if x.numel() == 0:
-        return batch, positions, C, max(C, 1)
     ld, step = None, 1
     for d, st in zip(reversed(shape[:-1]), reversed(stride[:-1])):
         if d > 1:
@@ -1044,28 +1057,24 @@ def _pixels_view(x, name):
 
 
 def _groupnorm_act_args(x, groups, gamma, beta):
-    x = _dev(x, "x"); gamma = _dev(gamma, "gamma"); beta = _dev(beta, "beta")
-    batch, positions, C, ld = _pixels_view(x, "x")
-    for t, nm in ((gamma, "gamma"), (beta, "beta")):
-        if t is not None and (t.dim() != 1 or t.shape[0] != C or not t.is_contiguous()):
-            raise ValueError("%s must be a contiguous [C] tensor" % nm)
-    _here(x=x, gamma=gamma, beta=beta)
-    return x, gamma, beta, (batch, positions, C, int(groups), ld, max(C, 1))
+    """The current device, x's shape, the addresses of x, gamma and beta, and the sizes and strides of the C call, checked."""
+    _torch_module or _torch()
+    here = _current_device()
+    shape = _on(x, _float32, here, "x")
+    batch, positions, C, ld = _pixels_view(x, shape, "x")
+    return here, shape, (x.data_ptr(), _vector(gamma, C, here, "gamma"), _vector(beta, C, here, "beta")), (batch, positions, C, int(groups), ld, C or 1)
 
 
 def tao_bound_groupnorm_act(x, groups, gamma=None, beta=None, eps=1e-5, act=ACT_SILU, model=None, y=None, tau=None,
                             with_y=True, with_tau=True, ws=None):
     """(y, tau) of act(GroupNorm(x)) for channels-last x[N, *spatial, C]: the re-executed output and its bound, both contiguous
     (None in the place of one that is not asked for).  act: ACT_SILU, ACT_RELU or ACT_EXACT (none)."""
-    x, gamma, beta, dims = _groupnorm_act_args(x, groups, gamma, beta)
-    y, tau = _reexecuted(y, tau, with_y, with_tau, x.shape, x.device)
-    need = lib().tao_groupnorm_act_workspace_bytes(*dims[:4])
-    if ws is None:
-        ws = _capture_scratch(x.device, need)
-    _here(ws=ws)
-    _bytes(ws, "ws", need)
-    rc = lib().tao_bound_groupnorm_act(int(act), x.data_ptr(), _ptr(gamma), _ptr(beta), float(eps), _ptr(y), _ptr(tau), *dims,
-                                       _mref(model), ws.data_ptr(), ws.numel(), _stream())
+    here, shape, inputs, dims = _groupnorm_act_args(x, groups, gamma, beta)
+    L = _lib or lib()
+    y, tau, yp, tp = _reexecuted(y, tau, with_y, with_tau, shape, x, here)
+    need = L.tao_groupnorm_act_workspace_bytes(*dims[:4])
+    ws = _capture_scratch(x.device, need) if ws is None else _bytes(ws, here, "ws", need)
+    rc = L.tao_bound_groupnorm_act(int(act), *inputs, float(eps), yp, tp, *dims, _mref(model), ws.data_ptr(), ws.numel(), _raw_stream(here))
     _check(rc, "tao_bound_groupnorm_act")
     return y, tau
 
@@ -1074,14 +1083,12 @@ def tao_bound_check_groupnorm_act(x, claimed, groups, gamma=None, beta=None, eps
                                   eps_rel=1e-12, model=None, out=None, ws=None, readback=True):
     """act(GroupNorm(x)) re-executed, bounded and checked against `claimed` in one call, nothing else stored (y_ref: check against
     this output instead of the re-executed one).  Returns the profile dict (readback=True) or the device buffer."""
-    x, gamma, beta, dims = _groupnorm_act_args(x, groups, gamma, beta)
-    if claimed is None:
-        raise TypeError("claimed must be a float32 CUDA tensor")
-    claimed = _like_output(claimed, "claimed", x.shape); y_ref = _like_output(y_ref, "y_ref", x.shape)
-    _here(claimed=claimed, y_ref=y_ref)
-    out, ws = _profile_and_scratch(out, ws, x.device, lib().tao_bound_check_groupnorm_act_workspace_bytes(*dims[:4]))
-    rc = lib().tao_bound_check_groupnorm_act(int(act), x.data_ptr(), _ptr(gamma), _ptr(beta), float(eps), _ptr(y_ref), claimed.data_ptr(), *dims,
-                                             float(alpha), float(eps_rel), _mref(model), out.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
+    here, shape, inputs, dims = _groupnorm_act_args(x, groups, gamma, beta)
+    L = _lib or lib()
+    cp, rp = _output(claimed, shape, here, "claimed"), None if y_ref is None else _output(y_ref, shape, here, "y_ref")
+    out, ws = _profile_and_scratch(out, ws, x, here, L.tao_bound_check_groupnorm_act_workspace_bytes(*dims[:4]))
+    rc = L.tao_bound_check_groupnorm_act(int(act), *inputs, float(eps), rp, cp, *dims, float(alpha), float(eps_rel), _mref(model),
+                                         out.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(here))
     _check(rc, "tao_bound_check_groupnorm_act")
     return read_profile(out) if readback else out
 

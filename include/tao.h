@@ -398,11 +398,11 @@ size_t tao_groupnorm_workspace_bytes(long batch, long channels, long positions, 
  * y is the formula in binary64, rounded once to binary32; no re-executed output is needed for tau.  tau is at or above its formula's value and
  * within 1e-6 of it (for RELU within 1e-6 E).  A group whose bound is not finite gets NaN, as in tao_bound_norm.
  * x: pixel stride ldx >= channels; y, tau: pixel stride ldy; samples follow each other; either of y, tau may be NULL (not stored).  gamma, beta:
- * [channels] or NULL.  16-byte vectors are used where channels, ldx and ldy are multiples of 4 and the tensors 16-byte aligned.
+ * [channels] or NULL.  Any address and stride of whole elements; channels that are a multiple of 4 (of 2) move as vectors of as many.
  * ws / ws_bytes: DEVICE scratch of tao_groupnorm_act_workspace_bytes(...), 256-byte aligned, contents irrelevant before and
- * garbage after; calls that share ws must be ordered on one stream.
+ * garbage after; calls that share ws must be ordered on one stream.  The query is 0, and ws may be NULL, where one workgroup a group does.
  * TAO_ERR_KIND for another act; TAO_ERR_SHAPE when channels is not a multiple of groups, a group has 2^31 elements or more, the
- * tensor 2^36 or more, or the batch exceeds about 16 million samples; TAO_ERR_K_RANGE as for tao_bound_norm's LAYERNORM. */
+ * tensor 2^36 or more, or there are 2^22 groups of samples (batch times groups) or more; TAO_ERR_K_RANGE as for tao_bound_norm's LAYERNORM. */
 int tao_bound_groupnorm_act(int act, const float *x, const float *gamma, const float *beta, double eps, float *y, float *tau,
                             long batch, long positions, long channels, long groups, long ldx, long ldy,
                             const tao_fp_model *model, void *ws, size_t ws_bytes, void *stream);

@@ -178,7 +178,7 @@ struct Int8Check {
         const unsigned int known = newest(largest);
         bool ok = accurate && cols == 4 && ordinary;
         if (y_ref) ok = ok && fmaxf(fmaxf(fabsf(y[0]), fabsf(y[1])), fmaxf(fabsf(y[2]), fabsf(y[3]))) <= 0x1p100f;
-        if (settle(a.c, y, t, known, ok)) return;
+        if (settle_four(a.c, y, t, q, known, ok, acc, zeros, [&](unsigned bin) __attribute__((always_inline)) { Int8Bins::add(hist, bin); })) return;
         if (ROOM && known == 0 && accurate && cols == 4) {
             const float c4[4] = {a.c[0], a.c[1], a.c[2], a.c[3]}, y4[4] = {y[0], y[1], y[2], y[3]}, t4[4] = {t[0], t[1], t[2], t[3]};
             check_four<1>(c4, y4, t4, alpha, eps_rel, hist, 0, acc);
@@ -198,29 +198,6 @@ struct Int8Check {
             }
         }
         if (acc.max_bits > known) atomicMax(largest, acc.max_bits);
-    }
-    // Quick settlement (tao_check.hpp) of four claims at once, also of those that leave their bounds.  `at`, alpha tau to within 2^-17, decides a comparison that
-    // d misses by more than 2^-13 of it; the error's estimate a bin that it is 16 steps inside of (of 0 and of the smallest ones, whose bin has no
-    // lower edge, too).  What is no number, or too large, has an estimate beyond any error that occurs.
-    __device__ __forceinline__ bool settle(floatv4 c, floatv4 r, floatv4 t, unsigned int known, bool ok) {
-        unsigned int bits[4], lowest = ~0u, highest = 0u, out = 0;
-        float clear = INFINITY;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float d = fabsf(c[e] - r[e]), at = t[e] * q.alpha;
-            bits[e] = max(__float_as_uint(d * __builtin_amdgcn_rcpf(fabsf(r[e]) + q.eps)), 64u) + 16u;
-            lowest = min(lowest, bits[e] & 0xfffffu);
-            highest = max(highest, bits[e]);
-            clear = fminf(clear, fmaf(at, -0x1p-13f, fabsf(d - at)));
-            out += d > at;
-        }
-        if (!(ok && lowest >= 32u && highest <= known && clear > 0x1p-90f)) return false;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (bits[e] == 80u) ++zeros; else Int8Bins::add(hist, bits[e] >> 20);
-        }
-        acc.violations += out;
-        return true;
     }
     // (before the histogram is read, with a barrier behind)
     __device__ __forceinline__ void finish() { if (zeros) atomicAdd(&hist[0], zeros); }

@@ -19,6 +19,7 @@ struct BlockStats {          // one per pass-1 workgroup, in the workspace after
     unsigned int flag;       // not a counter: no pass writes it (linear_screen.hpp)
 };
 
+typedef float floatv4 __attribute__((ext_vector_type(4)));      // (indexed by a variable it stays in registers)
 struct ThreadAcc {
     unsigned int violations = 0, nans = 0, max_bits = 0;
 };
@@ -126,7 +127,6 @@ __device__ __forceinline__ bool quick_settled(float c, float r, float at, const 
     const float lhs = zero ? 0.f : fmaf(d, 1.f + 0x1p-16f, 0x1p-90f);     // (a bound near the subnormal range settles nothing)
     return lhs <= at && at <= 0x1p120f && den <= 0x1p100f && (zero || ((t & 0xfffffu) >= 32u && t <= known));
 }
-typedef float floatv4 __attribute__((ext_vector_type(4)));      // (indexed by a variable it stays in registers)
 // Four elements: settled together or checked exactly, with tau(i) the binary32 bound of element i.  largest: the
 // workgroup's largest exactly computed error (LDS), known: this thread's copy, no newer than it needs to be.  WIDE: the
 // exact way takes the four side by side, for kernels that have the registers (small tensors see little else);
@@ -162,6 +162,33 @@ __device__ __forceinline__ bool quick_check_four(floatv4 c, floatv4 r, floatv4 a
     if (acc.max_bits > known) atomicMax(largest, acc.max_bits);
     known = max(known, acc.max_bits);
     return false;
+}
+// Quick settlement of four claims at once, also of those that leave their bounds, for kernels that have their elements in fours; t: binary32 bounds,
+// ok: whether estimates may be taken at all (q.alpha and q.eps ordinary, |r| at most 2^100, t at most 2^90).  alpha t to within 2^-17 decides a comparison
+// that d misses by more than 2^-13 of it; the error's estimate, a bin that it is 16 steps inside of (of 0 and of the smallest ones, whose bin has
+// no lower edge, too).  What is no number, or too large, has an estimate beyond any error that occurs.  add(bin) counts an element.
+template <class Add>
+__device__ __forceinline__ bool settle_four(floatv4 c, floatv4 r, floatv4 t, const QuickCheck& q, unsigned known, bool ok, ThreadAcc& acc, unsigned int& zeros, Add&& add) {
+    unsigned int bits[4], lowest = ~0u, highest = 0u, out = 0;
+    float clear = INFINITY, furthest = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float d = fabsf(c[e] - r[e]), at = t[e] * q.alpha;
+        furthest = fmaxf(furthest, d);
+        bits[e] = max(__float_as_uint(d * __builtin_amdgcn_rcpf(fabsf(r[e]) + q.eps)), 64u) + 16u;
+        lowest = min(lowest, bits[e] & 0xfffffu);
+        highest = max(highest, bits[e]);
+        clear = fminf(clear, fmaf(at, -0x1p-13f, fabsf(d - at)));
+        out += d > at;
+    }
+    // (four errors of 0 need no error that occurs)
+    if (!(ok && lowest >= 32u && (highest <= known || (highest == 80u && furthest == 0.f)) && clear > 0x1p-90f)) return false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (bits[e] == 80u) ++zeros; else add(bits[e] >> 20);
+    }
+    acc.violations += out;
+    return true;
 }
 __device__ __forceinline__ unsigned newest(unsigned int* largest) {
     return __hip_atomic_load(largest, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);

@@ -46,7 +46,8 @@ def assert_outputs(y, tau, ye, te, E, act):
 
 
 SHAPES = [(1, 1, 4, 1), (1, 1, 4, 2), (2, 3, 5, 5), (1, 7, 6, 3), (2, 64, 1280, 32), (3, 50, 40, 8), (1, 300, 37, 1), (2, 256, 320, 32), (1, 1024, 128, 32),
-          (4, 33, 96, 96), (1, 5000, 8, 2), (2, 500, 516, 4), (1, 100, 2048, 1), (1, 20, 4100, 4), (1, 9000, 12, 1), (40, 10, 64, 16), (300, 4, 12, 3), (1, 17, 1030, 515), (1, 3, 700, 700)]
+          (4, 33, 96, 96), (1, 5000, 8, 2), (2, 500, 516, 4), (1, 100, 2048, 1), (1, 20, 4100, 4), (1, 9000, 12, 1), (40, 10, 64, 16), (300, 4, 12, 3), (1, 17, 1030, 515), (1, 3, 700, 700),
+          (2, 2500, 320, 32), (1, 1300, 1030, 103), (520, 1, 12, 3), (8, 100, 256, 64), (1, 513, 2052, 513)]
 
 
 @pytest.mark.parametrize("B,P,C,groups", SHAPES)

@@ -64,10 +64,11 @@ def test_quantisation_refusals(tao):
 
 def test_groupnorm_act_refusals(tao):
     L = tao.lib()
-    need = L.tao_groupnorm_act_workspace_bytes(2, 16, 8, 4)
+    need = L.tao_groupnorm_act_workspace_bytes(2, 4096, 8, 4)
     assert need > 0
+    assert L.tao_groupnorm_act_workspace_bytes(2, 16, 8, 4) == 0      # one workgroup a group: nothing to keep
 
-    def call(act=tao.ACT_SILU, x=P, g=P, b=P, eps=1e-5, y=P, tau=P, batch=2, positions=16, channels=8, groups=4, ldx=8, ldy=8, model=None, ws=P, bytes=need):
+    def call(act=tao.ACT_SILU, x=P, g=P, b=P, eps=1e-5, y=P, tau=P, batch=2, positions=4096, channels=8, groups=4, ldx=8, ldy=8, model=None, ws=P, bytes=need):
         return L.tao_bound_groupnorm_act(act, x, g, b, eps, y, tau, batch, positions, channels, groups, ldx, ldy, model, ws, bytes, None)
     assert call(act=tao.ACT_GELU_ERF) == call(act=-1) == call(act=99) == tao.ERR_KIND
     assert call(groups=3) == call(groups=0) == call(batch=-1) == call(positions=-1) == call(channels=-4) == tao.ERR_SHAPE
@@ -81,11 +82,11 @@ def test_groupnorm_act_refusals(tao):
     for k in ("batch", "positions", "channels"):
         assert call(**{k: 0}, x=NUL, y=NUL, tau=NUL, ws=NUL, bytes=0) == tao.OK, k
 
-    cneed = L.tao_bound_check_groupnorm_act_workspace_bytes(2, 16, 8, 4)
-    assert cneed == need + L.tao_check_workspace_bytes(256)
+    cneed = L.tao_bound_check_groupnorm_act_workspace_bytes(2, 4096, 8, 4)
+    assert cneed == need + L.tao_check_workspace_bytes(2 * 4096 * 8)
 
     def check(act=tao.ACT_SILU, y_ref=NUL, claimed=P, alpha=1.0, eps=0.0, out=P, ws=P, bytes=cneed, groups=4):
-        return L.tao_bound_check_groupnorm_act(act, P, P, P, 1e-5, y_ref, claimed, 2, 16, 8, groups, 8, 8, alpha, eps, None, out, ws, bytes, None)
+        return L.tao_bound_check_groupnorm_act(act, P, P, P, 1e-5, y_ref, claimed, 2, 4096, 8, groups, 8, 8, alpha, eps, None, out, ws, bytes, None)
     assert check(act=3) == tao.ERR_KIND and check(groups=5) == tao.ERR_SHAPE
     for v in (-1.0, float("nan"), float("inf")):
         assert check(alpha=v) == check(eps=v) == tao.ERR_SHAPE

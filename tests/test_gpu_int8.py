@@ -195,7 +195,7 @@ def test_checks_of_nothing(tao):
         assert y.shape == (M, N)
 
 
-@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 5), (7, 64), (2, 255), (5, 256), (64, 257), (9, 1000), (3, 1024), (4, 2049), (6, 4096), (2, 5001), (3, 12288), (1, 40000), (700, 33), (20000, 17)])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 5), (7, 64), (2, 255), (5, 256), (64, 257), (9, 1000), (3, 1024), (4, 2049), (6, 4096), (2, 5001), (3, 12288), (1, 40000), (700, 33), (20000, 17), (8, 2), (2, 16385), (3, 32769), (17000, 1030), (5, 4)])
 def test_quantised_rows_bit_for_bit(tao, rows, cols):
     rng = np.random.default_rng(rows * cols)
     x = (rng.normal(0, 1, (rows, cols)) * np.exp(rng.normal(0, 3, (rows, 1)))).astype(np.float32)
@@ -219,6 +219,27 @@ def test_quantised_rows_of_every_alignment(tao):
         qe, _ = int8.quantize_rows(x.cpu().numpy())
         assert np.array_equal(q.cpu().numpy(), qe)
         assert bool((store[atq:].view(rows, ldq)[:, cols:] == 99).all()) and bool((store[:atq] == 99).all())
+
+
+@pytest.mark.parametrize("largest", [127.0, 1.0, 3.7e-5, 2.9e30, 1e-38, 2.0 ** -93, 2.0 ** -94])
+def test_quotients_in_the_middle_of_two_whole_numbers(tao, largest):
+    """The rounded quotient decides, at ties to even: arguments at and next to every middle, also where the scale is next to having no reciprocal."""
+    m = np.float32(largest)
+    s = m / np.float32(127)
+    k = (np.arange(-127, 127) + 0.5).astype(np.float32)
+    x = [m]
+    for step in range(-3, 4):
+        v = (k * s).astype(np.float32)
+        for _ in range(abs(step)):
+            v = np.nextafter(v, np.float32(np.inf if step > 0 else -np.inf))
+        x.append(v)
+    x = np.hstack(x).astype(np.float32)
+    assert np.abs(x).max() == m
+    for cols in (len(x), 1000, 200, 60):
+        rows = np.stack([np.concatenate([[m], c]) for c in np.array_split(x[1:], max(1, len(x) // cols)) for c in [np.resize(c, cols - 1)]]).astype(np.float32)
+        q, scale = tao.tao_quantize_rows(cuda(rows)[0])
+        qe, se = int8.quantize_rows(rows)
+        assert np.array_equal(scale.cpu().numpy(), se) and np.array_equal(q.cpu().numpy(), qe)
 
 
 def test_refusals_of_the_binding(tao):

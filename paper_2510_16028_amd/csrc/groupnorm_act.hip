@@ -491,7 +491,19 @@ __global__ __launch_bounds__(kNormThreads) void norm_sums(NormArgs p) {
     __shared__ __align__(16) double smem[2 * kNormThreads * VEC];
     double* mean = smem;                                     // of the block's groups, read before the sums are left there
     const Place<VEC> at(p, blockIdx.x);
+    const float* x = p.x + at.s * p.positions * p.ldx + at.c0;
+    const long end = at.active ? at.p1 : 0;
     double mu[VEC] = {}, v[VEC][2] = {};
+    // (the first pixels are on their way while the means are added up)
+    constexpr int AHEAD = 4;
+    float e[AHEAD][VEC];
+    long i = at.p0 + at.ty;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) e[k][c] = 0.f;
+        if (i + k * at.TY < end) load_floats<VEC, false>(x + (i + k * at.TY) * p.ldx, e[k]);
+    }
     if constexpr (DEVIATIONS) {
         group_totals<false>(p, at, [&](int g, const double2& t, const double2&) __attribute__((always_inline)) { mean[g] = t.x * p.k.inv_n; });
         __syncthreads();
@@ -501,19 +513,23 @@ __global__ __launch_bounds__(kNormThreads) void norm_sums(NormArgs p) {
         }
         __syncthreads();
     }
-    if (at.active) {
-        const float* x = p.x + at.s * p.positions * p.ldx + at.c0;
-#pragma unroll 4
-        for (long i = at.p0 + at.ty; i < at.p1; i += at.TY) {
-            float e[VEC];
-            load_floats<VEC, false>(x + i * p.ldx, e);
+    auto add = [&](const float (&f)[VEC]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int c = 0; c < VEC; ++c) {
-                const double d = DEVIATIONS ? (double)e[c] - mu[c] : (double)e[c];
-                if constexpr (DEVIATIONS) { v[c][0] += fabs(d); v[c][1] = fma(d, d, v[c][1]); }
-                else                      { v[c][0] += d; v[c][1] += fabs(d); }
-            }
+        for (int c = 0; c < VEC; ++c) {
+            const double d = DEVIATIONS ? (double)f[c] - mu[c] : (double)f[c];
+            if constexpr (DEVIATIONS) { v[c][0] += fabs(d); v[c][1] = fma(d, d, v[c][1]); }
+            else                      { v[c][0] += d; v[c][1] += fabs(d); }
         }
+    };
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+        if (i + k * at.TY < end) add(e[k]);
+    i += AHEAD * at.TY;
+#pragma unroll 4
+    for (; i < end; i += at.TY) {
+        float f[VEC];
+        load_floats<VEC, false>(x + i * p.ldx, f);
+        add(f);
     }
     channel_sums<VEC>(p, at, v, smem, DEVIATIONS ? 1 : 0);
 }
@@ -522,7 +538,25 @@ __global__ __launch_bounds__(kNormThreads) void norm_sums(NormArgs p) {
 template <int ACT, int VEC, class Sink>
 __device__ __forceinline__ void norm_part(const NormArgs& p, long item, GroupCoef* coef, Sink& sink) {
     const Place<VEC> at(p, item);
-    group_totals<true>(p, at, [&](int g, const double2& t, const double2& d) __attribute__((always_inline)) { coef[g] = group_coef(p.k, p.n, t.x, t.y, d.x, d.y); });
+    // (the next four elements are requested while four are computed, the first while the totals are added up; left: pixels from the thread's next one to the part's end)
+    constexpr int PIX = kPixels<VEC>;
+    const long step_x = at.TY * p.ldx, step_y = at.TY * p.ldy, pixel = at.s * p.positions + at.p0 + at.ty;
+    const float* x = p.x + pixel * p.ldx + at.c0;
+    long out = pixel * p.ldy + at.c0;
+    int left = at.active ? (int)(at.p1 - at.p0) - at.ty : 0;
+    float e1[4], claims1[4];
+    const auto request = [&]() __attribute__((always_inline)) {
+        load_quad<VEC, true>(x, [&](int j) { return j == 0 ? 0 : plain(j * at.TY < left ? j * step_x : 0); }, e1);
+        sink.template request<VEC>([&](int j) { return j == 0 ? out : plain(j * at.TY < left ? out + j * step_y : out); }, claims1);
+    };
+    if (left > 0) request();
+    // (totals first, then a thread a group: a chain of dependent operations, run once for all groups)
+    group_totals<true>(p, at, [&](int g, const double2& t, const double2& d) __attribute__((always_inline)) { coef[g].mu = t.x; coef[g].r = t.y; coef[g].K1 = d.x; coef[g].K0 = d.y; });
+    __syncthreads();
+    for (int g = thread_here(); g < at.g_hi - at.g_lo; g += kNormThreads) {
+        const GroupCoef t = coef[g];
+        coef[g] = group_coef(p.k, p.n, t.mu, t.r, t.K1, t.K0);
+    }
     __syncthreads();
     if (!at.active) return;
     ChannelCoef ch[VEC];
@@ -534,18 +568,6 @@ __device__ __forceinline__ void norm_part(const NormArgs& p, long item, GroupCoe
         m = fmax(m, g.m);
     }
     const UpFactors up(m);
-    // (the next four elements are requested while four are computed; left: pixels from the thread's next one to the part's end)
-    constexpr int PIX = kPixels<VEC>;
-    const long step_x = at.TY * p.ldx, step_y = at.TY * p.ldy, pixel = at.s * p.positions + at.p0 + at.ty;
-    const float* x = p.x + pixel * p.ldx + at.c0;
-    long out = pixel * p.ldy + at.c0;
-    int left = (int)(at.p1 - at.p0) - at.ty;
-    float e1[4], claims1[4];
-    const auto request = [&]() __attribute__((always_inline)) {
-        load_quad<VEC, true>(x, [&](int j) { return j == 0 ? 0 : plain(j * at.TY < left ? j * step_x : 0); }, e1);
-        sink.template request<VEC>([&](int j) { return j == 0 ? out : plain(j * at.TY < left ? out + j * step_y : out); }, claims1);
-    };
-    if (left > 0) request();
     while (left > 0) {
         float e[4], claims[4], ref[4], y[4], t[4];
         const long here = out;
@@ -602,7 +624,7 @@ static NormParts norm_parts(long batch, long positions, long channels) {
     return r;
 }
 // Whether one workgroup a group does: groups of at most two vectors a thread; no more than two workgroups a compute unit, as each walks through its sums and its outputs on
-// its own; and little work in all.  GPU us, norm_rows / the three passes, bound and check: 2 x 64 x 1280 in 32 groups 8.0 / 18 and 17 / 29, 2 x 256 x 1024 11 / 18 and 21 / 29,
+// its own; and little work in all.  GPU us, norm_rows / the three passes, bound and check: 2 x 64 x 1280 in 32 groups 7.5 / 18 and 17 / 29, 2 x 256 x 1024 11 / 18 and 21 / 29,
 // 16 x 64 x 1024 8.8 / 19 and 23 / 29; beyond, 2 x 256 x 2048 20 / 20 and 39 / 30, 16 x 256 x 1024 23 / 31 and 37 / 40, 64 x 16 x 256 in 64 16 / 16 and 87 / 25.
 static bool holds_row(long batch, long positions, long channels, long groups) {
     const long per = channels / groups, vectors = per / channel_vec(per) * positions, rows = batch * groups;
@@ -667,7 +689,8 @@ template <int ACT, int VEC>
 static void rows_launch(const NormArgs& p, hipStream_t st) {
     const dim3 grid((unsigned)((p.batch * p.groups + 7) / 8 * 8));
     const long vectors = (long)p.per / VEC * p.positions;
-    if (vectors <= 4 * 256)               hipLaunchKernelGGL((norm_rows<ACT, VEC, 4, 256>), grid, dim3(256), 0, st, p);
+    // (320 vectors: 6.3 us with 256 threads, 6.5 with 1024; 640: 8.0 and 7.5)
+    if (vectors <= 2 * 256)               hipLaunchKernelGGL((norm_rows<ACT, VEC, 2, 256>), grid, dim3(256), 0, st, p);
     else                                  hipLaunchKernelGGL((norm_rows<ACT, VEC, kRowVectors, kNormThreads>), grid, dim3(kNormThreads), 0, st, p);
 }
 template <int ACT>

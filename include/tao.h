@@ -402,7 +402,7 @@ size_t tao_groupnorm_workspace_bytes(long batch, long channels, long positions, 
  * ws / ws_bytes: DEVICE scratch of tao_groupnorm_act_workspace_bytes(...), 256-byte aligned, contents irrelevant before and
  * garbage after; calls that share ws must be ordered on one stream.  The query is 0, and ws may be NULL, where one workgroup a group does.
  * TAO_ERR_KIND for another act; TAO_ERR_SHAPE when channels is not a multiple of groups, a group has 2^31 elements or more, the
- * tensor 2^36 or more, or there are 2^22 groups of samples (batch times groups) or more; TAO_ERR_K_RANGE as for tao_bound_norm's LAYERNORM. */
+ * tensor 2^36 or more, or there are 2^22 groups (batch times groups) or more, or as many blocks of 512 channels; TAO_ERR_K_RANGE as for tao_bound_norm's LAYERNORM. */
 int tao_bound_groupnorm_act(int act, const float *x, const float *gamma, const float *beta, double eps, float *y, float *tau,
                             long batch, long positions, long channels, long groups, long ldx, long ldy,
                             const tao_fp_model *model, void *ws, size_t ws_bytes, void *stream);

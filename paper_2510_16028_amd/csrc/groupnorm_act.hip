@@ -11,6 +11,7 @@
 // be known before the deviations, and sum |d| with it: (a) sum x, sum |x|, (b) sum |d|, sum d^2, (c) the outputs; every workgroup of (b) and (c) adds up
 // the parts of its groups in the same order.  4 x 16384 x 512 SiLU: 24 + 24 + 70 us (134 MB read at 5.5 TB/s twice, 402 MB moved at 5.7 TB/s); the check in place
 // of (c) 92 us, bound by its instructions (about 95 an element, 40 of them binary64, four cycles each).
+#include <algorithm>
 #include <type_traits>
 #include "tao_check.hpp"
 #include "tao_device.hpp"
@@ -23,11 +24,11 @@ struct NormArgs {
     const float* x; const float* gamma; const float* beta;
     float* y; float* tau;
     const float* y_ref; const float* claimed;
-    double2* part;                   // [sample][2][group][part]: (sum x, sum |x|), (sum |d|, sum d^2)
+    double2* part;                   // [sample][2][group][column block of the group, pixel part]: (sum x, sum |x|), (sum |d|, sum d^2)
     long positions, ldx, ldy, batch;
     int channels, groups, per;
-    int nparts;                      // of a sample: pixel parts x column blocks
-    int ncb;                         // column blocks
+    int ncb, pixel_parts;            // of a sample: column blocks, parts of its pixels
+    int span;                        // column blocks that a group lies in, at most
     long pixels;                     // of a part
     RowConsts k;
     double silu_k;                   // silu_f / (1 - silu_f)
@@ -66,7 +67,7 @@ __device__ __forceinline__ void store_floats(float* __restrict__ p, const float 
 // ---- one element
 
 // What an element's bound takes of its group.
-struct GroupCoef { double mu, r, K1, K0, m; };
+struct GroupCoef { double mu, r, K1, K0; };
 // The thread's number, of which nothing is formed ahead: in loops over rows or items the compiler else keeps what follows from it from trip to trip, in registers that
 // the loops over pixels then lack.
 __device__ __forceinline__ int thread_here() {
@@ -91,7 +92,9 @@ __device__ __forceinline__ GroupCoef group_coef(const RowConsts& k, double n, do
     const double E_mu = ((k.G * s_ax) * k.inv_n + k.cd_u * fabs(c.mu)) * k.inv1mcd;
     double amp;
     layernorm_tail(E_mu, s_ad, s_d2, n, k, c.K1, c.K0, amp, &c.r);
-    c.m = amp > 0.0 && amp < INFINITY ? k.m * (1.0 + 2.0 * amp) : 0.0;      // (else K0 is NaN, and so is the bound)
+    // the group's own rounding margin goes into its E_p, which everything after it grows with: neighbours in a thread may be of another group
+    const double m = amp > 0.0 && amp < INFINITY ? k.m * (1.0 + 2.0 * amp) : 0.0;      // (else K0 is NaN, and so is the bound)
+    c.K1 *= 1.0 + 2.0 * m; c.K0 *= 1.0 + 2.0 * m;
     return c;
 }
 // ... and of its channel: p = d rg + b, E_p = k1 |d| + k0
@@ -130,7 +133,8 @@ __device__ __forceinline__ double sigmoid(double p, double& rest) {
 // Output and bound of one element.  The slacks keep an evaluation in round-to-nearest binary64 at or above the formula's value: near
 // a zero of s' its relative error is large, but 2^-36 (the sigmoid's error many times over) of E is far below 1e-6 of the other terms.
 template <int ACT>
-__device__ __forceinline__ void norm_element(float x, const ChannelCoef& c, double u, double silu_k, double mul, double sub, float& y, float& tau) {
+__device__ __forceinline__ void norm_element(float x, const ChannelCoef& c, double u, double silu_k, float& y, float& tau) {
+    constexpr double mul = 1.0 + 0x1p-24 + 0x1p-32, sub = 1.0 + 0x1p-48;      // (of the final upper rounding: the few roundings of an element)
     const double d = (double)x - c.mu;
     const double p = fma(d, c.rg, c.b);
     const double ep = fma(c.k1, fabs(d), c.k0);
@@ -286,7 +290,6 @@ __device__ __forceinline__ void norm_row(const NormArgs& p, long row, double* sm
     }
     block_sums<THREADS>(b, smem + 2 * (THREADS / kWave));
     const GroupCoef coef = group_coef(p.k, p.n, a[0], a[1], b[0], b[1]);
-    const UpFactors up(coef.m);
     const long out = s * p.positions * p.ldy + (long)g * p.per;
     // (a loop that reads x again, from the caches, and the next four elements while four are computed: unrolled over the registers it would take several times the
     // code, and registers that spill)
@@ -331,7 +334,7 @@ __device__ __forceinline__ void norm_row(const NormArgs& p, long row, double* sm
 #pragma unroll 1
         for (int e = 0; e < 4; ++e) {
             float y1, t1;
-            norm_element<ACT>(xv[0], channel_coef(coef, p.gamma, p.beta, (int)of[0]), p.k.u, p.silu_k, up.mul, up.sub, y1, t1);
+            norm_element<ACT>(xv[0], channel_coef(coef, p.gamma, p.beta, (int)of[0]), p.k.u, p.silu_k, y1, t1);
 #pragma unroll
             for (int i = 0; i < 3; ++i) { xv[i] = xv[i + 1]; of[i] = of[i + 1]; y[i] = y[i + 1]; t[i] = t[i + 1]; }
             y[3] = y1; t[3] = t1;
@@ -382,13 +385,15 @@ constexpr int kColumns = 512;
 template <int VEC>
 struct Place {
     long s, p0, p1;
-    int part, TX, TY, tx, ty, c0, c_lo, c_hi, g_lo, g_hi;
+    int cb, part, TX, TY, tx, ty, c0, c_lo, c_hi, g_lo, g_hi;
     bool active;
     __device__ __forceinline__ Place(const NormArgs& p, long item) {
         const int tid = thread_here();
-        s = item / p.nparts; part = (int)(item - s * p.nparts);
-        const int cb = part % p.ncb;
-        p0 = part / p.ncb * p.pixels; p1 = min(p0 + p.pixels, p.positions);
+        const long of_sample = (long)p.pixel_parts * p.ncb;
+        s = item / of_sample;
+        const int in = (int)(item - s * of_sample);
+        part = in / p.ncb; cb = in - part * p.ncb;
+        p0 = part * p.pixels; p1 = min(p0 + p.pixels, p.positions);
         c_lo = cb * kColumns;
         TX = min(kColumns, p.channels - c_lo) / VEC;
         TY = kNormThreads / TX;
@@ -399,7 +404,9 @@ struct Place {
         g_lo = c_lo / p.per; g_hi = (c_hi - 1) / p.per + 1;
     }
 };
-__device__ __forceinline__ double2* parts_of(const NormArgs& p, long s, int which, int g) { return p.part + ((s * 2 + which) * p.groups + g) * p.nparts; }
+__device__ __forceinline__ double2* parts_of(const NormArgs& p, long s, int which, int g) { return p.part + ((s * 2 + which) * p.groups + g) * p.span * p.pixel_parts; }
+__device__ __forceinline__ int first_block(const NormArgs& p, int g) { return g * p.per / kColumns; }
+__device__ __forceinline__ int parts_in(const NormArgs& p, int g) { return (((g + 1) * p.per - 1) / kColumns - first_block(p, g) + 1) * p.pixel_parts; }
 
 // A number of lanes for `items` items: enough that each has few.
 template <class Use> __device__ __forceinline__ void with_lanes(int items, Use&& use) {
@@ -409,7 +416,7 @@ template <class Use> __device__ __forceinline__ void with_lanes(int items, Use&&
     else                  use(std::integral_constant<int, 64>());
 }
 
-// The threads' sums v[channel][i] to those of the block's groups, this part's entry of each; groups without a channel here get 0.  Where a thread's channels are of
+// The threads' sums v[channel][i] to those of the block's groups, this part's entry of each.  Where a thread's channels are of
 // one group, the thread leaves one entry, else one a channel; the lanes of a group then take its entries of all rows of threads, so the number of threads
 // that add does not depend on the number of channels.  smem: 2 kNormThreads VEC doubles.
 template <int VEC>
@@ -429,9 +436,6 @@ __device__ __forceinline__ void channel_sums(const NormArgs& p, const Place<VEC>
         }
     }
     __syncthreads();
-    double2* out = parts_of(p, at.s, which, 0) + at.part;
-    for (int g = threadIdx.x; g < p.groups; g += kNormThreads)
-        if (g < at.g_lo || g >= at.g_hi) out[(long)g * p.nparts] = make_double2(0.0, 0.0);
     with_lanes(kNormThreads / (at.g_hi - at.g_lo), [&](auto lanes) __attribute__((always_inline)) {
         constexpr int LANES = decltype(lanes)::value, AT_ONCE = kNormThreads / LANES;
         const int sub = threadIdx.x % LANES;
@@ -445,7 +449,7 @@ __device__ __forceinline__ void channel_sums(const NormArgs& p, const Place<VEC>
                 for (int t = row; t < at.TY; t += rows)
                     for (int c = first_c; c < n; c += LANES) { const double2 q = entry[t * width + lo - lo_c + c]; s.x += q.x; s.y += q.y; }
             s.x = lanes_sum<LANES>(s.x); s.y = lanes_sum<LANES>(s.y);
-            if (sub == 0 && g < at.g_hi) out[(long)g * p.nparts] = s;
+            if (sub == 0 && g < at.g_hi) parts_of(p, at.s, which, g)[(at.cb - first_block(p, g)) * p.pixel_parts + at.part] = s;
         }
     });
 }
@@ -453,7 +457,7 @@ __device__ __forceinline__ void channel_sums(const NormArgs& p, const Place<VEC>
 // (The parts come from other XCDs, through memory: four of each sum are requested at a time.)
 template <bool BOTH, int VEC, class Use>
 __device__ __forceinline__ void group_totals(const NormArgs& p, const Place<VEC>& at, Use&& use) {
-    with_lanes(p.nparts, [&](auto lanes) __attribute__((always_inline)) {
+    with_lanes(p.span * p.pixel_parts, [&](auto lanes) __attribute__((always_inline)) {
         constexpr int LANES = decltype(lanes)::value, AT_ONCE = kNormThreads / LANES, SUMS = BOTH ? 2 : 1;
         const int tid = thread_here();
         const int sub = tid % LANES;
@@ -462,18 +466,19 @@ __device__ __forceinline__ void group_totals(const NormArgs& p, const Place<VEC>
             double2 t[2] = {};
             if (g < at.g_hi) {
                 const double2* v = parts_of(p, at.s, 0, g);
-                const long second = (long)p.groups * p.nparts;
-                for (int i = sub; i < p.nparts; i += 4 * LANES) {
+                const long second = (long)p.groups * p.span * p.pixel_parts;
+                const int parts = parts_in(p, g);
+                for (int i = sub; i < parts; i += 4 * LANES) {
                     double2 q[4][SUMS];
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
 #pragma unroll
-                        for (int w = 0; w < SUMS; ++w) q[k][w] = v[min(i + k * LANES, p.nparts - 1) + w * second];
+                        for (int w = 0; w < SUMS; ++w) q[k][w] = v[min(i + k * LANES, parts - 1) + w * second];
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
 #pragma unroll
                         for (int w = 0; w < SUMS; ++w) {
-                            const bool in = i + k * LANES < p.nparts;
+                            const bool in = i + k * LANES < parts;
                             t[w].x += in ? q[k][w].x : 0.0; t[w].y += in ? q[k][w].y : 0.0;
                         }
                 }
@@ -560,14 +565,11 @@ __device__ __forceinline__ void norm_part(const NormArgs& p, long item, GroupCoe
     __syncthreads();
     if (!at.active) return;
     ChannelCoef ch[VEC];
-    double m = 0.0;
 #pragma unroll
     for (int c = 0; c < VEC; ++c) {
         const GroupCoef g = coef[(at.c0 + c) / p.per - at.g_lo];
         ch[c] = channel_coef(g, p.gamma, p.beta, at.c0 + c);
-        m = fmax(m, g.m);
     }
-    const UpFactors up(m);
     while (left > 0) {
         float e[4], claims[4], ref[4], y[4], t[4];
         const long here = out;
@@ -579,7 +581,7 @@ __device__ __forceinline__ void norm_part(const NormArgs& p, long item, GroupCoe
         left -= PIX * at.TY; x += PIX * step_x; out += PIX * step_y;
         if (left > 0) request();
 #pragma unroll
-        for (int c = 0; c < 4; ++c) norm_element<ACT>(e[c], ch[c % VEC], p.k.u, p.silu_k, up.mul, up.sub, y[c], t[c]);
+        for (int c = 0; c < 4; ++c) norm_element<ACT>(e[c], ch[c % VEC], p.k.u, p.silu_k, y[c], t[c]);
         const int vectors = now > (PIX - 1) * at.TY ? PIX : (now + at.TY - 1) / at.TY;
         sink.template put<VEC>(place, vectors, y, t, claims, ref);
     }
@@ -609,9 +611,9 @@ __global__ __launch_bounds__(kCheckThreads) void norm_act_check(NormCheckArgs) {
 
 // Parts of a sample: pixel parts, each for every column block, so that every compute unit has a workgroup; of eight trips of a workgroup over
 // its pixels at least.
-struct NormParts { int nparts, ncb; long pixels; };
+struct NormParts { int ncb, pixel_parts, span; long pixels; };
 static int channel_vec(long channels) { return channels % 4 == 0 ? 4 : channels % 2 == 0 ? 2 : 1; }
-static NormParts norm_parts(long batch, long positions, long channels) {
+static NormParts norm_parts(long batch, long positions, long channels, long groups) {
     const int ncb = (int)((channels + kColumns - 1) / kColumns);
     const long ty = kNormThreads / ((channels < kColumns ? channels : kColumns) / channel_vec(channels)), cus = 256;
     long want = cus / (batch * ncb);
@@ -620,7 +622,8 @@ static NormParts norm_parts(long batch, long positions, long channels) {
     NormParts r;
     r.ncb = ncb;
     r.pixels = (positions + want - 1) / want;
-    r.nparts = (int)((positions + r.pixels - 1) / r.pixels) * ncb;
+    r.pixel_parts = (int)((positions + r.pixels - 1) / r.pixels);
+    r.span = (int)std::min<long>(ncb, (channels / groups + kColumns - 2) / kColumns + 1);      // (a group's first channel is the last of a block at worst)
     return r;
 }
 // Whether one workgroup a group does: groups of at most two vectors a thread; no more than two workgroups a compute unit, as each walks through its sums and its outputs on
@@ -634,11 +637,13 @@ static bool norm_shape_ok(long batch, long positions, long channels, long groups
     if (batch < 0 || positions < 0 || channels < 0 || groups < 1 || channels % groups) return false;
     const long lim = 1L << 31;
     if (batch >= lim || positions >= lim || channels >= lim) return false;
+    if ((__int128)batch * groups >= (1L << 22) || (__int128)batch * ((channels + kColumns - 1) / kColumns) >= (1L << 22)) return false;      // workgroups of a launch
     return (__int128)(channels / groups) * positions < lim && (__int128)batch * positions * channels < ((__int128)1 << 36);
 }
 static size_t sums_bytes(long batch, long positions, long channels, long groups) {
     if (!norm_shape_ok(batch, positions, channels, groups) || batch * positions * channels == 0 || holds_row(batch, positions, channels, groups)) return 0;
-    return (size_t)batch * (size_t)norm_parts(batch, positions, channels).nparts * (size_t)groups * 2 * sizeof(double2);
+    const NormParts r = norm_parts(batch, positions, channels, groups);
+    return (size_t)batch * (size_t)groups * (size_t)r.span * (size_t)r.pixel_parts * 2 * sizeof(double2);
 }
 
 // Checks the arguments that the two entry points share and fills the kernels'.
@@ -649,7 +654,6 @@ static int norm_setup(int act, const float* x, const float* gamma, const float* 
     if (act != TAO_ACT_EXACT && act != TAO_ACT_RELU && act != TAO_ACT_SILU) return TAO_ERR_KIND;
     if (!norm_shape_ok(batch, positions, channels, groups) || ldx < channels || ldy < channels) return TAO_ERR_SHAPE;
     if ((__int128)batch * positions * ldx >= ((__int128)1 << 60) || (__int128)batch * positions * ldy >= ((__int128)1 << 60)) return TAO_ERR_SHAPE;
-    if ((__int128)batch * groups >= (1L << 22)) return TAO_ERR_SHAPE;      // workgroups of a launch
     if (!(eps >= 0.0) || !std::isfinite(eps)) return TAO_ERR_SHAPE;
     if (batch * positions * channels > 0 && !x) return TAO_ERR_NULL;
     if (!aligned(x, 4) || !aligned(gamma, 4) || !aligned(beta, 4)) return TAO_ERR_ALIGN;
@@ -664,8 +668,10 @@ static int norm_setup(int act, const float* x, const float* gamma, const float* 
     p.x = x; p.gamma = gamma; p.beta = beta;
     p.batch = batch; p.positions = positions; p.ldx = ldx; p.ldy = ldy;
     p.channels = (int)channels; p.groups = (int)groups; p.per = (int)per; p.n = (double)n;
-    const NormParts parts = n > 0 && batch > 0 ? norm_parts(batch, positions, channels) : NormParts{1, 1, 1};
-    p.nparts = parts.nparts; p.ncb = parts.ncb; p.pixels = parts.pixels;
+    if (n > 0 && batch > 0) {
+        const NormParts r = norm_parts(batch, positions, channels, groups);
+        p.ncb = r.ncb; p.pixel_parts = r.pixel_parts; p.span = r.span; p.pixels = r.pixels;
+    }
     return TAO_OK;
 }
 // LDS for what the last two passes keep of the groups that a column block can touch: one a channel, or all there are.
@@ -675,7 +681,7 @@ static size_t block_lds(const NormArgs& p, size_t each) {
 // The sums of all groups, left in p.part.
 template <int VEC>
 static void sums_launch(const NormArgs& p, hipStream_t st) {
-    const dim3 grid((unsigned)(p.batch * p.nparts)), blk(kNormThreads);
+    const dim3 grid((unsigned)(p.batch * p.pixel_parts * p.ncb)), blk(kNormThreads);
     hipLaunchKernelGGL((norm_sums<VEC, false>), grid, blk, 0, st, p);
     hipLaunchKernelGGL((norm_sums<VEC, true>), grid, blk, 0, st, p);
 }
@@ -703,7 +709,7 @@ static void norm_launch(const NormArgs& p, hipStream_t st) {
         return;
     }
     norm_sums_launch(p, st);
-    const dim3 grid((unsigned)(p.batch * p.nparts)), blk(kNormThreads);
+    const dim3 grid((unsigned)(p.batch * p.pixel_parts * p.ncb)), blk(kNormThreads);
     const size_t lds = block_lds(p, sizeof(GroupCoef));
     const int vec = channel_vec(p.channels);
     if (vec == 4)      hipLaunchKernelGGL((norm_apply<ACT, 4>), grid, blk, lds, st, p);
@@ -713,7 +719,7 @@ static void norm_launch(const NormArgs& p, hipStream_t st) {
 template <int ACT>
 static int norm_check_launch(NormArgs& p, const CheckWorkspace& w, long n, double alpha, double eps_rel, tao_profile* out, hipStream_t st) {
     const bool rows = n == 0 || holds_row(p.batch, p.positions, p.channels, p.groups);
-    const long items = n == 0 ? 0 : p.batch * (rows ? p.groups : p.nparts);
+    const long items = n == 0 ? 0 : p.batch * (rows ? p.groups : (long)p.pixel_parts * p.ncb);
     const int nblocks = (int)(items < 1 ? 1 : items < kMaxCheckBlocks ? items : kMaxCheckBlocks);
     if (n == 0) p.batch = 0;                                 // (no row is taken)
     const NormCheckArgs a = {p, items, alpha, eps_rel, pass_out(w, nblocks, n, out)};

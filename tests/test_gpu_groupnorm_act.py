@@ -173,3 +173,22 @@ def test_refusals_of_the_binding(tao):
     for bad in (lambda: tao.tao_bound_groupnorm_act(x, 3), lambda: tao.tao_bound_groupnorm_act(x, 2, act=tao.ACT_GELU_TANH), lambda: tao.tao_bound_groupnorm_act(x, 2, eps=-1.0)):
         with pytest.raises(tao.TaoError):
             bad()
+
+
+@pytest.mark.parametrize("act", [gn.NONE, gn.SILU])
+def test_a_group_next_to_one_that_almost_has_no_bound(tao, act):
+    """The smallest eps with which the first group's variance stays apart from its error: its bound grows by a step of eps a millionfold and may
+    take a margin for that; its neighbour, of which a thread has a channel too, keeps its own."""
+    x, gamma, beta = inputs(1, 500, 10, 8)
+    x[..., :5] = (30000 + x[..., :5] * 0.01).astype(np.float32)
+    lo, hi = 0, int(np.float32(1e6).view(np.int32))          # bit patterns of eps
+    bound = lambda bits: np.isfinite(gn.groupnorm_act(gn.NONE, x, 2, gamma, beta, float(np.int32(bits).view(np.float32)))[1][0, 0, 0])
+    assert bound(hi) and not bound(lo)
+    while hi - lo > 1:
+        mid = (lo + hi) // 2
+        lo, hi = (lo, mid) if bound(mid) else (mid, hi)
+    eps = float(np.int32(hi + 2).view(np.float32))
+    y, tau = tao.tao_bound_groupnorm_act(*cuda(x), 2, *cuda(gamma, beta), eps, act=kinds(tao)[act])
+    ye, te, E = gn.groupnorm_act(act, x, 2, gamma, beta, eps)
+    assert_outputs(y[..., 5:], tau[..., 5:], ye[..., 5:], te[..., 5:], E[..., 5:], act)
+    assert (tau[..., :5].cpu().numpy() >= te[..., :5] * (1 - np.longdouble(2) ** -58)).all()

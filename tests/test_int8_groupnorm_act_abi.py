@@ -74,6 +74,9 @@ def test_groupnorm_act_refusals(tao):
     assert call(groups=3) == call(groups=0) == call(batch=-1) == call(positions=-1) == call(channels=-4) == tao.ERR_SHAPE
     assert call(ldx=7) == call(ldy=7) == call(eps=-1.0) == call(eps=float("nan")) == call(ldx=2 ** 59) == tao.ERR_SHAPE
     assert call(positions=2 ** 31) == call(positions=2 ** 30) == call(batch=2 ** 29, positions=16) == tao.ERR_SHAPE
+    assert call(batch=2 ** 20, positions=1) == call(batch=2 ** 20, positions=1, channels=4096, groups=1, ldx=4096, ldy=4096) == tao.ERR_SHAPE
+    assert L.tao_groupnorm_act_workspace_bytes(2 ** 20, 1, 8, 4) == L.tao_groupnorm_act_workspace_bytes(2 ** 20, 1, 4096, 1) == 0
+    assert L.tao_groupnorm_act_workspace_bytes(1, 64, 2 ** 20, 2 ** 20) < 2 ** 30     # a group keeps parts of the blocks it lies in, not of all
     assert call(positions=2 ** 24) == tao.ERR_K_RANGE
     assert call(x=NUL) == call(y=NUL, tau=NUL) == tao.ERR_NULL
     assert call(x=ODD) == call(g=ODD) == call(b=ODD) == call(y=ODD) == call(tau=ODD) == tao.ERR_ALIGN

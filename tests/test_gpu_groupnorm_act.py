@@ -111,6 +111,37 @@ def test_slices_of_channels(tao, C, ld, at):
     assert_profile_equal(pf, oracle.check_and_profile(claimed.cpu().numpy(), y.cpu().numpy(), tau.cpu().numpy()))
 
 
+@pytest.mark.parametrize("P,C,groups,pad,at", [(900, 12, 2, 5, 3), (2500, 10, 2, 1, 1), (1200, 7, 1, 2, 0), (40, 36, 6, 4, 4)])
+def test_pixels_further_apart_than_they_are_long(tao, P, C, groups, pad, at):
+    """The same bits from padded pixels as from dense ones, and what lies between those of the results stays as it was."""
+    x, gamma, beta = inputs(2, P, C, 9)
+    xd, gd, bd = cuda(x, gamma, beta)
+    y, tau = tao.tao_bound_groupnorm_act(xd, groups, gd, bd)
+    ld = C + pad
+    room = torch.full((2, P, ld), 7.0, device="cuda")
+    room[..., at:at + C] = xd
+    outs = [torch.full((2 * P * ld,), 9.0, device="cuda") for _ in range(2)]
+    L, ws = tao.lib(), torch.empty(max(256, tao.tao_groupnorm_act_workspace_bytes(2, P, C, groups)), dtype=torch.uint8, device="cuda")
+    place = lambda t: t.data_ptr() + 4 * at
+    rc = L.tao_bound_groupnorm_act(tao.ACT_SILU, place(room), gd.data_ptr(), bd.data_ptr(), 1e-5, place(outs[0]), place(outs[1]), 2, P, C, groups, ld, ld, None,
+                                   ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+    assert rc == tao.OK
+    for out, dense in zip(outs, (y, tau)):
+        out = out.view(2, P, ld)
+        assert torch.equal(out[..., at:at + C], dense)
+        assert bool((out[..., :at] == 9).all()) and bool((out[..., at + C:] == 9).all())
+
+
+@pytest.mark.parametrize("P", [300, 700000])
+def test_offsets_beyond_32_bits(tao, P):
+    """Eight channels out of so many that the last pixel lies more than 2^31 elements on."""
+    ld = 2 ** 31 // P + 64
+    x = torch.empty((1, P, ld), device="cuda")[..., 40:48].normal_()
+    y, tau = tao.tao_bound_groupnorm_act(x, 2)
+    y2, tau2 = tao.tao_bound_groupnorm_act(x.contiguous(), 2)
+    assert torch.equal(y, y2) and torch.equal(tau, tau2)
+
+
 def test_channels_last_memory_format_is_taken_as_it_is(tao):
     x = torch.randn((2, 32, 7, 9), device="cuda").contiguous(memory_format=torch.channels_last)
     y, _ = tao.tao_bound_groupnorm_act(x.permute(0, 2, 3, 1), 8)

@@ -242,6 +242,21 @@ def test_quotients_in_the_middle_of_two_whole_numbers(tao, largest):
         assert np.array_equal(scale.cpu().numpy(), se) and np.array_equal(q.cpu().numpy(), qe)
 
 
+@pytest.mark.parametrize("M,N,K", [(70, 33, 96), (40, 40, 100)])
+def test_offsets_beyond_32_bits(tao, M, N, K):
+    """Rows of A and W so far apart that the last ones lie more than 2^31 elements on; the same for rows to be quantised and their values."""
+    A, sa, W, sw, _ = cuda(*operands(M, N, K, 3, False))
+    expect = tao.tao_bound_linear_int8(A, sa, W, sw)
+    far = lambda t: torch.empty((len(t), 2 ** 31 // len(t) + 2 ** 20), dtype=t.dtype, device="cuda")[:, 16:16 + t.shape[1]].copy_(t)
+    for a, w in ((far(A), W), (A, far(W)), (far(A), far(W))):
+        got = tao.tao_bound_linear_int8(a, sa, w, sw)
+        assert torch.equal(got[0], expect[0]) and torch.equal(got[1], expect[1])
+    x = torch.randn((M, K), device="cuda")
+    q, s = tao.tao_quantize_rows(x)
+    q2, s2 = tao.tao_quantize_rows(far(x), q=far(torch.zeros_like(q)))
+    assert torch.equal(q, q2) and torch.equal(s, s2)
+
+
 def test_refusals_of_the_binding(tao):
     A, sa, W, sw, b = cuda(*operands(8, 16, 32, 0, True))
     call = tao.tao_bound_linear_int8

@@ -187,7 +187,7 @@ struct NormStore {
 struct NormCheck {
     const float* y_ref; const float* claimed; double alpha, eps_rel; QuickCheck q; bool ordinary;
     unsigned int* hist; unsigned int* largest; int rep;
-    ThreadAcc acc; unsigned int zeros = 0;
+    ThreadAcc acc; unsigned int zeros = 0; Farthest top;
     __device__ __forceinline__ NormCheck(const NormCheckArgs& a, unsigned int* hist_, unsigned int* largest_)
         : y_ref(a.p.y_ref), claimed(a.p.claimed), alpha(a.alpha), eps_rel(a.eps_rel), q(a.p.k.quick_alpha, a.eps_rel), hist(hist_), largest(largest_), rep(threadIdx.x & (kReplicas - 1)) {
         ordinary = q.eps < INFINITY && q.alpha > 0.f;
@@ -200,8 +200,7 @@ struct NormCheck {
         for (int e = 0; e < 4; ++e) { r[e] = y_ref ? rv[e] : yv[e]; t[e] = tv[e]; k[e] = c[e]; }
         // (a NaN among the bounds, which are not negative, settles nothing; among the others it shows in the error)
         const float most = fmaxf(fmaxf(fabsf(r[0]), fabsf(r[1])), fmaxf(fabsf(r[2]), fabsf(r[3]))), bounds = (t[0] + t[1]) + (t[2] + t[3]);
-        const unsigned int known = newest(largest);
-        if (settle_four(k, r, t, q, known, ordinary && bounds <= 0x1p90f && most <= 0x1p90f && vectors >= kPixels<VEC>, acc, zeros,
+        if (settle_four<true>(k, r, t, q, top, largest, newest(largest), ordinary && bounds <= 0x1p90f && most <= 0x1p90f && vectors >= kPixels<VEC>, acc, zeros,
                         [&](unsigned bin) __attribute__((always_inline)) { atomicAdd(&hist[bin * kReplicas + rep], 1u); })) return;
         // (one at a time, in registers that move down: about one four in a thousand, and their divisions side by side take the registers of everything else)
         const int n = min(vectors * VEC, 4);
@@ -210,9 +209,11 @@ struct NormCheck {
             check_one(k[0], r[0], t[0], alpha, eps_rel, hist, rep, acc);
             k = k.yzww; r = r.yzww; t = t.yzww;
         }
-        if (acc.max_bits > known) atomicMax(largest, acc.max_bits);
     }
-    __device__ __forceinline__ void finish() { if (zeros) atomicAdd(&hist[rep], zeros); }
+    __device__ __forceinline__ void finish() {
+        if (zeros) atomicAdd(&hist[rep], zeros);
+        settled(top, alpha, eps_rel, acc);
+    }
 };
 // The check's LDS, in kernels of kCheckThreads threads.
 struct CheckShared { unsigned int hist[kBins * kReplicas], red[kRedWords], largest; };

@@ -146,13 +146,12 @@ struct Int8Bins {
         return c;
     }
 };
-// ROOM: the kernel has registers to spare (one workgroup a compute unit): two rows under way, and claims that are not settled are checked without a loop,
-// the first ones, whose errors no other one's tells the size of, side by side.
+// ROOM: the kernel has registers to spare (one workgroup a compute unit): two rows under way, and the element of the largest error kept.
 template <bool ROOM>
 struct Int8Check {
     const float* y_ref; const float* claimed; double alpha, eps_rel;
     unsigned int* hist; unsigned int* largest; QuickCheck q; bool ordinary;
-    ThreadAcc acc; unsigned int zeros = 0;
+    ThreadAcc acc; unsigned int zeros = 0; Farthest top;
     static constexpr int AHEAD = 4, UNROLL = ROOM ? 2 : 1;
     struct Ahead { floatv4 c; };
     __device__ __forceinline__ Int8Check(const float* y_ref_, const float* claimed_, double alpha_, double eps_rel_, float quick, unsigned int* hist_, unsigned int* largest_)
@@ -175,32 +174,20 @@ struct Int8Check {
             return;
         }
         if (y_ref) y = quad_load(y_ref, i, cols);
-        const unsigned int known = newest(largest);
+        const unsigned int published = newest(largest);
         bool ok = accurate && cols == 4 && ordinary;
         if (y_ref) ok = ok && fmaxf(fmaxf(fabsf(y[0]), fabsf(y[1])), fmaxf(fabsf(y[2]), fabsf(y[3]))) <= 0x1p100f;
-        if (settle_four(a.c, y, t, q, known, ok, acc, zeros, [&](unsigned bin) __attribute__((always_inline)) { Int8Bins::add(hist, bin); })) return;
-        if (ROOM && known == 0 && accurate && cols == 4) {
-            const float c4[4] = {a.c[0], a.c[1], a.c[2], a.c[3]}, y4[4] = {y[0], y[1], y[2], y[3]}, t4[4] = {t[0], t[1], t[2], t[3]};
-            check_four<1>(c4, y4, t4, alpha, eps_rel, hist, 0, acc);
-        } else {
-            auto one = [&](int e) __attribute__((always_inline)) {
-                check_one<1>(a.c[e], y[e], accurate ? t[e] : int8_bound(S[e], sa, sw[e], b[e], BIAS, p), alpha, eps_rel, hist, 0, acc);
-            };
-            if constexpr (ROOM) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (e < cols) one(e);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            } else {
+        if (settle_four<ROOM>(a.c, y, t, q, top, largest, published, ok, acc, zeros, [&](unsigned bin) __attribute__((always_inline)) { Int8Bins::add(hist, bin); })) return;
 #pragma unroll 1
-                for (int e = 0; e < cols; ++e) one(e);
-            }
-        }
-        if (acc.max_bits > known) atomicMax(largest, acc.max_bits);
+        for (int e = 0; e < cols; ++e)
+            check_one<1>(a.c[e], y[e], accurate ? t[e] : int8_bound(S[e], sa, sw[e], b[e], BIAS, p), alpha, eps_rel, hist, 0, acc);
+        if (!ROOM && acc.max_bits > published) atomicMax(largest, acc.max_bits);
     }
     // (before the histogram is read, with a barrier behind)
-    __device__ __forceinline__ void finish() { if (zeros) atomicAdd(&hist[0], zeros); }
+    __device__ __forceinline__ void finish() {
+        if (zeros) atomicAdd(&hist[0], zeros);
+        if (ROOM) settled(top, alpha, eps_rel, acc);
+    }
 };
 
 // ---- the product: a workgroup takes BM x BN outputs and walks the reduction in slabs of KB columns, of which STAGES lie in LDS: one is
@@ -500,7 +487,7 @@ __global__ __launch_bounds__(SH::THREADS, PAIR ? SH::THREADS * 2 / (4 * kWave) :
                                                                 float quick, CheckWorkspace w) {
     extern __shared__ __align__(16) char lds[];
     unsigned int* hist = reinterpret_cast<unsigned int*>(lds + SH::LDS + SH::SCALES);
-    unsigned int* rest = hist + Int8Bins::WORDS;       // largest error, three counters of every wavefront
+    unsigned int* rest = hist + Int8Bins::WORDS;       // largest estimate, three counters of every wavefront
     const int tid = threadIdx.x, wave = tid / kWave;
     for (int i = tid; i < Int8Bins::WORDS; i += SH::THREADS) hist[i] = 0;
     if (tid == 0) rest[0] = 0;

@@ -163,14 +163,23 @@ __device__ __forceinline__ bool quick_check_four(floatv4 c, floatv4 r, floatv4 a
     known = max(known, acc.max_bits);
     return false;
 }
+__device__ __forceinline__ unsigned newest(unsigned int* largest) {
+    return __hip_atomic_load(largest, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
 // Quick settlement of four claims at once, also of those that leave their bounds, for kernels that have their elements in fours; t: binary32 bounds,
-// ok: whether estimates may be taken at all (q.alpha and q.eps ordinary, |r| at most 2^100, t at most 2^90).  alpha t to within 2^-17 decides a comparison
+// published: newest(largest); ok: whether estimates may be taken at all (q.alpha and q.eps ordinary, |r| at most 2^100, t at most 2^90).  alpha t to within 2^-17 decides a comparison
 // that d misses by more than 2^-13 of it; the error's estimate, a bin that it is 16 steps inside of (of 0 and of the smallest ones, whose bin has
 // no lower edge, too).  What is no number, or too large, has an estimate beyond any error that occurs.  add(bin) counts an element.
-template <class Add>
-__device__ __forceinline__ bool settle_four(floatv4 c, floatv4 r, floatv4 t, const QuickCheck& q, unsigned known, bool ok, ThreadAcc& acc, unsigned int& zeros, Add&& add) {
+// The largest error is one element's: a thread that comes upon an estimate beyond its own largest and the workgroup's (*largest) keeps that element, whose exact error it
+// forms once, at its end (`settled`).  Estimates 32 steps apart are in the order of the errors; fours with an element closer to the largest one, or with two
+// that would replace it, are left to the exact check.  KEEP = false, for kernels without registers for that: what may exceed the largest error so far, then exact
+// and left in *largest by the caller, is left to the exact check.
+struct Farthest { unsigned int bits = 0; float c = 0.f, r = 0.f; };
+template <bool KEEP, class Add>
+__device__ __forceinline__ bool settle_four(floatv4 c, floatv4 r, floatv4 t, const QuickCheck& q, Farthest& top, unsigned int* largest, unsigned int published, bool ok, ThreadAcc& acc, unsigned int& zeros, Add&& add) {
     unsigned int bits[4], lowest = ~0u, highest = 0u, out = 0;
     float clear = INFINITY, furthest = 0.f;
+    const unsigned int known = KEEP ? max(published, top.bits) : published;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const float d = fabsf(c[e] - r[e]), at = t[e] * q.alpha;
@@ -181,8 +190,22 @@ __device__ __forceinline__ bool settle_four(floatv4 c, floatv4 r, floatv4 t, con
         clear = fminf(clear, fmaf(at, -0x1p-13f, fabsf(d - at)));
         out += d > at;
     }
-    // (four errors of 0 need no error that occurs)
-    if (!(ok && lowest >= 32u && (highest <= known || (highest == 80u && furthest == 0.f)) && clear > 0x1p-90f)) return false;
+    if (!KEEP) {
+        if (!(ok && lowest >= 32u && (highest <= known || (highest == 80u && furthest == 0.f)) && clear > 0x1p-90f)) return false;
+    } else if (!(ok && lowest >= 32u && highest <= 0x7f000000u && clear > 0x1p-90f)) return false;
+    if (KEEP && highest + 32u > known && !(highest == 80u && furthest == 0.f)) {
+        if (highest <= known + 32u) return false;
+        unsigned close = 0;
+        float hc = 0.f, hr = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            close += bits[e] + 32u >= highest;
+            if (bits[e] == highest) { hc = c[e]; hr = r[e]; }
+        }
+        if (close > 1) return false;
+        top.bits = highest; top.c = hc; top.r = hr;
+        if (published != 0 || (threadIdx.x & 15) == 0) atomicMax(largest, highest);      // (the first ones come all at once, and queue for the word)
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         if (bits[e] == 80u) ++zeros; else add(bits[e] >> 20);
@@ -190,8 +213,8 @@ __device__ __forceinline__ bool settle_four(floatv4 c, floatv4 r, floatv4 t, con
     acc.violations += out;
     return true;
 }
-__device__ __forceinline__ unsigned newest(unsigned int* largest) {
-    return __hip_atomic_load(largest, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+__device__ __forceinline__ void settled(const Farthest& top, double alpha, double eps_rel, ThreadAcc& acc) {
+    if (top.bits) acc.max_bits = max(acc.max_bits, check_arith(top.c, top.r, 0.f, alpha, eps_rel).bits);
 }
 
 // Workgroup totals of the per-thread counters (kCheckThreads threads) into ws_stats[blockIdx.x];

@@ -180,6 +180,26 @@ def test_check_is_the_streaming_check_of_the_stored_bound(tao, B, P, C, groups, 
         assert_profile_equal(pf, oracle.check_and_profile(claimed.cpu().numpy(), other.cpu().numpy(), tau.cpu().numpy(), alpha, eps_rel))
 
 
+def sets_of_errors(y):
+    """Claims whose largest error is one of many almost as large, the last of a rising row, the first of a falling one, or the only one."""
+    n = y.numel()
+    ramp = torch.arange(1, n + 1, device="cuda", dtype=torch.float64).view(y.shape) / n
+    one = y.clone()
+    one.view(-1)[n // 3] *= 1.5
+    d = y.double()
+    return [(d * (1 + 1e-3)).float(), (d * (1 + 1e-3 * ramp)).float(), (d * (1 + 1e-3 * (1 + 1 / n - ramp))).float(), one, torch.nextafter(y, torch.zeros_like(y)), 0 * y]
+
+
+@pytest.mark.parametrize("B,P,C,groups", [(2, 64, 320, 32), (1, 3000, 64, 8), (1, 1500, 35, 5)])
+def test_the_largest_error_among_many(tao, B, P, C, groups):
+    x, gamma, beta = inputs(B, P, C, 4)
+    a = cuda(x), groups, cuda(gamma, beta)
+    y, tau = tao.tao_bound_groupnorm_act(*a[0], groups, *a[2])
+    for claimed in sets_of_errors(y):
+        pf = tao.tao_bound_check_groupnorm_act(*a[0], claimed, groups, *a[2], eps_rel=1e-9)
+        assert_profile_equal(pf, oracle.check_and_profile(claimed.cpu().numpy(), y.cpu().numpy(), tau.cpu().numpy(), 1.0, 1e-9))
+
+
 def test_nothing_to_do(tao):
     for shape in ((0, 4, 4, 8), (2, 0, 4, 8)):
         x = torch.empty(shape, device="cuda")

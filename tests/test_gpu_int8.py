@@ -186,6 +186,20 @@ def test_check_is_the_streaming_check_of_the_stored_bound(tao, M, N, K, ref):
     assert honest["accept"] == 1 and honest["max_rel"] == 0.0 and honest["n"] == M * N
 
 
+@pytest.mark.parametrize("M,N,K", [(20, 300, 200), (150, 300, 640), (1500, 1000, 128), (2100, 2100, 64)])
+def test_the_largest_error_among_many(tao, M, N, K):
+    """Claims whose largest error is one of many almost as large, the last of a rising row, the first of a falling one, or the only one."""
+    a = cuda(*operands(M, N, K, 5, True))
+    y, tau = tao.tao_bound_linear_int8(*a)
+    d, n = y.double(), y.numel()
+    ramp = torch.arange(1, n + 1, device="cuda", dtype=torch.float64).view(y.shape) / n
+    one = y.clone()
+    one.view(-1)[n // 3] *= 1.5
+    for claimed in ((d * (1 + 1e-3)).float(), (d * (1 + 1e-3 * ramp)).float(), (d * (1 + 1e-3 * (1 + 1 / n - ramp))).float(), one, torch.nextafter(y, torch.zeros_like(y)), 0 * y):
+        pf = tao.tao_bound_check_linear_int8(*a[:4], claimed, a[4], eps_rel=1e-9)
+        assert_profile_equal(pf, oracle.check_and_profile(claimed.cpu().numpy(), y.cpu().numpy(), tau.cpu().numpy(), 1.0, 1e-9))
+
+
 def test_checks_of_nothing(tao):
     for M, N in ((0, 5), (5, 0)):
         A, sa, W, sw, _ = operands(M, N, 16)

@@ -10,7 +10,7 @@
 // per channel, whatever the number of channels per group, and reach their groups in LDS.  Three passes over x, as the mean has to
 // be known before the deviations, and sum |d| with it: (a) sum x, sum |x|, (b) sum |d|, sum d^2, (c) the outputs; every workgroup of (b) and (c) adds up
 // the parts of its groups in the same order.  4 x 16384 x 512 SiLU: 24 + 24 + 70 us (134 MB read at 5.5 TB/s twice, 402 MB moved at 5.7 TB/s); the check in place
-// of (c) 88 us, next to its instructions (about 80 an element, 40 of them binary64, four cycles each).
+// of (c) 85 us, next to its instructions (about 72 an element, 35 of them binary64, four cycles each).
 #include <algorithm>
 #include <type_traits>
 #include "tao_check.hpp"
@@ -31,7 +31,9 @@ struct NormArgs {
     int span;                        // column blocks that a group lies in, at most
     long pixels;                     // of a part
     RowConsts k;
-    double silu_k;                   // silu_f / (1 - silu_f)
+    // of norm_element, with the final upper rounding's factor in them, and SiLU's 1 + silu_f / (1 - silu_f) in the first two
+    double grow_ep, grow_p;          // of E: (1 + u) E_p, u |p|
+    double quarter, silu_k;          // of SiLU: of E^2 without the factors, silu_f / (1 - silu_f)
     double n;
 };
 // ... of a check: items are rows, or parts of all samples
@@ -97,16 +99,16 @@ __device__ __forceinline__ GroupCoef group_coef(const RowConsts& k, double n, do
     c.K1 *= 1.0 + 2.0 * m; c.K0 *= 1.0 + 2.0 * m;
     return c;
 }
-// ... and of its channel: p = d rg + b, E_p = k1 |d| + k0
+// ... and of its channel: p = d rg + b, grow_ep E_p = k1 |d| + k0
 struct ChannelCoef { double mu, rg, b, k1, k0; };
-__device__ __forceinline__ ChannelCoef channel_coef(const GroupCoef& g, const float* gamma, const float* beta, int channel) {
-    const double w = gamma ? (double)gamma[channel] : 1.0;
-    return ChannelCoef{g.mu, g.r * w, beta ? (double)beta[channel] : 0.0, fabs(w) * g.K1, fabs(w) * g.K0};
+__device__ __forceinline__ ChannelCoef channel_coef(const NormArgs& p, const GroupCoef& g, int channel) {
+    const double w = p.gamma ? (double)p.gamma[channel] : 1.0, grown = fabs(w) * p.grow_ep;
+    return ChannelCoef{g.mu, g.r * w, p.beta ? (double)p.beta[channel] : 0.0, grown * g.K1, grown * g.K0};
 }
 
 // 1 / (1 + exp(-p)) and 1 minus it, to 2^-39, for |p| <= 700 (beyond, those of 700 with p's sign: where |p| 2^-1009 stands for |p| exp(-|p|)).
 // exp(r) on |r| <= ln2 / 2 as a polynomial of degree 8 whose relative error, 2^-40.2, is the least possible (found by exchange of its extrema);
-// the quotient from v_rcp_f64 (2^-23) and one Newton step.  27 instructions of binary64, where exp_neg and a division take twice that:
+// the quotient from v_rcp_f64 (2^-23) and one Newton step.  22 instructions of binary64, where exp_neg and a division take twice that:
 // the outputs of 512 x 512 x 128 in 74 us instead of 129.
 __device__ __forceinline__ double sigmoid(double p, double& rest) {
     const double s = fmin(fmax(p, -700.0), 700.0);
@@ -130,29 +132,34 @@ __device__ __forceinline__ double sigmoid(double p, double& rest) {
     return q;
 }
 
-// Output and bound of one element.  The slacks keep an evaluation in round-to-nearest binary64 at or above the formula's value: near
-// a zero of s' its relative error is large, but 2^-36 (the sigmoid's error many times over) of E is far below 1e-6 of the other terms.
+// Output and bound of one element.  E comes with the factor of the final upper rounding (kUp: 2^-24 for it, 2^-32 for the few roundings before it) and, for
+// SiLU, with that of its own roundings, so both cost nothing here.  The slacks keep an evaluation in round-to-nearest binary64 at or above the formula's
+// value: near a zero of s' its relative error is large, but 2^-36 (the sigmoid's error many times over) of E is far below 1e-6 of the other terms.
+constexpr double kUp = 1.0 + 0x1p-24 + 0x1p-32;
+__device__ __forceinline__ float rounded_up(double v) {      // (v holds kUp)
+    float f = (float)v;
+    if (f < 0x1p-126f && (double)f < v) f = __uint_as_float(__float_as_uint(f) + 1u);
+    return f;
+}
 template <int ACT>
-__device__ __forceinline__ void norm_element(float x, const ChannelCoef& c, double u, double silu_k, float& y, float& tau) {
-    constexpr double mul = 1.0 + 0x1p-24 + 0x1p-32, sub = 1.0 + 0x1p-48;      // (of the final upper rounding: the few roundings of an element)
+__device__ __forceinline__ void norm_element(float x, const ChannelCoef& c, const NormArgs& a, float& y, float& tau) {
     const double d = (double)x - c.mu;
     const double p = fma(d, c.rg, c.b);
-    const double ep = fma(c.k1, fabs(d), c.k0);
-    const double E = fma(u, fabs(p) + ep, ep);
+    const double E = fma(a.grow_p, fabs(p), fma(c.k1, fabs(d), c.k0));
     if constexpr (ACT == TAO_ACT_SILU) {
         double rest;
         const double sig = sigmoid(p, rest), s = p * sig;
-        const double slope = fabs(sig * fma(p, rest, 1.0)) + 0x1p-36;
-        const double B = E * fmin(fma(0.25 + 0x1p-23, E, slope), 1.1);
+        const double slope = fabs(fma(s, rest, sig)) + 0x1p-36;
+        const double B = E * fmin(fma(a.quarter, E, slope), 1.1);
         y = (float)s;
-        tau = up32g(fma(silu_k, fabs(s) + B, B), mul, sub);  // (a minimum leaves a NaN out, but E times 1.1 is one)
+        tau = rounded_up(fma(a.silu_k, fabs(s), B));         // (a minimum leaves a NaN out, but E times 1.1 is one)
     } else if constexpr (ACT == TAO_ACT_RELU) {
         y = p <= 0.0 ? 0.f : (float)p;
         const double t = fmin(E, fma(E, 1.0 + 0x1p-24, p));
-        tau = E == E ? (t > 0.0 ? up32g(t, mul, sub) : 0.f) : (float)E;
+        tau = E == E ? (t > 0.0 ? rounded_up(t) : 0.f) : (float)E;
     } else {
         y = (float)p;
-        tau = up32g(E, mul, sub);
+        tau = rounded_up(E);
     }
 }
 
@@ -335,7 +342,7 @@ __device__ __forceinline__ void norm_row(const NormArgs& p, long row, double* sm
 #pragma unroll 1
         for (int e = 0; e < 4; ++e) {
             float y1, t1;
-            norm_element<ACT>(xv[0], channel_coef(coef, p.gamma, p.beta, (int)of[0]), p.k.u, p.silu_k, y1, t1);
+            norm_element<ACT>(xv[0], channel_coef(p, coef, (int)of[0]), p, y1, t1);
 #pragma unroll
             for (int i = 0; i < 3; ++i) { xv[i] = xv[i + 1]; of[i] = of[i + 1]; y[i] = y[i + 1]; t[i] = t[i + 1]; }
             y[3] = y1; t[3] = t1;
@@ -569,7 +576,7 @@ __device__ __forceinline__ void norm_part(const NormArgs& p, long item, GroupCoe
 #pragma unroll
     for (int c = 0; c < VEC; ++c) {
         const GroupCoef g = coef[(at.c0 + c) / p.per - at.g_lo];
-        ch[c] = channel_coef(g, p.gamma, p.beta, at.c0 + c);
+        ch[c] = channel_coef(p, g, at.c0 + c);
     }
     while (left > 0) {
         float e[4], claims[4], ref[4], y[4], t[4];
@@ -582,7 +589,7 @@ __device__ __forceinline__ void norm_part(const NormArgs& p, long item, GroupCoe
         left -= PIX * at.TY; x += PIX * step_x; out += PIX * step_y;
         if (left > 0) request();
 #pragma unroll
-        for (int c = 0; c < 4; ++c) norm_element<ACT>(e[c], ch[c % VEC], p.k.u, p.silu_k, y[c], t[c]);
+        for (int c = 0; c < 4; ++c) norm_element<ACT>(e[c], ch[c % VEC], p, y[c], t[c]);
         const int vectors = now > (PIX - 1) * at.TY ? PIX : (now + at.TY - 1) / at.TY;
         sink.template put<VEC>(place, vectors, y, t, claims, ref);
     }
@@ -665,7 +672,9 @@ static int norm_setup(int act, const float* x, const float* gamma, const float* 
     if (rc != TAO_OK) return rc;
     const double f = silu_factor(*md);
     if (!(f < 0.5)) return TAO_ERR_MODEL;
-    p.silu_k = widen(f / (1.0 - f));
+    const double k = widen(f / (1.0 - f)), own = act == TAO_ACT_SILU ? 1.0 + k : 1.0;
+    p.grow_ep = (1.0 + md->u) * own * kUp; p.grow_p = md->u * own * kUp;
+    p.quarter = (0.25 + 0x1p-23) / own; p.silu_k = k * kUp;
     p.x = x; p.gamma = gamma; p.beta = beta;
     p.batch = batch; p.positions = positions; p.ldx = ldx; p.ldy = ldy;
     p.channels = (int)channels; p.groups = (int)groups; p.per = (int)per; p.n = (double)n;

@@ -277,8 +277,9 @@ int tao_bound_check_linear_int8(const int8_t *A, const float *scale_a, const int
                                 long batch, long strideA, long strideW, long strideY, double alpha, double eps_rel,
                                 const tao_fp_model *model, tao_profile *out, void *ws, size_t ws_bytes, void *stream);
 /* The 8-bit operand of the product from binary32 activations: per row, with m = max |x|,
- *     scale[r] = fl(m / 127),   q[r][c] = round(fl(x[r][c] / scale[r])) to the nearest whole number, ties to even, in [-127, 127].
- * A row whose scale comes out as 0 (zeros; values below 127 2^-150) has q = 0; a row that is not finite has scale NaN and
+ *     scale[r] = fl(m fl(1/127)),   q[r][c] = round(fl(x[r][c] / scale[r])) to the nearest whole number, ties to even, in [-127, 127].
+ * (the product is how tensor programs on a device divide by a constant, so what they quantise is the same bit for bit).
+ * A row whose scale comes out as 0 (zeros; values below about 127 2^-150) has q = 0; a row that is not finite has scale NaN and
  * q = 0, so that its products are NaN, which no check admits.  Every step is one correctly rounded operation: the result is the same bit for
  * bit in any implementation.  x: [rows][cols], row stride ld; q: row stride ldq; scale: [rows]. */
 int tao_quantize_rows(const float *x, int8_t *q, float *scale, long rows, long cols, long ld, long ldq, void *stream);

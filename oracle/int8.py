@@ -22,7 +22,7 @@ def quantize_rows(x):
     x = np.asarray(x, dtype=np.float32)
     m = np.abs(x).max(axis=1, initial=0) if x.shape[1] else np.zeros(x.shape[0], np.float32)
     finite = np.isfinite(x).all(axis=1)
-    scale = np.where(finite, np.where(finite, m, 0).astype(np.float32) / np.float32(127), np.float32(np.nan)).astype(np.float32)
+    scale = np.where(finite, np.where(finite, m, 0).astype(np.float32) * (np.float32(1) / np.float32(127)), np.float32(np.nan)).astype(np.float32)
     some = scale > 0                                         # (NaN compares false)
     with np.errstate(invalid="ignore", over="ignore"):
         q = np.clip(np.rint(np.where(some[:, None], x, 0) / np.where(some, scale, 1)[:, None].astype(np.float32)), -127, 127)

@@ -940,7 +940,8 @@ def _reexecuted(y, tau, with_y, with_tau, shape, like, here):
 
 
 def tao_quantize_rows(x, q=None, scale=None):
-    """(q, scale): each row of x[..., cols] as int8 values q[..., cols] times a binary32 scale[...] = max|row| / 127."""
+    """(q, scale): each row of x[..., cols] as int8 values q[..., cols] times a binary32 scale[...] = max|row| / 127 (as a product
+    with the binary32 value of 1/127, which is what max|row| / 127 gives in a tensor program on the device)."""
     torch = _torch_module or _torch()
     here = _current_device()
     shape = _on(x, _float32, here, "x")

@@ -538,7 +538,7 @@ typedef Int8Shape<256, 256, 128, 64, 128, 2> Int8Wide;                       // 
 static_assert(tile_lds<Int8Tiny>(true) <= 160 * 1024 && tile_lds<Int8Flat>(true) <= 160 * 1024 &&
               tile_lds<Int8Wide>(true) <= 160 * 1024 && tile_lds<Int8Small>(true) <= 80 * 1024 && tile_lds<Int8Mid>(true) <= 80 * 1024, "a compute unit's LDS");
 
-// ---- quantisation of rows: scale = fl(max|x| / 127), q = round(fl(x / scale)), ties to even.  A row that is not finite has scale NaN
+// ---- quantisation of rows: scale = fl(max|x| fl(1/127)), q = round(fl(x / scale)), ties to even.  A row that is not finite has scale NaN
 // and q = 0 (so the product is NaN, which no check admits); a row of zeros, or one so small that its scale rounds to 0, scale 0 and q = 0.
 // A team of lanes holds its row in registers, so x is read once: 16 lanes or a wavefront for the short rows (several to a workgroup, no barrier), a
 // workgroup for the long ones, which reads what goes beyond its registers again.  A row is taken in fours at any alignment, the last of
@@ -610,7 +610,7 @@ __global__ __launch_bounds__(THREADS) void quantize_rows(QuantizeArgs p) {
             for (int w = 1; w < WAVES; ++w) m = max(m, most[w]);
             __syncthreads();                                 // (the next row's)
         }
-        const float s = m < 0x7f800000u ? __uint_as_float(m) / 127.f : NAN, inverse = __builtin_amdgcn_rcpf(s);
+        const float s = m < 0x7f800000u ? __uint_as_float(m) * (1.f / 127.f) : NAN, inverse = __builtin_amdgcn_rcpf(s);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             const long i = k * LANES + lane;
@@ -627,7 +627,7 @@ __global__ __launch_bounds__(256) void quantize_short_rows(QuantizeArgs p) {
     for (long r = (long)blockIdx.x * 256 + threadIdx.x; r < p.rows; r += (long)gridDim.x * 256) {
         unsigned m = 0;
         for (long c = 0; c < p.cols; ++c) m = max(m, __float_as_uint(p.x[r * p.ld + c]) & 0x7fffffffu);
-        const float s = m < 0x7f800000u ? __uint_as_float(m) / 127.f : NAN;
+        const float s = m < 0x7f800000u ? __uint_as_float(m) * (1.f / 127.f) : NAN;
         for (long c = 0; c < p.cols; ++c) p.q[r * p.ldq + c] = (signed char)quantized(p.x[r * p.ld + c], s);
         p.scale[r] = s;
     }

@@ -235,11 +235,20 @@ def test_quantised_rows_of_every_alignment(tao):
         assert bool((store[atq:].view(rows, ldq)[:, cols:] == 99).all()) and bool((store[:atq] == 99).all())
 
 
+@pytest.mark.parametrize("rows,cols", [(8, 4096), (3000, 777), (40, 20000)])
+def test_quantised_rows_are_those_of_a_tensor_program(tao, rows, cols):
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    x = torch.randn((rows, cols), generator=g, device="cuda") * torch.exp(torch.randn((rows, 1), generator=g, device="cuda"))
+    scale = x.abs().amax(dim=1) / 127
+    q, s = tao.tao_quantize_rows(x)
+    assert torch.equal(s, scale) and torch.equal(q, torch.round(x / scale[:, None]).to(torch.int8))
+
+
 @pytest.mark.parametrize("largest", [127.0, 1.0, 3.7e-5, 2.9e30, 1e-38, 2.0 ** -93, 2.0 ** -94])
 def test_quotients_in_the_middle_of_two_whole_numbers(tao, largest):
     """The rounded quotient decides, at ties to even: arguments at and next to every middle, also where the scale is next to having no reciprocal."""
     m = np.float32(largest)
-    s = m / np.float32(127)
+    s = m * (np.float32(1) / np.float32(127))
     k = (np.arange(-127, 127) + 0.5).astype(np.float32)
     x = [m]
     for step in range(-3, 4):

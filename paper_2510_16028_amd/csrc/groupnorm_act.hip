@@ -191,6 +191,8 @@ struct NormStore {
         }
     }
 };
+// REF: against the verifier's own outputs.  (No branch around their loads, behind which they would be waited for.)
+template <bool REF>
 struct NormCheck {
     const float* y_ref; const float* claimed; double alpha, eps_rel; QuickCheck q; bool ordinary;
     unsigned int* hist; unsigned int* largest; int rep;
@@ -200,11 +202,11 @@ struct NormCheck {
         ordinary = q.eps < INFINITY && q.alpha > 0.f;
     }
     template <int VEC, class At> __device__ __forceinline__ void request(At&& at, float (&c)[4]) const { load_quad<VEC, true>(claimed, at, c); }
-    template <int VEC, class At> __device__ __forceinline__ void reference(At&& at, float (&r)[4]) const { if (y_ref) load_quad<VEC, true>(y_ref, at, r); }
+    template <int VEC, class At> __device__ __forceinline__ void reference(At&& at, float (&r)[4]) const { if constexpr (REF) load_quad<VEC, true>(y_ref, at, r); }
     template <int VEC, class At> __device__ __forceinline__ void put(At&&, int vectors, const float (&yv)[4], const float (&tv)[4], const float (&c)[4], const float (&rv)[4]) {
         floatv4 r, t, k;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { r[e] = y_ref ? rv[e] : yv[e]; t[e] = tv[e]; k[e] = c[e]; }
+        for (int e = 0; e < 4; ++e) { r[e] = REF ? rv[e] : yv[e]; t[e] = tv[e]; k[e] = c[e]; }
         // (a NaN among the bounds, which are not negative, settles nothing; among the others it shows in the error)
         const float most = fmaxf(fmaxf(fabsf(r[0]), fabsf(r[1])), fmaxf(fabsf(r[2]), fabsf(r[3]))), bounds = (t[0] + t[1]) + (t[2] + t[3]);
         if (settle_four<true>(k, r, t, q, top, largest, newest(largest), ordinary && bounds <= 0x1p90f && most <= 0x1p90f && vectors >= kPixels<VEC>, acc, zeros,
@@ -367,13 +369,13 @@ __global__ __launch_bounds__(THREADS) void norm_rows(NormArgs p) {
     const RowOrder o(p.batch * p.groups);
     if (o.at < o.n) norm_row<ACT, VEC, V, THREADS>(p, o.base + o.at, smem, sink);
 }
-template <int ACT, int VEC>
+template <int ACT, int VEC, bool REF>
 __global__ __launch_bounds__(kCheckThreads) void norm_rows_check(NormCheckArgs) {
     __shared__ CheckShared chk;
     __shared__ double smem[4 * (kCheckThreads / kWave)];
     clear_check(chk);
     const NormCheckArgs& a = args_here<NormCheckArgs>();
-    NormCheck sink(a, chk.hist, &chk.largest);
+    NormCheck<REF> sink(a, chk.hist, &chk.largest);
     const RowOrder o(a.items);
     for (long i = o.at; i < o.n; i += o.step) {
         norm_row<ACT, VEC, kRowVectors, kCheckThreads>(args_here<NormCheckArgs>().p, o.base + i, smem, sink);
@@ -601,13 +603,13 @@ __global__ __launch_bounds__(kNormThreads) void norm_apply(NormArgs p) {
     norm_part<ACT, VEC>(p, blockIdx.x, coef, sink);
 }
 // checked on the spot: workgroups of the streaming check, which take the parts in turn
-template <int ACT, int VEC>
+template <int ACT, int VEC, bool REF>
 __global__ __launch_bounds__(kCheckThreads) void norm_act_check(NormCheckArgs) {
     __shared__ CheckShared chk;
     extern __shared__ GroupCoef coef[];
     clear_check(chk);
     const NormCheckArgs& a = args_here<NormCheckArgs>();
-    NormCheck sink(a, chk.hist, &chk.largest);
+    NormCheck<REF> sink(a, chk.hist, &chk.largest);
     for (long it = blockIdx.x; it < a.items; it += gridDim.x) {
         norm_part<ACT, VEC>(args_here<NormCheckArgs>().p, it, coef, sink);
         __syncthreads();                                     // (the coefficients are replaced)
@@ -726,7 +728,7 @@ static void norm_launch(const NormArgs& p, hipStream_t st) {
     else if (vec == 2) hipLaunchKernelGGL((norm_apply<ACT, 2>), grid, blk, lds, st, p);
     else               hipLaunchKernelGGL((norm_apply<ACT, 1>), grid, blk, lds, st, p);
 }
-template <int ACT>
+template <int ACT, bool REF>
 static int norm_check_launch(NormArgs& p, const CheckWorkspace& w, long n, double alpha, double eps_rel, tao_profile* out, hipStream_t st) {
     const bool rows = n == 0 || holds_row(p.batch, p.positions, p.channels, p.groups);
     const long items = n == 0 ? 0 : p.batch * (rows ? p.groups : (long)p.pixel_parts * p.ncb);
@@ -736,15 +738,15 @@ static int norm_check_launch(NormArgs& p, const CheckWorkspace& w, long n, doubl
     const dim3 grid((unsigned)nblocks), blk(kCheckThreads);
     if (rows) {
         const int vec = channel_vec(p.per);
-        if (vec == 4)      hipLaunchKernelGGL((norm_rows_check<ACT, 4>), grid, blk, 0, st, a);
-        else if (vec == 2) hipLaunchKernelGGL((norm_rows_check<ACT, 2>), grid, blk, 0, st, a);
-        else               hipLaunchKernelGGL((norm_rows_check<ACT, 1>), grid, blk, 0, st, a);
+        if (vec == 4)      hipLaunchKernelGGL((norm_rows_check<ACT, 4, REF>), grid, blk, 0, st, a);
+        else if (vec == 2) hipLaunchKernelGGL((norm_rows_check<ACT, 2, REF>), grid, blk, 0, st, a);
+        else               hipLaunchKernelGGL((norm_rows_check<ACT, 1, REF>), grid, blk, 0, st, a);
     } else {
         norm_sums_launch(p, st);
         const size_t lds = block_lds(p, sizeof(GroupCoef));
         // (two channels a thread: the coefficients of four leave no registers for the check)
-        if (p.channels % 2 == 0) hipLaunchKernelGGL((norm_act_check<ACT, 2>), grid, blk, lds, st, a);
-        else                     hipLaunchKernelGGL((norm_act_check<ACT, 1>), grid, blk, lds, st, a);
+        if (p.channels % 2 == 0) hipLaunchKernelGGL((norm_act_check<ACT, 2, REF>), grid, blk, lds, st, a);
+        else                     hipLaunchKernelGGL((norm_act_check<ACT, 1, REF>), grid, blk, lds, st, a);
     }
     return nblocks;
 }
@@ -802,10 +804,11 @@ int tao_bound_check_groupnorm_act(int act, const float* x, const float* gamma, c
     p.k.quick_alpha = quick_alpha(alpha, md);
     hipStream_t st = (hipStream_t)stream;
     const CheckWorkspace w = carve_check_workspace(ws);
-    int nblocks;
-    if (act == TAO_ACT_SILU)      nblocks = norm_check_launch<TAO_ACT_SILU>(p, w, n, alpha, eps_rel, out, st);
-    else if (act == TAO_ACT_RELU) nblocks = norm_check_launch<TAO_ACT_RELU>(p, w, n, alpha, eps_rel, out, st);
-    else                          nblocks = norm_check_launch<TAO_ACT_EXACT>(p, w, n, alpha, eps_rel, out, st);
+    const auto launch = [&](auto kind) { return y_ref ? norm_check_launch<decltype(kind)::value, true>(p, w, n, alpha, eps_rel, out, st)
+                                                      : norm_check_launch<decltype(kind)::value, false>(p, w, n, alpha, eps_rel, out, st); };
+    const int nblocks = act == TAO_ACT_SILU   ? launch(std::integral_constant<int, TAO_ACT_SILU>())
+                        : act == TAO_ACT_RELU ? launch(std::integral_constant<int, TAO_ACT_RELU>())
+                                              : launch(std::integral_constant<int, TAO_ACT_EXACT>());
     launch_finish(w, nblocks, n, out, st);
     return launch_status();
 }

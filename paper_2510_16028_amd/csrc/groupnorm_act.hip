@@ -10,7 +10,7 @@
 // per channel, whatever the number of channels per group, and reach their groups in LDS.  Three passes over x, as the mean has to
 // be known before the deviations, and sum |d| with it: (a) sum x, sum |x|, (b) sum |d|, sum d^2, (c) the outputs; every workgroup of (b) and (c) adds up
 // the parts of its groups in the same order.  4 x 16384 x 512 SiLU: 24 + 24 + 70 us (134 MB read at 5.5 TB/s twice, 402 MB moved at 5.7 TB/s); the check in place
-// of (c) 85 us, next to its instructions (about 72 an element, 35 of them binary64, four cycles each).
+// of (c) 80 us, next to its instructions (about 72 an element, 35 of them binary64, four cycles each).
 #include <algorithm>
 #include <type_traits>
 #include "tao_check.hpp"

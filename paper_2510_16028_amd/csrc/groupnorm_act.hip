@@ -637,11 +637,12 @@ static NormParts norm_parts(long batch, long positions, long channels, long grou
     return r;
 }
 // Whether one workgroup a group does: groups of at most two vectors a thread; no more than two workgroups a compute unit, as each walks through its sums and its outputs on
-// its own; and little work in all.  GPU us, norm_rows / the three passes, bound and check: 2 x 64 x 1280 in 32 groups 7.5 / 18 and 17 / 29, 2 x 256 x 1024 11 / 18 and 21 / 29,
-// 16 x 64 x 1024 8.8 / 19 and 23 / 29; beyond, 2 x 256 x 2048 20 / 20 and 39 / 30, 16 x 256 x 1024 23 / 31 and 37 / 40, 64 x 16 x 256 in 64 16 / 16 and 87 / 25.
+// its own; and little work in all, or pixels of 64 bytes a group at least (lines that are not shared out).  GPU us, norm_rows / the three passes, bound and check: 2 x 64 x 1280 in
+// 32 groups 7.4 / 19 and 13 / 26, 2 x 256 x 1024 11.5 / 19 and 18 / 26, 16 x 256 x 256 9.7 / 19 and 20 / 26, 16 x 256 x 1024 20 / 31 and 30 / 36; beyond,
+// 2 x 256 x 2048 20 / 20 and 39 / 30, 16 x 1024 x 128 38 / 21 and 32 / 31, 64 x 16 x 256 in 64 14 / 16 and 78 / 22.
 static bool holds_row(long batch, long positions, long channels, long groups) {
     const long per = channels / groups, vectors = per / channel_vec(per) * positions, rows = batch * groups;
-    return vectors <= kRowVectors * kNormThreads && rows <= 512 && rows * vectors <= 1 << 18;
+    return vectors <= kRowVectors * kNormThreads && rows <= 512 && (rows * vectors <= 1 << 18 || per >= 16);
 }
 static bool norm_shape_ok(long batch, long positions, long channels, long groups) {
     if (batch < 0 || positions < 0 || channels < 0 || groups < 1 || channels % groups) return false;

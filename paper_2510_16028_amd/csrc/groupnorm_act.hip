@@ -207,9 +207,9 @@ struct NormCheck {
         floatv4 r, t, k;
 #pragma unroll
         for (int e = 0; e < 4; ++e) { r[e] = REF ? rv[e] : yv[e]; t[e] = tv[e]; k[e] = c[e]; }
-        // (a NaN among the bounds, which are not negative, settles nothing; among the others it shows in the error)
-        const float most = fmaxf(fmaxf(fabsf(r[0]), fabsf(r[1])), fmaxf(fabsf(r[2]), fabsf(r[3]))), bounds = (t[0] + t[1]) + (t[2] + t[3]);
-        if (settle_four<true>(k, r, t, q, top, largest, newest(largest), ordinary && bounds <= 0x1p90f && most <= 0x1p90f && vectors >= kPixels<VEC>, acc, zeros,
+        // (a NaN among them shows in the error)
+        const float most = fmaxf(fmaxf(fabsf(r[0]), fabsf(r[1])), fmaxf(fabsf(r[2]), fabsf(r[3])));
+        if (settle_four<true>(k, r, t, q, top, largest, newest(largest), ordinary && most <= 0x1p90f && vectors >= kPixels<VEC>, acc, zeros,
                         [&](unsigned bin) __attribute__((always_inline)) { atomicAdd(&hist[bin * kReplicas + rep], 1u); })) return;
         // (one at a time, in registers that move down: about one four in a thousand, and their divisions side by side take the registers of everything else)
         const int n = min(vectors * VEC, 4);

@@ -42,8 +42,8 @@ __device__ __forceinline__ float int8_bound(int S, float sa, float sw, float b, 
 //   Without a bias, e32 = fl(|v32| c) with c >= Gamma (1 + 4.2 h), its successor at most, lies in [1, 1 + 10.4 h] Gamma|v|.
 //   With one, y32 = fl(v32 + b) is within h|y32| + 3h|v| of v + b, and 3h u|v| <= 1.5 h Gamma|v|; with c >= Gamma (1 + 6.8 h) and
 //   cu >= u (1 + 3.2 h), fma(cu, |y32| + e32, e32) lies in [1, 1 + 15.4 h] tau.
-// 15.4 h = 9.2e-7; what is left out is of the order h^2.  Returns whether that holds for all four (a NaN has a NaN for its bound either way)
-// and they are no larger than 2^90 (alpha times a bound is then an ordinary number); otherwise the bounds are left to int8_bound.
+// 15.4 h = 9.2e-7; what is left out is of the order h^2.  Returns whether that holds for all four (a NaN, which the tests leave out, has a NaN
+// for its bound either way) and they are no larger than 2^90 (alpha times a bound is then an ordinary number); otherwise the bounds are left to int8_bound.
 template <bool BIAS>
 __device__ __forceinline__ bool int8_quad(const Int8Args& p, intx4 S, float sa, floatv4 sw, floatv4 b, floatv4& y, floatv4& tau) {
     float f[4], v[4];

@@ -167,7 +167,8 @@ __device__ __forceinline__ unsigned newest(unsigned int* largest) {
     return __hip_atomic_load(largest, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 }
 // Quick settlement of four claims at once, also of those that leave their bounds, for kernels that have their elements in fours; t: binary32 bounds,
-// published: newest(largest); ok: whether estimates may be taken at all (q.alpha and q.eps ordinary, |r| at most 2^100, t at most 2^90).  alpha t to within 2^-17 decides a comparison
+// published: newest(largest); ok: whether estimates may be taken at all (q.alpha and q.eps ordinary, |r| at most 2^100).  Four bounds of 2^90 in all at most are numbers, which is
+// asked of their sum, as a minimum or a comparison would leave a NaN among them out (and admit its claim).  alpha t to within 2^-17 decides a comparison
 // that d misses by more than 2^-13 of it; the error's estimate, a bin that it is 16 steps inside of (of 0 and of the smallest ones, whose bin has
 // no lower edge, too).  What is no number, or too large, has an estimate beyond any error that occurs.  add(bin) counts an element.
 // The largest error is one element's: a thread that comes upon an estimate beyond its own largest and the workgroup's (*largest) keeps that element, whose exact error it
@@ -180,6 +181,7 @@ __device__ __forceinline__ bool settle_four(floatv4 c, floatv4 r, floatv4 t, con
     unsigned int bits[4], lowest = ~0u, highest = 0u, out = 0;
     float clear = INFINITY, furthest = 0.f;
     const unsigned int known = KEEP ? max(published, top.bits) : published;
+    ok = ok && (t[0] + t[1]) + (t[2] + t[3]) <= 0x1p90f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const float d = fabsf(c[e] - r[e]), at = t[e] * q.alpha;

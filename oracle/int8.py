@@ -46,5 +46,9 @@ def linear_int8(A, sa, W, sw, bias=None, model=None):
             tau = tau + L(u) * (np.abs(v + np.asarray(bias, np.float32).astype(L)[None, :]) + tau)
         if flags & 1:
             tau = tau + (np.abs(S) + np.abs(sa).astype(L) + np.abs(sw).astype(L) + 1) * L(2) ** -149
+        finite = np.isfinite(sa) & np.isfinite(sw)
+        if bias is not None:
+            finite = finite & np.isfinite(np.asarray(bias, np.float32))[None, :]
+        tau = np.where(finite, tau, L(np.nan))               # (finite operands beyond the binary32 range keep their value)
     assert y.dtype == np.float32
     return y, tau

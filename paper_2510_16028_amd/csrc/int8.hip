@@ -29,12 +29,14 @@ __device__ __forceinline__ bool beyond_limit(int S, const Int8Args& p) { return 
 
 // The bound of one sum in binary64.  Binary64 holds S sa exactly to a rounding of 2^-53, far inside the margin of the final upper
 // rounding; the sum with the bias may cancel, but its rounding is relative to terms that the bound itself carries.
+// NaN where an operand is not finite, as an infinite bound would admit every finite claim: finite ones stay far inside the binary64 range, so a sum
+// that is infinite there comes of an infinite operand.  (int8_quad leaves them to this, or has a NaN itself.)
 __device__ __forceinline__ float int8_bound(int S, float sa, float sw, float b, bool has_bias, const Int8Args& p) {
     const double s = (double)S, v = s * (double)sa * (double)sw;
     double e = (beyond_limit(S, p) ? p.g3 : p.g2) * fabs(v);
     if (has_bias) e = fma(p.u, fabs(v + (double)b) + e, e);
     e = fma(p.uflow, fabs(s) + fabs((double)sa) + fabs((double)sw) + 1.0, e);
-    return up32g(e);
+    return up32g(fma(0.0, e, e));                            // (0 times infinity is NaN)
 }
 // Outputs and bounds of four sums of a row.  The bound takes binary32 where that is accurate enough (eight binary64 instructions and three
 // conversions less).  With h = 2^-24: v32, of three roundings, is within 3h of v (a product with S is exact where it is subnormal, so only the

@@ -397,7 +397,8 @@ size_t tao_groupnorm_workspace_bytes(long batch, long channels, long positions, 
  *       TAO_ACT_SILU   y = s(p) = p/(1 + exp(-p)),  B = min(|s'(p)| E + E^2/4, 1.1 E),   tau = B + f/(1 - f) (|s(p)| + B),
  *                      f the relative error of tao_bound_act's SILU (|s''| <= 1/2 and |s'| < 1.1 everywhere).
  * y is the formula in binary64, rounded once to binary32; no re-executed output is needed for tau.  tau is at or above its formula's value and
- * within 1e-6 of it (for RELU within 1e-6 E).  A group whose bound is not finite gets NaN, as in tao_bound_norm.
+ * within 1e-6 of it (for RELU within 1e-6 E).  A group whose bound is not finite gets NaN, as in tao_bound_norm,
+ * and so does a channel whose gamma or beta is not finite.
  * x: pixel stride ldx >= channels; y, tau: pixel stride ldy; samples follow each other; either of y, tau may be NULL (not stored).  gamma, beta:
  * [channels] or NULL.  Any address and stride of whole elements; channels that are a multiple of 4 (of 2) move as vectors of as many.
  * ws / ws_bytes: DEVICE scratch of tao_groupnorm_act_workspace_bytes(...), 256-byte aligned, contents irrelevant before and

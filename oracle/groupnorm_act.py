@@ -44,7 +44,7 @@ def groupnorm_act(act, x, groups, gamma=None, beta=None, eps=1e-5, model=None):
         b = L(0) if beta is None else beta.astype(L).reshape(1, 1, groups, per)
         E_p = np.abs(g) * E_h + u * np.abs(g) * (ad * r + E_h)
         p = d * r * g + b
-        E = E_p + u * (np.abs(p) + E_p)
+        E = np.where(np.isfinite(g) & np.isfinite(b), E_p + u * (np.abs(p) + E_p), L(np.nan))
         if act == SILU:
             sig = 1 / (1 + np.exp(-p))
             y = p * sig

@@ -99,11 +99,12 @@ __device__ __forceinline__ GroupCoef group_coef(const RowConsts& k, double n, do
     c.K1 *= 1.0 + 2.0 * m; c.K0 *= 1.0 + 2.0 * m;
     return c;
 }
-// ... and of its channel: p = d rg + b, grow_ep E_p = k1 |d| + k0
+// ... and of its channel: p = d rg + b, grow_ep E_p = k1 |d| + k0 (NaN where gamma or beta is infinite: such a bound would admit every finite claim)
 struct ChannelCoef { double mu, rg, b, k1, k0; };
 __device__ __forceinline__ ChannelCoef channel_coef(const NormArgs& p, const GroupCoef& g, int channel) {
-    const double w = p.gamma ? (double)p.gamma[channel] : 1.0, grown = fabs(w) * p.grow_ep;
-    return ChannelCoef{g.mu, g.r * w, p.beta ? (double)p.beta[channel] : 0.0, grown * g.K1, grown * g.K0};
+    const float gamma = p.gamma ? p.gamma[channel] : 1.f, beta = p.beta ? p.beta[channel] : 0.f;
+    const double w = (double)gamma, grown = fabs(w) * p.grow_ep;
+    return ChannelCoef{g.mu, g.r * w, (double)beta, grown * g.K1, fma(grown, g.K0, (double)(gamma * 0.f + beta * 0.f))};
 }
 
 // 1 / (1 + exp(-p)) and 1 minus it, to 2^-39, for |p| <= 700 (beyond, those of 700 with p's sign: where |p| 2^-1009 stands for |p| exp(-|p|)).

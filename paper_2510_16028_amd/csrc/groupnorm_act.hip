@@ -135,7 +135,10 @@ __device__ __forceinline__ double sigmoid(double p, double& rest) {
 
 // Output and bound of one element.  E comes with the factor of the final upper rounding (kUp: 2^-24 for it, 2^-32 for the few roundings before it) and, for
 // SiLU, with that of its own roundings, so both cost nothing here.  The slacks keep an evaluation in round-to-nearest binary64 at or above the formula's
-// value: near a zero of s' its relative error is large, but 2^-36 (the sigmoid's error many times over) of E is far below 1e-6 of the other terms.
+// value.  s' = q (1 + p rest) is formed from q and rest = e q, e = exp(-p): a relative error of e (2^-40) reaches it as at most 2^-40 |s'| +
+// 2^-41 q, as |p| q rest < 0.28, and one of q (2^-46, the reciprocal's) as 2^-46 (|s'| + |p| q rest), at most 2^-45 |s'| + 2^-46 q.  kUp has the parts of |s'|, and 2^-39 q those of q.
+// That vanishes where s' does far below 0; about its zero at -1.278, where q = 0.22, it is 4e-13 E, far below 1e-6 of E^2/4 and the own roundings, 0.28 silu_f, together
+// (for unit roundoffs from 2^-40 on).
 constexpr double kUp = 1.0 + 0x1p-24 + 0x1p-32;
 __device__ __forceinline__ float rounded_up(double v) {      // (v holds kUp)
     float f = (float)v;
@@ -150,7 +153,7 @@ __device__ __forceinline__ void norm_element(float x, const ChannelCoef& c, cons
     if constexpr (ACT == TAO_ACT_SILU) {
         double rest;
         const double sig = sigmoid(p, rest), s = p * sig;
-        const double slope = fabs(fma(s, rest, sig)) + 0x1p-36;
+        const double slope = fma(0x1p-39, sig, fabs(fma(s, rest, sig)));
         const double B = E * fmin(fma(a.quarter, E, slope), 1.1);
         y = (float)s;
         tau = rounded_up(fma(a.silu_k, fabs(s), B));         // (a minimum leaves a NaN out, but E times 1.1 is one)

@@ -270,6 +270,9 @@ int tao_bound_linear_int8(const int8_t *A, const float *scale_a, const int8_t *W
 /* The same operator checked on the spot (Sec. 5.4 leaf check, Sec. 5.3 profile): *out receives exactly what
  * tao_check_and_profile(claimed, y, tau, ...) returns for the y and tau of tao_bound_linear_int8, neither of which is
  * stored.  y_ref: the verifier's own output to check against instead of y, or NULL.  y_ref, claimed: laid out like y.
+ * alpha: tau is the distance of an execution from the real-number value, and y is one execution itself, so two of those that tau covers lie up to
+ * 2 tau apart: alpha = 2 admits them all.  With alpha = 1 a proposer that applies the scales in y's order is admitted (the same bits); one that takes
+ * the other order, or multiplies the scales first, leaves tau in 3 to 6 elements of 1000, as the bound is a few roundings with no slack of a long sum.
  * ws / ws_bytes: DEVICE scratch of at least tao_check_workspace_bytes(M * N * batch), 256-byte aligned.  Errors as
  * for the two calls. */
 int tao_bound_check_linear_int8(const int8_t *A, const float *scale_a, const int8_t *W, const float *scale_w, const float *bias,
@@ -411,7 +414,8 @@ int tao_bound_groupnorm_act(int act, const float *x, const float *gamma, const f
 size_t tao_groupnorm_act_workspace_bytes(long batch, long positions, long channels, long groups);
 /* The same operator checked on the spot: *out receives what tao_check_and_profile(claimed, y, tau, ...) returns for the y and
  * tau of tao_bound_groupnorm_act, neither of which is stored.  y_ref: the verifier's own output to check against instead of y, or NULL.
- * y_ref, claimed: laid out like y (pixel stride ldy).  ws / ws_bytes: DEVICE scratch of
+ * y_ref, claimed: laid out like y (pixel stride ldy).  alpha: y is the formula's value rounded once, within u |y| <= tau of it, and a y_ref is any execution: a
+ * claim that tau covers lies up to 2 tau from either, and alpha = 2 admits it always.  ws / ws_bytes: DEVICE scratch of
  * tao_bound_check_groupnorm_act_workspace_bytes(...), 256-byte aligned. */
 int tao_bound_check_groupnorm_act(int act, const float *x, const float *gamma, const float *beta, double eps, const float *y_ref,
                                   const float *claimed, long batch, long positions, long channels, long groups, long ldx, long ldy,

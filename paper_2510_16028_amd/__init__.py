@@ -1014,7 +1014,8 @@ def tao_bound_linear_int8(A, scale_a, W, scale_w, bias=None, model=None, y=None,
 def tao_bound_check_linear_int8(A, scale_a, W, scale_w, claimed, bias=None, y_ref=None, alpha=1.0, eps_rel=1e-12, model=None,
                                 out=None, ws=None, readback=True):
     """The 8-bit product re-executed, bounded and checked against `claimed` in one call, nothing else stored (y_ref: check against
-    this output instead of the re-executed one).  Returns the profile dict (readback=True) or the device buffer."""
+    this output instead of the re-executed one).  alpha = 2 admits every execution that the bound covers; alpha = 1 refuses elements of
+    those that apply the scales in another order.  Returns the profile dict (readback=True) or the device buffer."""
     here, shape, operands, dims = _int8_args(A, scale_a, W, scale_w, bias)
     L = _lib or lib()
     cp, rp = _output(claimed, shape, here, "claimed"), None if y_ref is None else _output(y_ref, shape, here, "y_ref")
@@ -1083,7 +1084,8 @@ def tao_bound_groupnorm_act(x, groups, gamma=None, beta=None, eps=1e-5, act=ACT_
 def tao_bound_check_groupnorm_act(x, claimed, groups, gamma=None, beta=None, eps=1e-5, act=ACT_SILU, y_ref=None, alpha=1.0,
                                   eps_rel=1e-12, model=None, out=None, ws=None, readback=True):
     """act(GroupNorm(x)) re-executed, bounded and checked against `claimed` in one call, nothing else stored (y_ref: check against
-    this output instead of the re-executed one).  Returns the profile dict (readback=True) or the device buffer."""
+    this output instead of the re-executed one).  alpha = 2 admits every execution that the bound covers.  Returns the profile dict
+    (readback=True) or the device buffer."""
     here, shape, inputs, dims = _groupnorm_act_args(x, groups, gamma, beta)
     L = _lib or lib()
     cp, rp = _output(claimed, shape, here, "claimed"), None if y_ref is None else _output(y_ref, shape, here, "y_ref")

@@ -281,10 +281,12 @@ int tao_bound_check_linear_int8(const int8_t *A, const float *scale_a, const int
                                 const tao_fp_model *model, tao_profile *out, void *ws, size_t ws_bytes, void *stream);
 /* The 8-bit operand of the product from binary32 activations: per row, with m = max |x|,
  *     scale[r] = fl(m fl(1/127)),   q[r][c] = round(fl(x[r][c] / scale[r])) to the nearest whole number, ties to even, in [-127, 127].
- * (the product is how tensor programs on a device divide by a constant, so what they quantise is the same bit for bit).
+ * Every step is one correctly rounded operation: an implementation of these steps gives the same bit for bit.  The scale is the product, as tensor
+ * programs on the device form max / 127 (their quotient by a constant), so what those quantise is met bit for bit.  A program that divides, as on a host,
+ * has the next binary32 value above for 4.7 % of the scales, and in such a row another q, one beside this one, for arguments next to the middle of two:
+ * its product is checked on its own q and scale, not on these.
  * A row whose scale comes out as 0 (zeros; values below about 127 2^-150) has q = 0; a row that is not finite has scale NaN and
- * q = 0, so that its products are NaN, which no check admits.  Every step is one correctly rounded operation: the result is the same bit for
- * bit in any implementation.  x: [rows][cols], row stride ld; q: row stride ldq; scale: [rows]. */
+ * q = 0, so that its products are NaN, which no check admits.  x: [rows][cols], row stride ld; q: row stride ldq; scale: [rows]. */
 int tao_quantize_rows(const float *x, int8_t *q, float *scale, long rows, long cols, long ld, long ldq, void *stream);
 
 /* 2-D convolution bound without a stored patch matrix (Sec. 3.1: conv is a

@@ -294,7 +294,8 @@ struct Int8Walk {
     // columns k .. k + KB - 1 into stage `stage` (DIRECT) or into registers; units from column K on become 0
     __device__ __forceinline__ void request(int stage, int k) {
         if constexpr (DIRECT) {
-            // (written as assembly: the compiler would wait for these copies before every barrier; the waits are the explicit ones in the loop)
+            // (written as assembly: the compiler would wait for these copies before every barrier; the waits are the explicit ones in the loop.  m0 is a reserved register, which
+            // the compiler sets itself right before it needs it: it is not named as overwritten, which the compiler warns of.)
             if (k + SH::KB <= p.K) {
                 const signed char* a = A + k;
                 const signed char* w = W + k;

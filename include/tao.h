@@ -256,7 +256,7 @@ size_t tao_selftest_workspace_bytes(long cases);
  * The sum being exact, y is the same bit for bit whatever order forms it, and tau covers every execution that
  * accumulates in 32-bit whole numbers and applies the two scales in either order, or as one product, in binary32.
  * TAO_FLAG_UNDERFLOW_TERMS adds (|S| + |scale_a| + |scale_w| + 1) 2^-149 for scales and products that underflow.
- * exact <= tau <= exact (1 + 1e-6); tau is NaN where a scale or the bias is not finite, +inf beyond the binary32 range.
+ * exact <= tau <= exact (1 + 1e-6), or the next step where it is subnormal; tau is NaN where a scale or the bias is not finite, +inf beyond the binary32 range.
  * A: [batch][M][K] with row stride lda and batch stride strideA; W: [batch][N][K] (row j = weights of output j), ldw, strideW
  * (0 shares one W and one scale_w across the batch); any strides and addresses (rows of whole 16-byte units on
  * 16-byte addresses are read fastest).  scale_a: [batch][M], scale_w: [N] with strideW == 0, else [batch][N]; contiguous.
@@ -402,7 +402,7 @@ size_t tao_groupnorm_workspace_bytes(long batch, long channels, long positions, 
  *       TAO_ACT_SILU   y = s(p) = p/(1 + exp(-p)),  B = min(|s'(p)| E + E^2/4, 1.1 E),   tau = B + f/(1 - f) (|s(p)| + B),
  *                      f the relative error of tao_bound_act's SILU (|s''| <= 1/2 and |s'| < 1.1 everywhere).
  * y is the formula in binary64, rounded once to binary32; no re-executed output is needed for tau.  tau is at or above its formula's value and
- * within 1e-6 of it (for RELU within 1e-6 E).  A group whose bound is not finite gets NaN, as in tao_bound_norm,
+ * within 1e-6 of it (for RELU within 1e-6 E; more in a group whose var + eps lies within 3 % of its own error bound).  A group whose bound is not finite gets NaN, as in tao_bound_norm,
  * and so does a channel whose gamma or beta is not finite.
  * x: pixel stride ldx >= channels; y, tau: pixel stride ldy; samples follow each other; either of y, tau may be NULL (not stored).  gamma, beta:
  * [channels] or NULL.  Any address and stride of whole elements; channels that are a multiple of 4 (of 2) move as vectors of as many.

@@ -213,7 +213,7 @@ struct NormCheck {
         for (int e = 0; e < 4; ++e) { r[e] = REF ? rv[e] : yv[e]; t[e] = tv[e]; k[e] = c[e]; }
         // (a NaN among them shows in the error)
         const float most = fmaxf(fmaxf(fabsf(r[0]), fabsf(r[1])), fmaxf(fabsf(r[2]), fabsf(r[3])));
-        if (settle_four<true>(k, r, t, q, top, largest, newest(largest), ordinary && most <= 0x1p90f && vectors >= kPixels<VEC>, acc, zeros,
+        if (settle_four<true, true>(k, r, t, q, top, largest, newest(largest), ordinary && most <= 0x1p90f && vectors >= kPixels<VEC>, acc, zeros,
                         [&](unsigned bin) __attribute__((always_inline)) { atomicAdd(&hist[bin * kReplicas + rep], 1u); })) return;
         // (one at a time, in registers that move down: about one four in a thousand, and their divisions side by side take the registers of everything else)
         const int n = min(vectors * VEC, 4);

@@ -198,7 +198,7 @@ struct Int8Check {
         const unsigned int published = newest(largest);
         bool ok = estimated && cols == 4 && ordinary;
         if (y_ref) ok = ok && most_of(y) <= 0x1p100f;
-        if (settle_four<ROOM>(a.c, y, t, q, top, largest, published, ok, acc, zeros, [&](unsigned bin) __attribute__((always_inline)) { Int8Bins::add(hist, bin); })) return;
+        if (settle_four<ROOM, false>(a.c, y, t, q, top, largest, published, ok, acc, zeros, [&](unsigned bin) __attribute__((always_inline)) { Int8Bins::add(hist, bin); })) return;
 #pragma unroll 1
         for (int e = 0; e < cols; ++e)
             check_one<1>(a.c[e], y[e], int8_rounded(int8_bound<BIAS>(S[e], sa, sw[e], b[e], int8_own(S[e], p), p)), alpha, eps_rel, hist, 0, acc);

@@ -169,14 +169,14 @@ __device__ __forceinline__ unsigned newest(unsigned int* largest) {
 // Quick settlement of four claims at once, also of those that leave their bounds, for kernels that have their elements in fours; t: binary32 bounds,
 // published: newest(largest); ok: whether estimates may be taken at all (q.alpha and q.eps ordinary, |r| at most 2^100).  Four bounds of 2^90 in all at most are numbers, which is
 // asked of their sum, as a minimum or a comparison would leave a NaN among them out (and admit its claim).  alpha t to within 2^-17 decides a comparison
-// that d misses by more than 2^-13 of it, and any with d = 0 (t = 0 too: what ReLU leaves of most elements below 0); the error's estimate, a bin that it is 16 steps inside of (of 0 and of the smallest ones, whose bin has
+// that d misses by more than 2^-13 of it, and with ZEROS any with d = 0 (where bounds of 0 are common: what ReLU leaves of most elements below 0); the error's estimate, a bin that it is 16 steps inside of (of 0 and of the smallest ones, whose bin has
 // no lower edge, too).  What is no number, or too large, has an estimate beyond any error that occurs.  add(bin) counts an element.
 // The largest error is one element's: a thread that comes upon an estimate beyond its own largest and the workgroup's (*largest) keeps that element, whose exact error it
 // forms once, at its end (`settled`).  Estimates 32 steps apart are in the order of the errors; fours with an element closer to the largest one, or with two
 // that would replace it, are left to the exact check.  KEEP = false, for kernels without registers for that: what may exceed the largest error so far, then exact
 // and left in *largest by the caller, is left to the exact check.
 struct Farthest { unsigned int bits = 0; float c = 0.f, r = 0.f; };
-template <bool KEEP, class Add>
+template <bool KEEP, bool ZEROS, class Add>
 __device__ __forceinline__ bool settle_four(floatv4 c, floatv4 r, floatv4 t, const QuickCheck& q, Farthest& top, unsigned int* largest, unsigned int published, bool ok, ThreadAcc& acc, unsigned int& zeros, Add&& add) {
     unsigned int bits[4], lowest = ~0u, highest = 0u, out = 0;
     float clear = INFINITY, furthest = 0.f;
@@ -189,7 +189,7 @@ __device__ __forceinline__ bool settle_four(floatv4 c, floatv4 r, floatv4 t, con
         bits[e] = max(__float_as_uint(d * __builtin_amdgcn_rcpf(fabsf(r[e]) + q.eps)), 64u) + 16u;
         lowest = min(lowest, bits[e] & 0xfffffu);
         highest = max(highest, bits[e]);
-        clear = fminf(clear, d == 0.f ? INFINITY : fmaf(at, -0x1p-13f, fabsf(d - at)));
+        clear = fminf(clear, ZEROS && d == 0.f ? INFINITY : fmaf(at, -0x1p-13f, fabsf(d - at)));
         out += d > at;
     }
     if (!KEEP) {

@@ -502,8 +502,8 @@ __global__ __launch_bounds__(kCheckThreads) void clear_partials(CheckWorkspace w
     if (tid < kGroups) w.coarse[blockIdx.x * kGroups + tid] = 0;
     if (tid == 0) { BlockStats& o = w.stats[blockIdx.x]; o.violations = 0; o.nans = 0; o.max_bits = 0; }
 }
-// PAIR: two workgroups a compute unit, from two tiles for each on: one's checks go on under the other's products (2048 x 4096 x 12288 200 -> 180 us;
-// with one tile each the registers are worth more, 2048 x 2048 x 2048 33 us against 42, and with 288 tiles a launch less, 512 x 768 x 2304 22 against 26).
+// PAIR: two workgroups a compute unit, from two tiles for each on: one's checks go on under the other's products (2048 x 4096 x 12288 200 -> 165 us;
+// with one tile each the registers are worth more, 2048 x 2048 x 2048 32 us against 39, and with 288 tiles a launch less, 512 x 768 x 2304 22 against 28).
 template <class SH, bool DIRECT, bool PAIR>
 __global__ __launch_bounds__(SH::THREADS, PAIR ? SH::THREADS * 2 / (4 * kWave) : 1) void int8_tiles_check(Int8Args p, Int8Grid grid, const float* y_ref, const float* claimed, double alpha, double eps_rel,
                                                                 float quick, CheckWorkspace w) {

@@ -186,8 +186,8 @@ struct Int8Check {
     __device__ __forceinline__ void put(const Int8Args& p, long i, int cols, intx4 S, float sa, floatv4 sw, floatv4 b, const Ahead& a) {
         floatv4 y, t;
         const bool estimated = int8_quad<BIAS>(p, S, sa, sw, b, y, t);
-        // four claims equal to their outputs, within bounds that are ordinary numbers: errors of 0
-        bool same = estimated && !y_ref && cols == 4 && ordinary;
+        // four claims equal to their outputs: errors of 0 inside any bounds that are numbers, as they are where the outputs are (outputs and bounds of 0, of padded rows, too)
+        bool same = most_of(y) < INFINITY && !y_ref && cols == 4 && ordinary;
 #pragma unroll
         for (int e = 0; e < 4; ++e) same &= a.c[e] == y[e];
         if (same) {

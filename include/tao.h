@@ -12,7 +12,7 @@
  *
  * Conventions for every entry point
  *  - All tensor pointers are DEVICE pointers to binary32 data (8-bit whole
- *    numbers where int8_t is written) owned by the caller; row-major; leading
+ *    numbers where int8_t or uint8_t is written, positions as int64_t) owned by the caller; row-major; leading
  *    dimensions are in elements.  `tau` buffers (and `y`, `q`, `scale` of the
  *    operators that are re-executed) are written, everything else is read only.  Nothing is retained after return.
  *  - `stream` is the caller's hipStream_t passed as void* (NULL = the null
@@ -101,7 +101,7 @@ typedef struct tao_profile {
 
 /* Operator kinds of tao_bound_norm and tao_bound_act (operator list of App. A.3). */
 enum { TAO_NORM_LAYERNORM = 0, TAO_NORM_RMSNORM = 1, TAO_NORM_BN_AFFINE = 2,
-       TAO_NORM_SUM = 3, TAO_NORM_MEAN = 4 };
+       TAO_NORM_SUM = 3, TAO_NORM_MEAN = 4, TAO_NORM_NONE = 5 /* tao_bound_norm_rope only */ };
 enum { TAO_ACT_GELU_ERF = 0, TAO_ACT_SILU = 1, TAO_ACT_MUL = 2, TAO_ACT_ADD = 3, TAO_ACT_RELU = 4,
        TAO_ACT_SUB = 5, TAO_ACT_DIV = 6, TAO_ACT_EXACT = 7, TAO_ACT_SQRT = 8, TAO_ACT_RSQRT = 9,
        TAO_ACT_EXP = 10, TAO_ACT_LOG = 11, TAO_ACT_SIN = 12, TAO_ACT_COS = 13, TAO_ACT_TANH = 14,
@@ -288,6 +288,36 @@ int tao_bound_check_linear_int8(const int8_t *A, const float *scale_a, const int
  * A row whose scale comes out as 0 (zeros; values below about 127 2^-150) has q = 0; a row that is not finite has scale NaN and
  * q = 0, so that its products are NaN, which no check admits.  x: [rows][cols], row stride ld; q: row stride ldq; scale: [rows]. */
 int tao_quantize_rows(const float *x, int8_t *q, float *scale, long rows, long cols, long ld, long ldq, void *stream);
+
+/* Matrix product of binary32 activations with weights in 4 bits that have a scale, and possibly a zero point, for each group of a row's
+ * columns, as weight-quantised layers compute it, re-executed and bounded in one call:
+ *     w[j][k]   = (q[j][k] - z[j][k / group]) scale[j][k / group],
+ *     y[i][j]   = sum_k A[i][k] w[j][k] + bias[j],
+ *     tau[i][j] = Gamma(K') (sum_k |A[i][k]| |w[j][k]| + |bias[j]|),     K' = K + 1, or K + 2 with a bias:
+ * a product, at most K - 1 additions, the bias, and one rounding more where (q - z) scale is formed first or the scale is applied to a group's sum.
+ * q - z is a whole number and exact; executions that round q scale and z scale apart are not covered.
+ * y is the formula with an error of at most 27 u (sum_k |A||w| + |bias|), the last rounding among it (K <= 32: the formula in binary64, rounded once), which tau covers itself, so that alpha = 2 admits every execution that
+ * tau covers.  exact <= tau <= exact (1 + 1e-6), or the next step where it is subnormal; tau is NaN where an operand is not finite, +inf beyond the binary32 range.
+ * TAO_FLAG_UNDERFLOW_TERMS adds (K' + sum_k |A[i][k]| + sum_k |scale[j][k / group]|) 2^-149 (and takes the slower kernel of short reductions).
+ * A: [M][K], row stride lda.  W: [N][(K + 1) / 2] bytes, row stride ldw bytes: column 2i in the low four bits of byte i, 2i + 1 in the high ones (those behind an odd K
+ * are ignored).  scale: [N][G], zero: [N][G] whole numbers from 0 to 255 or NULL (8: the signed values -8 .. 7), contiguous, G = ceil(K / group).  group: a multiple of 32, or
+ * any number from K on (one scale a row).  bias: [N] or NULL.  y, tau: [M][N], row stride ldy; either may be NULL (not stored).  Any strides and addresses; rows of W
+ * and A on 16-byte addresses are read fastest.
+ * ws / ws_bytes: DEVICE scratch of tao_linear_int4_workspace_bytes(M, N, K), 256-byte aligned (NULL where that is 0), contents irrelevant before and garbage after; calls that
+ * share ws must be ordered on one stream.  TAO_ERR_K_RANGE where Gamma(K') is undefined; TAO_ERR_SHAPE also for another group, M or N >= 2^31 and M N >= 2^36.
+ * M or N equal to 0 is a no-op; K == 0 gives y = bias. */
+int tao_bound_linear_int4(const float *A, const uint8_t *W, const float *scale, const uint8_t *zero, long group, const float *bias,
+                          float *y, float *tau, long M, long N, long K, long lda, long ldw, long ldy,
+                          const tao_fp_model *model, void *ws, size_t ws_bytes, void *stream);
+size_t tao_linear_int4_workspace_bytes(long M, long N, long K);
+/* The same operator checked on the spot: *out receives exactly what tao_check_and_profile(claimed, y, tau, ...) returns for the y and tau of
+ * tao_bound_linear_int4.  y_ref: the verifier's own output to check against instead of y, or NULL.  y_ref, claimed: laid out like y.
+ * ws / ws_bytes: DEVICE scratch of tao_bound_check_linear_int4_workspace_bytes(M, N, K), 256-byte aligned.  Errors as for the two calls. */
+int tao_bound_check_linear_int4(const float *A, const uint8_t *W, const float *scale, const uint8_t *zero, long group, const float *bias,
+                                const float *y_ref, const float *claimed, long M, long N, long K, long lda, long ldw, long ldy,
+                                double alpha, double eps_rel, const tao_fp_model *model, tao_profile *out,
+                                void *ws, size_t ws_bytes, void *stream);
+size_t tao_bound_check_linear_int4_workspace_bytes(long M, long N, long K);
 
 /* 2-D convolution bound without a stored patch matrix (Sec. 3.1: conv is a
  * reduction with gamma_k of the output element; Conv2D of the operator list,
@@ -478,6 +508,47 @@ int tao_bound_check_rope(const float *x, const float *cos_table, const float *si
                          const float *claimed, long rows, long d, long inner, long npos, int interleaved,
                          double alpha, double eps_rel, const tao_fp_model *model, tao_profile *out,
                          void *ws, size_t ws_bytes, void *stream);
+
+/* The tables that tao_bound_rope and tao_bound_norm_rope take, from positions p and frequencies f (what a model makes of its base and of a longer context's scaling),
+ * re-executed and bounded in one call; m = scale is the amplitude that some scalings of long contexts carry:
+ *     cos_table[r][j] = m cos(p_r f_j),  sin_table[r][j] = m sin(p_r f_j),
+ *     E = Gamma(d) |p f|, d = 1, or 2 where |p| > 1/u (p is rounded too);
+ *     tau_cos = |m| B' [+ u |m| (|cos| + B') for m != 1],  B' = B + c_cos u (|cos| + B),  B = min(|sin| E + E^2/2, E, 1 + |cos|),   tau_sin likewise with c_sin.
+ * tau covers programs that form the angle in binary32, whose error grows with it, and those that form it in more bits.  The tables are the formula in binary64 (to |m| (2^-44 + 2^-52 |p f|)),
+ * rounded once; tau is at or above its formula's value and within 1e-6 of it.  m is rounded to binary32 first, as the operator does.  Angles from 2^50 on, and frequencies that are no numbers, give NaN.
+ * positions: [npos] or NULL (0, 1, 2, ...).  inv_freq: [half].  Outputs: [npos][half] contiguous; any of the four may be NULL (not stored).
+ * TAO_ERR_SHAPE for a scale that is not finite, half or npos >= 2^31 and npos half >= 2^40; TAO_ERR_ALIGN also for positions off 8 bytes. */
+int tao_bound_rope_tables(const int64_t *positions, const float *inv_freq, double scale, float *cos_table, float *sin_table,
+                          float *tau_cos, float *tau_sin, long npos, long half, const tao_fp_model *model, void *stream);
+
+/* Queries and keys before attention: the RMS norm of every head and the rotation of its first `rot` elements, re-executed and bounded in one call.  With h = x r g,
+ * r = 1/sqrt(mean(x^2) + eps) over the head's d elements (norm = TAO_NORM_RMSNORM; TAO_NORM_NONE: h = x, r = 1),
+ *     y_a = h_a cos - h_b sin,  y_b = h_b cos + h_a sin  on the pairs (j, j + rot/2), or (2j, 2j+1) when interleaved != 0, of the first rot elements,  y = h  on the others;
+ *     |h^ - h| <= F |x g|,  F = E_r + u R + u R (1+u)^2  of tao_bound_norm's RMSNORM without y_ref (0 for TAO_NORM_NONE),
+ *     tau_a = |x_a g_a| (k C + r tau_cos) + |x_b g_b| (k S + r tau_sin),  k = Gamma(2) (r + F) + F,  C = |cos| + tau_cos,  S = |sin| + tau_sin
+ *     (tau_b with a and b exchanged),  tau = F |x g|  on the others.
+ * Without a norm and without the tables' bounds this is tao_bound_rope's bound.  y is the formula in binary64, rounded once, so no re-executed output is needed, and
+ * alpha = 2 admits every execution that tau covers.  tau is at or above its formula's value and within 1e-6 of it; a head whose bound is not finite, an element whose
+ * operands are not, and the rotated elements of a token whose position lies outside the tables (y too) get NaN.  TAO_FLAG_UNDERFLOW_TERMS adds 2 2^-149 to rotated elements.
+ * x: head h of token t at x + t ldt + h ldh; heads_q heads with gain gamma_q, then heads_k with gamma_k (d elements each, or NULL: 1), as a fused projection leaves queries and keys.
+ * y, tau: at t ldyt + h ldyh, without overlap; either may be NULL (not stored).  cos_table, sin_table: [npos][rot/2] contiguous; tau_cos, tau_sin: their bounds, both or neither (NULL: 0).
+ * positions: [tokens], the table's row of each token, or NULL: t % npos.  eps is rounded to binary32 first.  Any strides and addresses; d and rot that are multiples of 8, on 16-byte
+ * addresses and strides, are read fastest.
+ * TAO_ERR_KIND for another norm, or a gain without one; TAO_ERR_SHAPE for an odd rot or rot > d, npos < 1, negative strides, overlapping outputs, one of tau_cos and tau_sin alone (TAO_ERR_NULL), d >= 2^30, or
+ * 2^36 elements or more; TAO_ERR_K_RANGE as for tao_bound_norm's RMSNORM. */
+int tao_bound_norm_rope(int norm, const float *x, const float *gamma_q, const float *gamma_k, double eps,
+                        const float *cos_table, const float *sin_table, const float *tau_cos, const float *tau_sin,
+                        const int64_t *positions, float *y, float *tau, long tokens, long heads_q, long heads_k, long d, long rot, long npos,
+                        long ldt, long ldh, long ldyt, long ldyh, int interleaved, const tao_fp_model *model, void *stream);
+/* The same operator checked on the spot: *out receives exactly what tao_check_and_profile(claimed, y, tau, ...) returns for the y and tau of tao_bound_norm_rope,
+ * neither of which is stored.  y_ref: the verifier's own output to check against instead of y, or NULL.  y_ref, claimed: laid out like y.
+ * ws / ws_bytes: DEVICE scratch of at least tao_check_workspace_bytes(tokens (heads_q + heads_k) d), 256-byte aligned.  Errors as for the two calls. */
+int tao_bound_check_norm_rope(int norm, const float *x, const float *gamma_q, const float *gamma_k, double eps,
+                              const float *cos_table, const float *sin_table, const float *tau_cos, const float *tau_sin,
+                              const int64_t *positions, const float *y_ref, const float *claimed,
+                              long tokens, long heads_q, long heads_k, long d, long rot, long npos,
+                              long ldt, long ldh, long ldyt, long ldyh, int interleaved, double alpha, double eps_rel,
+                              const tao_fp_model *model, tao_profile *out, void *ws, size_t ws_bytes, void *stream);
 
 /* Leaf check (Sec. 5.4) and relative-error profile (Sec. 5.3; Sec. 3.2 Eq. 2)
  * of n elements, in IEEE binary64 per element:

@@ -20,7 +20,7 @@ ERR_NULL, ERR_SHAPE, ERR_ALIGN, ERR_K_RANGE, ERR_MODEL, ERR_KIND, ERR_LAUNCH, ER
     -1, -2, -3, -4, -5, -6, -7, -8
 MODE_DETERMINISTIC, MODE_PROBABILISTIC = 0, 1
 FLAG_UNDERFLOW_TERMS, FLAG_FAST_ACCUM, FLAG_CHECK_IN_EPILOGUE = 1, 2, 4
-NORM_LAYERNORM, NORM_RMSNORM, NORM_BN_AFFINE, NORM_SUM, NORM_MEAN = 0, 1, 2, 3, 4
+NORM_LAYERNORM, NORM_RMSNORM, NORM_BN_AFFINE, NORM_SUM, NORM_MEAN, NORM_NONE = 0, 1, 2, 3, 4, 5
 ACT_GELU_ERF, ACT_SILU, ACT_MUL, ACT_ADD, ACT_RELU = 0, 1, 2, 3, 4
 (ACT_SUB, ACT_DIV, ACT_EXACT, ACT_SQRT, ACT_RSQRT, ACT_EXP, ACT_LOG, ACT_SIN, ACT_COS, ACT_TANH,
  ACT_POW, ACT_SIGMOID, ACT_GELU_TANH) = range(5, 18)
@@ -104,6 +104,8 @@ EXPORTS = ["tao_default_model", "tao_gamma", "tao_bound_linear", "tao_bound_line
            "tao_quantize_rows", "tao_bound_linear_int8", "tao_bound_check_linear_int8",
            "tao_bound_groupnorm_act", "tao_groupnorm_act_workspace_bytes", "tao_bound_check_groupnorm_act",
            "tao_bound_check_groupnorm_act_workspace_bytes",
+           "tao_bound_linear_int4", "tao_linear_int4_workspace_bytes", "tao_bound_check_linear_int4", "tao_bound_check_linear_int4_workspace_bytes",
+           "tao_bound_rope_tables", "tao_bound_norm_rope", "tao_bound_check_norm_rope",
            "tao_selftest_matrix_core", "tao_last_hip_error", "tao_status_string"]
 
 _lib = None
@@ -191,6 +193,15 @@ def lib():
     for f in (L.tao_groupnorm_act_workspace_bytes, L.tao_bound_check_groupnorm_act_workspace_bytes):
         f.argtypes = [lg] * 4
         f.restype = ctypes.c_size_t
+    L.tao_bound_linear_int4.argtypes = [vp] * 4 + [lg] + [vp] * 3 + [lg] * 6 + [mp, vp, ctypes.c_size_t, vp]
+    L.tao_bound_check_linear_int4.argtypes = [vp] * 4 + [lg] + [vp] * 3 + [lg] * 6 + [dbl, dbl, mp, vp, vp, ctypes.c_size_t, vp]
+    for f in (L.tao_linear_int4_workspace_bytes, L.tao_bound_check_linear_int4_workspace_bytes):
+        f.argtypes = [lg] * 3
+        f.restype = ctypes.c_size_t
+    L.tao_bound_rope_tables.argtypes = [vp, vp, dbl] + [vp] * 4 + [lg] * 2 + [mp, vp]
+    heads = [ctypes.c_int] + [vp] * 3 + [dbl] + [vp] * 7 + [lg] * 10 + [ctypes.c_int]
+    L.tao_bound_norm_rope.argtypes = heads + [mp, vp]
+    L.tao_bound_check_norm_rope.argtypes = heads + [dbl, dbl, mp, vp, vp, ctypes.c_size_t, vp]
     L.tao_selftest_matrix_core.argtypes = [ctypes.POINTER(ctypes.c_uint), vp, ctypes.c_size_t, vp]
     L.tao_last_hip_error.restype = ctypes.c_int
     L.tao_status_string.argtypes = [ctypes.c_int]
@@ -201,17 +212,17 @@ def lib():
 
 _torch_module = None
 # what every call asks torch for, looked up once with the module
-_Tensor = _float32 = _int8 = _uint8 = _raw_stream = _current_device = _capturing = None
+_Tensor = _float32 = _int8 = _uint8 = _int64 = _raw_stream = _current_device = _capturing = None
 
 
 def _torch():
     # (asked once: the answer costs more than the launch of a small kernel)
-    global _torch_module, _Tensor, _float32, _int8, _uint8, _raw_stream, _current_device, _capturing
+    global _torch_module, _Tensor, _float32, _int8, _uint8, _int64, _raw_stream, _current_device, _capturing
     if _torch_module is None:
         import torch
         if not torch.cuda.is_available():
             raise RuntimeError("paper_2510_16028_amd needs a GPU: no CPU fallback exists")
-        _Tensor, _float32, _int8, _uint8 = torch.Tensor, torch.float32, torch.int8, torch.uint8
+        _Tensor, _float32, _int8, _uint8, _int64 = torch.Tensor, torch.float32, torch.int8, torch.uint8, torch.int64
         _capturing = torch.cuda.is_current_stream_capturing
         _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         _torch_module = torch
@@ -874,7 +885,7 @@ INT8_MAX_K = 131071
 
 def _wrong(t, dtype, name):
     if not (isinstance(t, _Tensor) and t.is_cuda and t.dtype is dtype):
-        raise TypeError("%s must be %s CUDA tensor" % (name, "an int8" if dtype is _int8 else "a float32"))
+        raise TypeError("%s must be %s CUDA tensor" % (name, {_int8: "an int8", _uint8: "a uint8", _int64: "an int64"}.get(dtype, "a float32")))
     raise ValueError("%s is on device %d, the current device is %d" % (name, t.get_device(), _current_device()))
 
 
@@ -1023,6 +1034,173 @@ def tao_bound_check_linear_int8(A, scale_a, W, scale_w, claimed, bias=None, y_re
     rc = L.tao_bound_check_linear_int8(*operands, rp, cp, *dims, float(alpha), float(eps_rel), _mref(model), out.data_ptr(),
                                        ws.data_ptr(), ws.numel(), _raw_stream(here))
     _check(rc, "tao_bound_check_linear_int8")
+    return read_profile(out) if readback else out
+
+
+def tao_linear_int4_workspace_bytes(M, N, K):
+    return int(lib().tao_linear_int4_workspace_bytes(int(M), int(N), int(K)))
+
+
+def tao_bound_check_linear_int4_workspace_bytes(M, N, K):
+    return int(lib().tao_bound_check_linear_int4_workspace_bytes(int(M), int(N), int(K)))
+
+
+def _int4_args(A, W, scale, group, zero, bias):
+    """The current device, the output's shape, and the operands' addresses and the sizes and strides of the C call, checked."""
+    _torch_module or _torch()
+    here = _current_device()
+    As, Ws, Ss = _on(A, _float32, here, "A"), _on(W, _uint8, here, "W"), _on(scale, _float32, here, "scale")
+    if A.numel() > 0:
+        M, K, lda = _rows_view(A, "A")
+    elif len(As) > 0:                                    # (a tensor without elements has no strides to speak of)
+        M, K = 1, As[-1]
+        for n in As[:-1]:
+            M *= n
+        lda = K
+    else:
+        raise ValueError("A: need at least one dimension")
+    if len(Ws) != 2 or Ws[1] != (K + 1) // 2:
+        raise ValueError("W must be [N, %d]: two weights to a byte of a row" % ((K + 1) // 2))
+    N, ldw = Ws[0], Ws[1]
+    group = int(group)
+    if group < 1:
+        raise ValueError("group must be positive")
+    G = -(-K // group)
+    if tuple(Ss) != (N, G) or not scale.is_contiguous():
+        raise ValueError("scale must be contiguous and of shape (%d, %d)" % (N, G))
+    if zero is not None and (_on(zero, _uint8, here, "zero") != Ss or not zero.is_contiguous()):
+        raise ValueError("zero must be contiguous and shaped like scale")
+    if W.numel() > 0:
+        t = W.stride()
+        if ldw > 1 and t[1] != 1:
+            raise ValueError("W: last dimension must be contiguous")
+        if N > 1:
+            ldw = t[0]                                   # (rows that overlap are refused below, those of A too)
+    return (here, As[:-1] + Ws[:1], (A.data_ptr(), W.data_ptr(), scale.data_ptr(), _ptr(zero), group, _vector(bias, N, here, "bias")),
+            (M, N, K, lda if M > 1 else K, ldw, N or 1))
+
+
+def tao_bound_linear_int4(A, W, scale, group, zero=None, bias=None, model=None, y=None, tau=None, with_y=True, with_tau=True, ws=None):
+    """(y, tau) of A[..., K] times 4-bit weights W[N, (K + 1) / 2] (uint8, the even column in the low four bits) with scale[N, G] and zero[N, G]
+    (uint8; None: 8) for each group of `group` columns: the re-executed output and its bound (None in the place of one that is not asked for)."""
+    here, shape, operands, dims = _int4_args(A, W, scale, group, zero, bias)
+    L = _lib or lib()
+    y, tau, yp, tp = _reexecuted(y, tau, with_y, with_tau, shape, A, here)
+    need = L.tao_linear_int4_workspace_bytes(*dims[:3])
+    ws = (_capture_scratch(A.device, need) if need else None) if ws is None else _bytes(ws, here, "ws", need)
+    rc = L.tao_bound_linear_int4(*operands, yp, tp, *dims, _mref(model), _ptr(ws), 0 if ws is None else ws.numel(), _raw_stream(here))
+    _check(rc, "tao_bound_linear_int4")
+    return y, tau
+
+
+def tao_bound_check_linear_int4(A, W, scale, group, claimed, zero=None, bias=None, y_ref=None, alpha=1.0, eps_rel=1e-12, model=None,
+                                out=None, ws=None, readback=True):
+    """The product with 4-bit weights re-executed, bounded and checked against `claimed` in one call (y_ref: check against this output instead
+    of the re-executed one).  alpha = 2 admits every execution that the bound covers.  Returns the profile dict (readback=True) or the device buffer."""
+    here, shape, operands, dims = _int4_args(A, W, scale, group, zero, bias)
+    L = _lib or lib()
+    cp, rp = _output(claimed, shape, here, "claimed"), None if y_ref is None else _output(y_ref, shape, here, "y_ref")
+    out, ws = _profile_and_scratch(out, ws, A, here, L.tao_bound_check_linear_int4_workspace_bytes(*dims[:3]))
+    rc = L.tao_bound_check_linear_int4(*operands, rp, cp, *dims, float(alpha), float(eps_rel), _mref(model), out.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(here))
+    _check(rc, "tao_bound_check_linear_int4")
+    return read_profile(out) if readback else out
+
+
+def _table(t, shape, here, name):
+    """The address of a contiguous table, or None."""
+    if t is None:
+        return None
+    if _on(t, _float32, here, name) != shape or not t.is_contiguous():
+        raise ValueError("%s must be contiguous and of shape %s" % (name, tuple(shape)))
+    return t.data_ptr()
+
+
+def _positions(t, n, here):
+    if t is None:
+        return None
+    shape = _on(t, _int64, here, "positions")
+    if len(shape) != 1 or (n is not None and shape[0] != n) or not t.is_contiguous():
+        raise ValueError("positions must be a contiguous int64 vector" + ("" if n is None else " of %d" % n))
+    return t.data_ptr()
+
+
+def tao_bound_rope_tables(inv_freq, positions=None, npos=None, scale=1.0, model=None, cos=None, sin=None, tau_cos=None, tau_sin=None, with_tau=True):
+    """(cos, sin, tau_cos, tau_sin), each [npos, half]: the rotary tables scale * cos / sin of positions[npos] (int64; None: 0 .. npos - 1) times
+    inv_freq[half], and their bounds (None in their places without with_tau)."""
+    _torch_module or _torch()
+    here = _current_device()
+    fs = _on(inv_freq, _float32, here, "inv_freq")
+    if len(fs) != 1 or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq must be a contiguous vector")
+    pp = _positions(positions, None, here)
+    if positions is not None:
+        if npos is not None and npos != positions.shape[0]:
+            raise ValueError("npos is not the number of positions")
+        npos = positions.shape[0]
+    elif npos is None:
+        raise ValueError("positions or npos must be given")
+    shape = _torch_module.Size((int(npos), fs[0]))
+    outs = [cos, sin] + ([tau_cos, tau_sin] if with_tau else [None, None])
+    for i in range(4 if with_tau else 2):
+        if outs[i] is None:
+            outs[i] = _torch_module.empty(shape, dtype=_float32, device=inv_freq.device)
+    ptrs = [_table(t, shape, here, name) for t, name in zip(outs, ("cos", "sin", "tau_cos", "tau_sin"))]
+    rc = (_lib or lib()).tao_bound_rope_tables(pp, inv_freq.data_ptr(), float(scale), *ptrs, shape[0], shape[1], _mref(model), _raw_stream(here))
+    _check(rc, "tao_bound_rope_tables")
+    return tuple(outs)
+
+
+def _heads_args(x, cos, sin, norm, gamma, gamma_k, heads_k, eps, tau_cos, tau_sin, positions, interleaved):
+    """The current device, x's shape, and the arguments of the C calls before and after the outputs, checked."""
+    _torch_module or _torch()
+    here = _current_device()
+    shape = _on(x, _float32, here, "x")
+    if len(shape) != 3:
+        raise ValueError("x must be [tokens, heads, d]")
+    tokens, heads, d = shape
+    heads_k = int(heads_k)
+    if not 0 <= heads_k <= heads:
+        raise ValueError("heads_k must lie between 0 and the number of heads")
+    if gamma_k is not None and heads_k == 0:
+        raise ValueError("gamma_k needs heads_k")
+    ldt, ldh = heads * d, d
+    if x.numel() > 0:
+        t = x.stride()
+        if d > 1 and t[2] != 1:
+            raise ValueError("x: last dimension must be contiguous")
+        ldt, ldh = t[0] if tokens > 1 else 0, t[1] if heads > 1 else 0
+    table = _on(cos, _float32, here, "cos")
+    if len(table) != 2:
+        raise ValueError("cos and sin must be [npos, rot / 2]")
+    tables = [_table(t, table, here, name) for t, name in ((cos, "cos"), (sin, "sin"), (tau_cos, "tau_cos"), (tau_sin, "tau_sin"))]
+    if sin is None or (tau_cos is None) != (tau_sin is None):
+        raise ValueError("cos and sin, and tau_cos and tau_sin, come together")
+    return (here, shape, (int(norm), x.data_ptr(), _vector(gamma, d, here, "gamma"), _vector(gamma_k, d, here, "gamma_k"), float(eps), *tables, _positions(positions, tokens, here)),
+            (tokens, heads - heads_k, heads_k, d, 2 * table[1], table[0], ldt, ldh, heads * d, d, int(bool(interleaved))))
+
+
+def tao_bound_norm_rope(x, cos, sin, norm=NORM_RMSNORM, gamma=None, gamma_k=None, heads_k=0, eps=1e-6, positions=None, tau_cos=None, tau_sin=None,
+                        interleaved=False, model=None, y=None, tau=None, with_y=True, with_tau=True):
+    """(y, tau), contiguous, of the heads x[tokens, heads, d] (any strides but the last: a slice of a fused projection): RMS norm of each (NORM_NONE: none) with gain
+    gamma[d] (the last heads_k heads: gamma_k), then the rotation of the first 2 * cos.shape[1] elements by row positions[token] (None: token modulo
+    npos) of the tables cos, sin[npos, rot / 2], whose own bounds are tau_cos, tau_sin: the re-executed output and its bound (None in the place of one not asked for)."""
+    here, shape, inputs, dims = _heads_args(x, cos, sin, norm, gamma, gamma_k, heads_k, eps, tau_cos, tau_sin, positions, interleaved)
+    y, tau, yp, tp = _reexecuted(y, tau, with_y, with_tau, shape, x, here)
+    rc = (_lib or lib()).tao_bound_norm_rope(*inputs, yp, tp, *dims, _mref(model), _raw_stream(here))
+    _check(rc, "tao_bound_norm_rope")
+    return y, tau
+
+
+def tao_bound_check_norm_rope(x, cos, sin, claimed, norm=NORM_RMSNORM, gamma=None, gamma_k=None, heads_k=0, eps=1e-6, positions=None, tau_cos=None, tau_sin=None,
+                              interleaved=False, y_ref=None, alpha=1.0, eps_rel=1e-12, model=None, out=None, ws=None, readback=True):
+    """The norm and rotation of the heads re-executed, bounded and checked against `claimed` in one call, nothing else stored (y_ref: check against this output
+    instead of the re-executed one).  alpha = 2 admits every execution that the bound covers.  Returns the profile dict (readback=True) or the device buffer."""
+    here, shape, inputs, dims = _heads_args(x, cos, sin, norm, gamma, gamma_k, heads_k, eps, tau_cos, tau_sin, positions, interleaved)
+    L = _lib or lib()
+    cp, rp = _output(claimed, shape, here, "claimed"), None if y_ref is None else _output(y_ref, shape, here, "y_ref")
+    out, ws = _profile_and_scratch(out, ws, x, here, L.tao_check_workspace_bytes(x.numel()))
+    rc = L.tao_bound_check_norm_rope(*inputs, rp, cp, *dims, float(alpha), float(eps_rel), _mref(model), out.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(here))
+    _check(rc, "tao_bound_check_norm_rope")
     return read_profile(out) if readback else out
 
 

@@ -1,0 +1,331 @@
+"""The product with 4-bit weights and group scales against its oracle: outputs within the documented distance of the formula, bounds one-sided within
+1e-6, profiles equal to the streaming check of the stored output and bound; and a run of the operators of a decode step."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from oracle import int4, rotary
+from opmap import assert_profile_equal
+from test_gpu_int8 import assert_bound, cuda
+
+pytestmark = pytest.mark.gpu
+F, L, U = np.float32, np.longdouble, 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def tao():
+    import paper_2510_16028_amd as t
+    return t
+
+
+def operands(M, N, K, group, seed=0, zero=False, bias=False, spread=1.0):
+    rng = np.random.default_rng(seed + M + N + K)
+    G = -(-K // group)
+    A = (rng.normal(0, 1, (M, K)) * np.exp(rng.normal(0, spread, (M, K)))).astype(F)
+    q = rng.integers(0, 16, (N, K)).astype(np.uint8)
+    s = (rng.uniform(0.001, 0.1, (N, G)) * rng.choice([-1, 1], (N, G))).astype(F)
+    z = rng.integers(0, 16, (N, G)).astype(np.uint8) if zero else None
+    return A, q, s, group, z, rng.normal(0, 1, N).astype(F) if bias else None
+
+
+def run(tao, A, q, s, group, z, b, **more):
+    Ad, Wd, sd, zd, bd = cuda(A, int4.pack(q), s, z, b)
+    return tao.tao_bound_linear_int4(Ad, Wd, sd, group, zero=zd, bias=bd, **more)
+
+
+def assert_product(got, A, q, s, group, z, b, model=None, what=""):
+    y, tau = (t.cpu().numpy() for t in got)
+    ye, te, size = int4.linear_int4(A, q, s, group, z, b, model=model)
+    assert_bound(tau, te, what)
+    ok = np.isfinite(size)
+    # K <= 32: one rounding of the formula in binary64 (a sum of K products there); else the documented 27 u of the sum of magnitudes
+    far = np.abs(ye) * L(U) + size * L(2) ** -46 if A.shape[1] <= 32 else size * 27 * L(U)
+    assert (np.abs(y.astype(L) - ye)[ok] <= far[ok] * (1 + L(2) ** -20) + L(2) ** -149).all(), "%s %g" % (what, float((np.abs(y.astype(L) - ye)[ok] / np.maximum(size[ok], 1e-300) / U).max()))
+    assert (np.abs(y.astype(L) - ye)[ok & (te > 1e-30)] <= te[ok & (te > 1e-30)] * (1 + L(2) ** -20)).all(), what
+
+
+SHAPES = [(1, 1, 1, 32), (1, 7, 3, 3), (2, 16, 64, 32), (5, 33, 100, 32), (1, 64, 128, 128), (3, 40, 129, 64), (8, 129, 257, 128), (9, 64, 64, 64), (1, 300, 1000, 1000), (16, 31, 96, 96), (17, 70, 513, 512),
+          (33, 128, 512, 128), (1, 1000, 4096, 128), (2, 96, 12288, 128), (64, 65, 640, 32), (65, 32, 1001, 32), (130, 250, 320, 64), (4, 515, 2050, 256), (7, 4100, 200, 32), (31, 33, 63, 63), (6, 48, 5000, 160)]
+
+
+@pytest.mark.parametrize("M,N,K,group", SHAPES)
+@pytest.mark.parametrize("zero", [False, True])
+@pytest.mark.parametrize("bias", [False, True])
+def test_product(tao, M, N, K, group, zero, bias):
+    o = operands(M, N, K, group, 0, zero, bias)
+    assert_product(run(tao, *o), *o)
+
+
+@pytest.mark.parametrize("K", [0, 1, 2, 15, 16, 17, 31, 32, 33, 34, 63, 64, 65, 127, 128, 129, 255, 256, 257, 1023, 1025])
+def test_reduction_lengths(tao, K):
+    for group in (32, 64, max(K, 1)):
+        o = operands(3, 37, K, group, K, True, True)
+        assert_product(run(tao, *o), *o)
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 5, 8, 9, 16, 24, 25, 32, 40, 100])
+def test_numbers_of_tokens(tao, M):
+    o = operands(M, 100, 300, 64, M, True, False, spread=3.0)
+    assert_product(run(tao, *o), *o)
+
+
+def test_codes_one_by_one(tao):
+    """Every code with every zero point, and zero points outside the codes: one weight a row, so nothing can hide in a sum."""
+    for K in (1, 40, 300):
+        N, G = 256, -(-K // 64)
+        A, s = np.zeros((2, K), F), np.full((N, G), 0.5, F)
+        A[0, K - 1], A[1, 0] = 1.0, -3.0
+        q, z = np.repeat(np.arange(N)[:, None] % 16, K, 1).astype(np.uint8), np.repeat(np.arange(N)[:, None] // 16, G, 1).astype(np.uint8)
+        for zz in (z, z * 17, None):
+            y, tau = run(tao, A, q, s, 64, zz, None)
+            w = (q[:, 0].astype(int) - (8 if zz is None else zz[:, 0].astype(int))) * 0.5
+            assert np.array_equal(y.cpu().numpy(), np.stack([w, -3 * w]).astype(F))
+            assert_product((y, tau), A, q, s, 64, zz, None)
+
+
+def test_columns_of_zero_weights(tao):
+    """Codes equal to their zero points: exactly 0, with a bound of 0."""
+    A, q, s, group, z, _ = operands(9, 40, 384, 128, 1, True)
+    q[:20] = np.repeat(z[:20], 128, 1)
+    y, tau = run(tao, A, q, s, group, z, None)
+    assert not y[:, :20].any() and not tau[:, :20].any() and bool((tau[:, 20:] > 0).all())
+
+
+@pytest.mark.parametrize("spread", [0.0, 6.0, 12.0])
+def test_tokens_of_any_range(tao, spread):
+    """Elements whose sizes differ by many octaves: what a sum keeps of the small ones is part of the bound's 1e-6."""
+    rng = np.random.default_rng(4)
+    o = list(operands(11, 64, 700, 128, 4, True, False, spread=spread))
+    if spread == 12.0:                                       # single bits, and all significant bits, at every place
+        o[0] = (o[0].view(np.uint32) & np.uint32(0xff800000) | rng.choice([0, 1, 0x7fffff, 0x400000, 0x00ffff, 0x7f0000, 0x7fff], o[0].shape).astype(np.uint32)).view(F)
+    assert_product(run(tao, *o), *o)
+
+
+@pytest.mark.parametrize("K,group", [(20, 20), (200, 64), (1024, 128)])
+def test_values_that_are_no_ordinary_numbers(tao, K, group):
+    M, N = 20, 40
+    A, q, s, _, z, b = operands(M, N, K, group, 5, True, True)
+    A[0, 3], A[1, 5], A[2, 0] = np.inf, np.nan, -np.inf
+    A[3], A[4], A[5, ::2], A[6] = 0, 1e-42, 1e-36, 3e38
+    A[7, 1], A[8, 2], A[9], A[10, 0] = 1e-45, 1e-38, A[9] * F(1e-35), 2.0 ** 120
+    A[11] *= F(2.0 ** -100)
+    A[12] *= F(2.0 ** 108)
+    A[13, K // 2] = 2.0 ** -101
+    s[2, 0], s[3, -1], s[4, 0], s[5], s[6] = np.nan, np.inf, 0.0, 1e-42, 1e38
+    b[10], b[11], b[12] = np.nan, -np.inf, 3e38
+    got = run(tao, A, q, s, group, z, b)
+    y, tau = (t.cpu().numpy() for t in got)
+    ye, te, size = int4.linear_int4(A, q, s, group, z, b)
+    assert_bound(tau, te)
+    with np.errstate(all="ignore"):
+        ok = np.isfinite(te) & (np.abs(ye) < 3e38)
+        assert (np.abs(y.astype(L) - ye)[ok] <= 27 * U * size[ok] * (1 + 1e-6) + L(2) ** -149).all()
+    pf = tao.tao_bound_check_linear_int4(*cuda(A, int4.pack(q), s), group, got[0].clone(), zero=cuda(z)[0], bias=cuda(b)[0])
+    assert_profile_equal(pf, oracle.check_and_profile(y, y, tau))
+
+
+@pytest.mark.parametrize("model", [dict(mode=1, lam=4.0), dict(flags=1), dict(u=2.0 ** -16), dict(flags=1, u=2.0 ** -20)])
+@pytest.mark.parametrize("K,group", [(30, 32), (700, 128)])
+def test_models(tao, model, K, group):
+    o = list(operands(7, 65, K, group, 8, True, True))
+    o[0][0] = 1e-40
+    o[2][0] = 1e-30
+    m = tao.FpModel(**model)
+    y, tau = run(tao, *o, model=m)
+    assert_bound(tau.cpu().numpy(), int4.linear_int4(*o, model=m)[1])
+
+
+@pytest.mark.parametrize("M,N,K,group", [(3, 50, 96, 32), (9, 70, 257, 64), (20, 40, 512, 128)])
+@pytest.mark.parametrize("pad,at,pada,ata", [(0, 0, 0, 0), (1, 0, 3, 1), (3, 5, 0, 2), (16, 0, 4, 0), (16, 16, 4, 4), (7, 1, 1, 3), (4, 4, 2, 0)])
+def test_strides_and_addresses(tao, M, N, K, group, pad, at, pada, ata):
+    """Rows further apart than they are long, from any address; what lies between is NaN in A and 255 in W and must not count."""
+    A, q, s, _, z, b = operands(M, N, K, group, pad + at, True, True)
+    W = int4.pack(q)
+
+    def placed(a, pad, at, fill):
+        rows, k = a.shape
+        flat = np.full(at + rows * (k + pad) + 64, fill, a.dtype)
+        for r in range(rows):
+            flat[at + r * (k + pad): at + r * (k + pad) + k] = a[r]
+        return torch.from_numpy(flat).cuda()[at: at + rows * (k + pad)].view(rows, k + pad)[:, :k]
+    sd, zd, bd = cuda(s, z, b)
+    got = tao.tao_bound_linear_int4(placed(A, pada, ata, np.nan), placed(W, pad, at, 255), sd, group, zero=zd, bias=bd)
+    assert_product(got, A, q, s, group, z, b)
+
+
+def test_wide_output_rows_keep_what_lies_between_them(tao):
+    for M, N, K in ((5, 33, 64), (30, 257, 128), (2, 64, 31)):
+        A, q, s, group, z, _ = operands(M, N, K, 32, 3)
+        Ad, Wd, sd = cuda(A, int4.pack(q), s)
+        y, tau = torch.full((M, N + 9), 7.0, device="cuda"), torch.full((M, N + 9), 7.0, device="cuda")
+        ws = torch.empty(max(256, tao.tao_linear_int4_workspace_bytes(M, N, K)), dtype=torch.uint8, device="cuda")
+        rc = tao.lib().tao_bound_linear_int4(Ad.data_ptr(), Wd.data_ptr(), sd.data_ptr(), None, 32, None, y.data_ptr(), tau.data_ptr(), M, N, K, K, (K + 1) // 2, N + 9, None,
+                                             ws.data_ptr(), ws.numel(), tao._stream())
+        assert rc == 0
+        assert_product((y[:, :N], tau[:, :N]), A, q, s, 32, None, None)
+        assert bool((y[:, N:] == 7).all()) and bool((tau[:, N:] == 7).all())
+        # claims and outputs of such rows are checked in place
+        claimed, ref = y.clone(), y.clone()
+        claimed[M - 1, 3] += 1.0
+        out, need = tao.new_profile_buffer(y.device), tao.tao_bound_check_linear_int4_workspace_bytes(M, N, K)
+        wsc = torch.empty(need, dtype=torch.uint8, device="cuda")
+        for r in (None, ref.data_ptr()):
+            rc = tao.lib().tao_bound_check_linear_int4(Ad.data_ptr(), Wd.data_ptr(), sd.data_ptr(), None, 32, None, r, claimed.data_ptr(), M, N, K, K, (K + 1) // 2, N + 9, 1.0, 1e-12, None,
+                                                       out.data_ptr(), wsc.data_ptr(), need, tao._stream())
+            pf = tao.read_profile(out)
+            assert rc == 0 and pf["n"] == M * N and pf["violations"] == 1
+
+
+def test_leading_dimensions_and_one_of_the_two_outputs(tao):
+    A, q, s, group, z, b = operands(24, 70, 256, 64, 1, True, True)
+    Ad, Wd, sd, zd, bd = cuda(A, int4.pack(q), s, z, b)
+    y, tau = tao.tao_bound_linear_int4(Ad, Wd, sd, group, zero=zd, bias=bd)
+    y3, t3 = tao.tao_bound_linear_int4(Ad.view(2, 3, 4, 256), Wd, sd, group, zero=zd, bias=bd)
+    assert y3.shape == (2, 3, 4, 70) and torch.equal(y3.view(24, 70), y) and torch.equal(t3.view(24, 70), tau)
+    one = tao.tao_bound_linear_int4(Ad[0], Wd, sd, group, zero=zd, bias=bd)
+    assert one[0].shape == (70,)
+    y1, none = tao.tao_bound_linear_int4(Ad, Wd, sd, group, zero=zd, bias=bd, with_tau=False)
+    none2, t1 = tao.tao_bound_linear_int4(Ad, Wd, sd, group, zero=zd, bias=bd, with_y=False)
+    assert none is None and none2 is None and torch.equal(y, y1) and torch.equal(tau, t1)
+
+
+CHECKED = [(1, 1, 1, 32), (3, 100, 70, 32), (16, 512, 512, 128), (1, 5000, 128, 128), (33, 300, 640, 64), (8, 2100, 256, 128), (70, 1000, 96, 96), (2, 40000, 64, 32)]
+
+
+@pytest.mark.parametrize("M,N,K,group", CHECKED)
+@pytest.mark.parametrize("ref", [False, True])
+def test_check_is_the_streaming_check_of_the_stored_bound(tao, M, N, K, group, ref):
+    A, q, s, _, z, b = operands(M, N, K, group, M * N, True, True)
+    Ad, Wd, sd, zd, bd = cuda(A, int4.pack(q), s, z, b)
+    y, tau = tao.tao_bound_linear_int4(Ad, Wd, sd, group, zero=zd, bias=bd)
+    g = torch.Generator(device="cuda").manual_seed(M + N)
+    f = torch.tensor([0.0, 0.0, 0.5, -0.99, 1.0, 1.01, -3.0, 1e6], device="cuda")[torch.randint(0, 8, y.shape, generator=g, device="cuda")]
+    claimed = (y.double() + f.double() * tau.double()).float()
+    claimed.view(-1)[0] = float("nan")
+    claimed.view(-1)[-1] = float("inf")
+    y_ref = (y * (1 + 2.0 ** -23)).contiguous() if ref else None
+    for alpha, eps_rel in ((1.0, 1e-12), (2.0, 0.0)):
+        pf = tao.tao_bound_check_linear_int4(Ad, Wd, sd, group, claimed, zero=zd, bias=bd, y_ref=y_ref, alpha=alpha, eps_rel=eps_rel)
+        other = y if y_ref is None else y_ref
+        assert_profile_equal(pf, oracle.check_and_profile(claimed.cpu().numpy(), other.cpu().numpy(), tau.cpu().numpy(), alpha, eps_rel))
+    honest = tao.tao_bound_check_linear_int4(Ad, Wd, sd, group, y.clone(), zero=zd, bias=bd)
+    assert honest["accept"] == 1 and honest["max_rel"] == 0.0 and honest["n"] == M * N
+
+
+def test_checks_of_nothing(tao):
+    for M, N in ((0, 5), (5, 0)):
+        A, q, s, group, _, _ = operands(M, N, 64, 32)
+        a = cuda(A, int4.pack(q), s)
+        pf = tao.tao_bound_check_linear_int4(*a, group, torch.empty((M, N), device="cuda"))
+        assert pf["n"] == 0 and pf["accept"] == 1 and pf["hist"].sum() == 0
+        assert tao.tao_bound_linear_int4(*a, group)[0].shape == (M, N)
+
+
+@pytest.mark.parametrize("M,N,K", [(10, 33, 96), (9, 40, 100)])
+def test_offsets_beyond_32_bits(tao, M, N, K):
+    """Rows of A and W so far apart that the last ones lie more than 2^31 elements on."""
+    A, q, s, group, z, b = operands(M, N, K, 32, 3, True)
+    Ad, Wd, sd, zd = cuda(A, int4.pack(q), s, z)
+    expect = tao.tao_bound_linear_int4(Ad, Wd, sd, group, zero=zd)
+    far = lambda t: torch.empty((len(t), 2 ** 31 // len(t) + 2 ** 20), dtype=t.dtype, device="cuda")[:, 16:16 + t.shape[1]].copy_(t)
+    for a, w in ((far(Ad), Wd), (Ad, far(Wd))):
+        got = tao.tao_bound_linear_int4(a, w, sd, group, zero=zd)
+        assert torch.equal(got[0], expect[0]) and torch.equal(got[1], expect[1])
+
+
+def test_refusals_of_the_binding(tao):
+    A, q, s, group, z, b = operands(8, 16, 64, 32, 0, True, True)
+    A, W, s, z, b = cuda(A, int4.pack(q), s, z, b)
+    call, check = tao.tao_bound_linear_int4, tao.tao_bound_check_linear_int4
+    for bad in (lambda: call(A.double(), W, s, 32), lambda: call(A, W.to(torch.int8), s, 32), lambda: call(A.cpu(), W, s, 32), lambda: call(A, W, s, 32, zero=z.float()), lambda: check(A, W, s, 32, None)):
+        with pytest.raises(TypeError):
+            bad()
+    for bad in (lambda: call(A, W[:, :31], s, 32), lambda: call(A, W, s[:, :1], 32), lambda: call(A, W, s, 64), lambda: call(A, W, s, 0), lambda: call(A, W, s, 32, zero=z[:8]),
+                lambda: call(A, W, s, 32, bias=b[:3]), lambda: call(A.t(), W, s, 32), lambda: call(A, W, s, 32, y=torch.empty((8, 15), device="cuda")),
+                lambda: call(A, W, s, 32, with_y=False, with_tau=False), lambda: check(A, W, s, 32, torch.empty((16, 8), device="cuda")),
+                lambda: check(A, W, s, 32, torch.empty((8, 16), device="cuda"), ws=torch.empty(64, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(tao.TaoError):                        # rows that overlap: read by no call, as their lengths are not the ones that strides say
+        call(A[:1].expand(8, 64), W, s, 32)
+    with pytest.raises(tao.TaoError):
+        call(A, W[:1].expand(16, 32), s, 32)
+    with pytest.raises(tao.TaoError):
+        call(A, W, torch.ones((16, 4), device="cuda"), 16)
+
+
+def step(tao, A, W, s, z, inv, pos, gq, gk, y=None):
+    """Queries, keys and values of a decode step from 4-bit weights; then the tables of the positions, and norm and rotation of the queries and keys where they lie."""
+    y, tau = tao.tao_bound_linear_int4(A, W, s, 128, zero=z)
+    tables = tao.tao_bound_rope_tables(inv, pos)
+    rows = torch.arange(len(pos), device="cuda")
+    x = y.view(len(pos), -1, 64)[:, :10]
+    h = tao.tao_bound_norm_rope(x, tables[0], tables[1], gamma=gq, gamma_k=gk, heads_k=2, positions=rows, tau_cos=tables[2], tau_sin=tables[3])
+    return (y, tau) + tables + h
+
+
+def test_a_decode_step(tao):
+    """The three operators together, eagerly and as a captured graph that is replayed on new inputs."""
+    rng = np.random.default_rng(9)
+    M, K, N = 6, 256, 12 * 64
+    q, s, z = rng.integers(0, 16, (N, K)).astype(np.uint8), rng.uniform(0.001, 0.02, (N, 2)).astype(F), rng.integers(6, 11, (N, 2)).astype(np.uint8)
+    inv = (1e6 ** (-np.arange(32) / 32)).astype(F)
+    gq, gk = (rng.normal(1, 0.1, 64).astype(F) for _ in range(2))
+    A = [rng.normal(0, 1, (M, K)).astype(F) for _ in range(3)]
+    pos = [rng.integers(0, 50000, M) for _ in range(3)]
+    fixed = cuda(int4.pack(q), s, z, inv)
+    gains = cuda(gq, gk)
+    eager = []
+    for a, p in zip(A, pos):
+        ad, pd = cuda(a, p)
+        got = step(tao, ad, *fixed, pd, *gains)
+        assert_product(got[:2], a, q, s, 128, z, None)
+        tables = rotary.rope_tables(p, inv)
+        for g, e in zip(got[4:6], tables[2:]):
+            assert_bound(g.cpu().numpy(), e)
+        arrays = [t.cpu().numpy() for t in got]
+        y, tau = rotary.norm_rope(arrays[0].reshape(M, -1, 64)[:, :10], arrays[2], arrays[3], 64, gamma_q=gq, gamma_k=gk, heads_k=2, tau_cos=arrays[4], tau_sin=arrays[5])
+        assert_bound(arrays[7], tau)
+        assert (np.abs(arrays[6].astype(L) - y) <= tau).all()
+        for alpha, off, accept in ((1.0, 0.0, 1), (1.0, 2.0, 0), (2.0, 1.9, 1)):
+            claim = (got[6].double() + off * got[7].double()).float()
+            pf = tao.tao_bound_check_norm_rope(got[0].view(M, -1, 64)[:, :10], got[2], got[3], claim, gamma=gains[0], gamma_k=gains[1], heads_k=2, positions=torch.arange(M, device="cuda"),
+                                               tau_cos=got[4], tau_sin=got[5], alpha=alpha)
+            assert pf["accept"] == accept
+        eager.append([t.clone() for t in got])
+    static_a, static_p = cuda(A[0], pos[0])
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step(tao, static_a, *fixed, static_p, *gains)
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step(tao, static_a, *fixed, static_p, *gains)
+    for round_ in range(2):
+        for a, p, expect in zip(A, pos, eager):
+            static_a.copy_(torch.from_numpy(a))
+            static_p.copy_(torch.from_numpy(p))
+            graph.replay()
+            torch.cuda.synchronize()
+            other = step(tao, static_a * 2, *fixed, static_p, *gains)       # eager work between the replays
+            for g, e in zip(captured, expect):
+                assert torch.equal(g, e)
+            del other
+
+
+def test_calls_on_two_streams(tao):
+    o = operands(9, 300, 1024, 128, 2, True)
+    A, W, s, z = cuda(o[0], int4.pack(o[1]), o[2], o[4])
+    y, tau = tao.tao_bound_linear_int4(A, W, s, 128, zero=z)
+    torch.cuda.synchronize()
+    streams, results = [torch.cuda.Stream() for _ in range(2)], []
+    for n in range(6):
+        with torch.cuda.stream(streams[n % 2]):
+            results.append((tao.tao_bound_linear_int4(A, W, s, 128, zero=z),
+                            tao.tao_bound_check_linear_int4(A, W, s, 128, y, zero=z, readback=False,
+                                                            ws=torch.empty(tao.tao_bound_check_linear_int4_workspace_bytes(9, 300, 1024), dtype=torch.uint8, device="cuda"))))
+    torch.cuda.synchronize()
+    for (y2, t2), pf in results:
+        assert torch.equal(y, y2) and torch.equal(tau, t2) and tao.read_profile(pf)["accept"] == 1

@@ -296,7 +296,7 @@ int tao_quantize_rows(const float *x, int8_t *q, float *scale, long rows, long c
  *     tau[i][j] = Gamma(K') (sum_k |A[i][k]| |w[j][k]| + |bias[j]|),     K' = K + 1, or K + 2 with a bias:
  * a product, at most K - 1 additions, the bias, and one rounding more where (q - z) scale is formed first or the scale is applied to a group's sum.
  * q - z is a whole number and exact; executions that round q scale and z scale apart are not covered.
- * y is the formula with an error of at most 27 u (sum_k |A||w| + |bias|), the last rounding among it (K <= 32: the formula in binary64, rounded once), which tau covers itself, so that alpha = 2 admits every execution that
+ * y is the formula with an error of at most 15 u (sum_k |A||w| + |bias|), the last rounding among it (K <= 32: the formula in binary64, rounded once), which tau covers itself, so that alpha = 2 admits every execution that
  * tau covers.  exact <= tau <= exact (1 + 1e-6), or the next step where it is subnormal; tau is NaN where an operand is not finite, +inf beyond the binary32 range.
  * TAO_FLAG_UNDERFLOW_TERMS adds (K' + sum_k |A[i][k]| + sum_k |scale[j][k / group]|) 2^-149 (and takes the slower kernel of short reductions).
  * A: [M][K], row stride lda.  W: [N][(K + 1) / 2] bytes, row stride ldw bytes: column 2i in the low four bits of byte i, 2i + 1 in the high ones (those behind an odd K

@@ -1,6 +1,7 @@
 // tao_bound_rope_tables, tao_bound_norm_rope, tao_bound_check_norm_rope: the tables of the rotary embedding from positions and frequencies, and the
 // RMS norm of every query and key head with the rotation of its first elements, re-executed and bounded in one call (operators of App. A.3; primitive
 // rule of Sec. 3.1, Gamma(n-1) and Gamma(2) for the reductions).
+#include <type_traits>
 #include "tao_check.hpp"
 #include "tao_device.hpp"
 #include "tao_host.hpp"
@@ -47,15 +48,24 @@ __device__ __forceinline__ void table_element(const TableArgs& a, double p, doub
     v[2] = up32g(fma(a.k1[0], bc, a.k2[0] * ac)); v[3] = up32g(fma(a.k1[1], bs, a.k2[1] * as));
     if (!(fabs(t) < 0x1p50)) { v[0] = v[1] = v[2] = v[3] = NAN; }
 }
+// A thread has VEC neighbouring frequencies of a position: 16-byte stores where rows are whole vectors.  What bounds it: the tables' bytes (16 an element) for long ones.
+template <int VEC>
 __global__ __launch_bounds__(256) void rope_tables(TableArgs a) {
-    const long n = a.npos * a.half, stride = (long)gridDim.x * 256;
+    const unsigned per = (unsigned)a.half / VEC;
+    const long n = a.npos * per, stride = (long)gridDim.x * 256;
     for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += stride) {
-        const long r = i / a.half;
-        const int j = (int)(i - r * a.half);
-        float v[4];
-        table_element(a, (double)(a.positions ? a.positions[r] : r), (double)a.inv_freq[j], v);
+        const long r = n < (1L << 32) ? (long)((unsigned)i / per) : i / per;
+        const int j = (int)(i - r * per) * VEC;
+        const double p = (double)(a.positions ? a.positions[r] : r);
+        float v[VEC][4];
 #pragma unroll
-        for (int o = 0; o < 4; ++o) if (a.out[o]) a.out[o][i] = v[o];
+        for (int e = 0; e < VEC; ++e) table_element(a, p, (double)a.inv_freq[j + e], v[e]);
+#pragma unroll
+        for (int o = 0; o < 4; ++o) {
+            if (!a.out[o]) continue;
+            if constexpr (VEC == 4) ntstore4(reinterpret_cast<float4*>(a.out[o] + i * 4), make_float4(v[0][o], v[1][o], v[2][o], v[3][o]));
+            else a.out[o][i] = v[0][o];
+        }
     }
 }
 
@@ -68,23 +78,31 @@ struct HeadArgs {
     const float* y_ref; const float* claimed;
     long tokens, npos, ldt, ldh, ldyt, ldyh;
     int heads_q, heads, d, rot;
-    bool interleaved;
+    bool interleaved, norm;
     RowConsts k;
     double g2, uflow;                // Gamma(2), 2 2^-149 or 0
     double norm_fy;                  // u (1 + u)^2
 };
-// What a head's sum of squares gives: r, F (an element's error is F |x g|), k of the rotation, and the factors of the final rounding.
+// What a head's sum of squares gives: r, F (an element's error is F |x g|), k of the rotation, and the factors of the final rounding.  The chain of rsqrt_tail with inverse roots from
+// v_rsq_f64 (2^-24) and two Newton steps in place of its roots and divisions (a few 2^-53, far inside the margin): it is run for every head by all lanes that have one.
 struct HeadCoef { double r, F, k, mul, sub; };
-template <bool NORM>
+__device__ __forceinline__ double inverse_root(double w) {
+    double r = __builtin_amdgcn_rsq(w);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r = fma(r * 0.5, fma(-w * r, r, 1.0), r);
+    return r;
+}
 __device__ __forceinline__ HeadCoef head_coef(const HeadArgs& a, double squares) {
     HeadCoef h{1.0, 0.0, a.g2, kUpMul, 1.0 + 0x1p-46};
-    if constexpr (NORM) {
+    if (a.norm) {
         const RowConsts& k = a.k;
         const double E_t = (k.G * (1.0 + k.u) + k.u) * squares, vstar = squares * k.inv_n;
         const double E_v = (E_t * k.inv_n + k.cd_u * vstar) * k.inv1mcd;
-        double E_r, R, amp;
-        const bool ok = rsqrt_tail(vstar, E_v, k, h.r, E_r, R, amp);
-        h.F = ok ? E_r + k.u * R + a.norm_fy * R : NAN;
+        const double w = vstar + k.eps, E_w = (E_v + k.u * w) * k.inv1mu, w_lo = w - E_w, s = inverse_root(w_lo);
+        const double E_r = fma(0.5 * E_w, s * s * s, k.cr_u * s), amp = (w + E_w) * s * s;
+        h.r = inverse_root(w);
+        const double R = h.r + E_r;
+        h.F = w_lo > 0.0 ? E_r + k.u * R + a.norm_fy * R : NAN;
         h.k = fma(a.g2, h.r + h.F, h.F);
         const UpFactors up(k.m * (1.0 + 2.0 * amp));
         h.mul = up.mul; h.sub = up.sub;
@@ -92,20 +110,29 @@ __device__ __forceinline__ HeadCoef head_coef(const HeadArgs& a, double squares)
     return h;
 }
 // (a bound that is infinite in binary64 comes of an infinite operand: it would admit every finite claim)
-__device__ __forceinline__ float head_bound(double e, const HeadCoef& h) { return e < INFINITY ? up32g(e, h.mul, h.sub) : NAN; }
+__device__ __forceinline__ float head_bound(double e, const HeadCoef& h) {
+    float f = (float)(e * h.mul);
+    if (!(f >= 0x1p-126f && f < INFINITY)) f = e < INFINITY ? up32g(e, h.mul, h.sub) : NAN;
+    return f;
+}
 // The two elements of a pair: ha, hb are x g.
+template <bool ERRORS>
 __device__ __forceinline__ void rotate_pair(const HeadArgs& a, const HeadCoef& h, double ha, double hb, float c, float s, float tc, float ts,
                                             float& ya, float& yb, float& ta, float& tb) {
-    const double C = (double)c, S = (double)s, ec = fabs((double)tc), es = fabs((double)ts);
-    const double kc = fma(h.k, fabs(C) + ec, h.r * ec), ks = fma(h.k, fabs(S) + es, h.r * es);
-    ya = (float)(h.r * (ha * C - hb * S)); yb = (float)(h.r * (hb * C + ha * S));
+    const double C = (double)c, S = (double)s;
+    double kc = h.k * fabs(C), ks = h.k * fabs(S);
+    if constexpr (ERRORS) {
+        const double ec = fabs((double)tc), es = fabs((double)ts), more = h.k + h.r;
+        kc = fma(more, ec, kc); ks = fma(more, es, ks);
+    }
+    ya = (float)(h.r * fma(ha, C, -(hb * S))); yb = (float)(h.r * fma(hb, C, ha * S));
     ta = head_bound(fma(fabs(ha), kc, fabs(hb) * ks) + a.uflow, h);
     tb = head_bound(fma(fabs(hb), kc, fabs(ha) * ks) + a.uflow, h);
 }
-template <bool NORM>
+// (without a norm F is 0, and what is not finite has NaN for its bound)
 __device__ __forceinline__ void plain_element(const HeadCoef& h, double hx, float& y, float& t) {
     y = (float)(h.r * hx);
-    t = head_bound(NORM ? h.F * fabs(hx) : hx * 0.0, h);
+    t = head_bound(h.F * fabs(hx), h);
 }
 // Sums over TEAM lanes, in every one of them.
 template <int TEAM>
@@ -126,7 +153,7 @@ struct HeadCheck {
     __device__ __forceinline__ void put1(long i, float yv, float tv) { check_one(claimed[i], y_ref ? y_ref[i] : yv, tv, alpha, eps_rel, hist, rep, acc); }
 };
 // Any size, stride and layout: a wavefront a head, element by element, x read twice.
-template <bool NORM, class Sink>
+template <class Sink>
 __device__ __forceinline__ void head_any(const HeadArgs& a, long row, Sink& sink) {
     const int lane = threadIdx.x & (kWave - 1), half = a.rot >> 1;
     const long t = row / a.heads;
@@ -135,11 +162,11 @@ __device__ __forceinline__ void head_any(const HeadArgs& a, long row, Sink& sink
     const float* g = a.gain[head >= a.heads_q];
     const long out = t * a.ldyt + head * a.ldyh;
     double sum = 0.0;
-    if constexpr (NORM) {
+    if (a.norm) {
         for (int j = lane; j < a.d; j += kWave) sum = fma((double)x[j], (double)x[j], sum);
         sum = team_sum<64>(sum);
     }
-    const HeadCoef h = head_coef<NORM>(a, sum);
+    const HeadCoef h = head_coef(a, sum);
     auto at = [&](int j) __attribute__((always_inline)) { return (double)x[j] * (g ? (double)g[j] : 1.0); };
     const long p = a.positions ? a.positions[t] : a.npos > 0 ? t % a.npos : 0;
     const bool inside = p >= 0 && p < a.npos;
@@ -147,23 +174,21 @@ __device__ __forceinline__ void head_any(const HeadArgs& a, long row, Sink& sink
         const int ja = a.interleaved ? 2 * j : j, jb = a.interleaved ? 2 * j + 1 : j + half;
         const long e = p * half + j;
         float ya, yb, ta, tb;
-        rotate_pair(a, h, at(ja), at(jb), inside ? a.c[e] : NAN, inside ? a.s[e] : NAN, inside && a.tc ? a.tc[e] : 0.f, inside && a.ts ? a.ts[e] : 0.f, ya, yb, ta, tb);
+        rotate_pair<true>(a, h, at(ja), at(jb), inside ? a.c[e] : NAN, inside ? a.s[e] : NAN, inside && a.tc ? a.tc[e] : 0.f, inside && a.ts ? a.ts[e] : 0.f, ya, yb, ta, tb);
         sink.put1(out + ja, ya, ta);
         sink.put1(out + jb, yb, tb);
     }
     for (int j = a.rot + lane; j < a.d; j += kWave) {
         float y, tau;
-        plain_element<NORM>(h, at(j), y, tau);
+        plain_element(h, at(j), y, tau);
         sink.put1(out + j, y, tau);
     }
 }
-template <bool NORM>
 __global__ __launch_bounds__(256) void heads_any(HeadArgs a) {
     HeadStore sink{a.y, a.tau};
     const long rows = a.tokens * a.heads;
-    for (long row = (long)blockIdx.x * 4 + threadIdx.x / kWave; row < rows; row += (long)gridDim.x * 4) head_any<NORM>(a, row, sink);
+    for (long row = (long)blockIdx.x * 4 + threadIdx.x / kWave; row < rows; row += (long)gridDim.x * 4) head_any(a, row, sink);
 }
-template <bool NORM>
 __global__ __launch_bounds__(kCheckThreads) void heads_any_check(HeadArgs a, double alpha, double eps_rel, PassOut pass) {
     __shared__ unsigned int hist[kBins * kReplicas];
     __shared__ unsigned int red[kRedWords];
@@ -172,8 +197,187 @@ __global__ __launch_bounds__(kCheckThreads) void heads_any_check(HeadArgs a, dou
     HeadCheck sink{a.y_ref, a.claimed, alpha, eps_rel, hist, (int)(threadIdx.x & (kReplicas - 1)), ThreadAcc()};
     const long rows = a.tokens * a.heads;
     constexpr int WAVES = kCheckThreads / kWave;
-    for (long row = (long)blockIdx.x * WAVES + threadIdx.x / kWave; row < rows; row += (long)gridDim.x * WAVES) head_any<NORM>(a, row, sink);
+    for (long row = (long)blockIdx.x * WAVES + threadIdx.x / kWave; row < rows; row += (long)gridDim.x * WAVES) head_any(a, row, sink);
     finish_pass(hist, sink.acc, red, pass);
+}
+
+// ---- heads of whole vectors: d and rot multiples of 8, on 16-byte addresses, up to 512 elements.  TEAM lanes a head; lane j has two vectors of four elements: those from 4 j and from rot / 2 + 4 j on
+// of the rotated ones (8 j and 8 j + 4 where pairs are neighbours), with entries 4 j of the tables; from lane rot / 8 on those from 8 j and 8 j + 4 on.  A head stays in registers, so x is read once.
+// What bounds it: HBM for many heads (12 bytes an element), launches for few.
+struct HeadPlace { const float* x; const float* g; long out, table; bool inside; };
+__device__ __forceinline__ HeadPlace head_place(const HeadArgs& a, unsigned row) {
+    const unsigned t = row / (unsigned)a.heads, head = row - t * (unsigned)a.heads;
+    const long p = a.positions ? a.positions[t] : a.npos > 0x7fffffffL ? (long)t : (long)(t % (unsigned)a.npos);
+    const bool inside = p >= 0 && p < a.npos;
+    return HeadPlace{a.x + t * a.ldt + head * a.ldh, a.gain[head >= (unsigned)a.heads_q], t * a.ldyt + head * a.ldyh, inside ? p * (a.rot >> 1) : 0, inside};
+}
+template <bool INTER>
+__device__ __forceinline__ void item_offsets(const HeadArgs& a, int j, int& first, int& second) {
+    const bool apart = !INTER && 8 * j < a.rot;
+    first = apart ? 4 * j : 8 * j;
+    second = apart ? first + (a.rot >> 1) : first + 4;
+}
+__device__ __forceinline__ floatv4 vector_at(const float* p) { return *reinterpret_cast<const floatv4*>(p); }
+__device__ __forceinline__ floatv4 stream_at(const float* p) { return __builtin_nontemporal_load(reinterpret_cast<const floatv4*>(p)); }
+// One item's outputs and bounds from its elements (x) and what it looks up.
+template <bool INTER, bool ERRORS>
+__device__ __forceinline__ void head_item(const HeadArgs& a, const HeadCoef& h, const HeadPlace& at, int j, const int (&o)[2], const floatv4 (&x)[2], floatv4 (&y)[2], floatv4 (&t)[2]) {
+    double hx[2][4];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        floatv4 g = {1.f, 1.f, 1.f, 1.f};
+        if (at.g) g = vector_at(at.g + o[k]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) hx[k][e] = (double)x[k][e] * (double)g[e];
+    }
+    if (8 * j < a.rot) {
+        const floatv4 none = {0.f, 0.f, 0.f, 0.f}, bad = {NAN, NAN, NAN, NAN};
+        floatv4 c = bad, s = bad, tc = none, ts = none;
+        if (at.inside) {
+            c = vector_at(a.c + at.table + 4 * j); s = vector_at(a.s + at.table + 4 * j);
+            if (ERRORS) { tc = vector_at(a.tc + at.table + 4 * j); ts = vector_at(a.ts + at.table + 4 * j); }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            // the pair's places: element e of both vectors, or neighbours
+            const int ka = INTER ? e >> 1 : 0, ea = INTER ? 2 * (e & 1) : e, kb = INTER ? ka : 1, eb = INTER ? ea + 1 : e;
+            float ya, yb, ta, tb;
+            rotate_pair<ERRORS>(a, h, hx[ka][ea], hx[kb][eb], c[e], s[e], tc[e], ts[e], ya, yb, ta, tb);
+            y[ka][ea] = ya; y[kb][eb] = yb; t[ka][ea] = ta; t[kb][eb] = tb;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float yv, tv;
+                plain_element(h, hx[k][e], yv, tv);
+                y[k][e] = yv; t[k][e] = tv;
+            }
+    }
+}
+template <int TEAM>
+__device__ __forceinline__ HeadCoef head_chain(const HeadArgs& a, const floatv4 (&x)[2]) {
+    double sum = 0.0;
+    if (a.norm) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = fma((double)x[k][e], (double)x[k][e], sum);
+        sum = team_sum<TEAM>(sum);
+    }
+    return head_coef(a, sum);
+}
+template <int TEAM, bool INTER, bool ERRORS>
+__global__ __launch_bounds__(256) void heads_rows(HeadArgs a) {
+    constexpr int TEAMS = 256 / TEAM;
+    const int j = threadIdx.x % TEAM;
+    const bool mine = 8 * j < a.d;
+    const unsigned rows = (unsigned)(a.tokens * a.heads);
+    int o[2];
+    item_offsets<INTER>(a, j, o[0], o[1]);
+    for (unsigned row = blockIdx.x * TEAMS + threadIdx.x / TEAM; row < rows; row += gridDim.x * TEAMS) {
+        const HeadPlace at = head_place(a, row);
+        floatv4 x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        if (mine) { x[0] = stream_at(at.x + o[0]); x[1] = stream_at(at.x + o[1]); }
+        const HeadCoef h = head_chain<TEAM>(a, x);
+        if (!mine) continue;
+        floatv4 y[2], t[2];
+        head_item<INTER, ERRORS>(a, h, at, j, o, x, y, t);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (a.y) __builtin_nontemporal_store(y[k], reinterpret_cast<floatv4*>(a.y + at.out + o[k]));
+            if (a.tau) __builtin_nontemporal_store(t[k], reinterpret_cast<floatv4*>(a.tau + at.out + o[k]));
+        }
+    }
+}
+// ... checked on the spot: fours of claims settled in binary32 where that is clear (settle_four).
+struct HeadCheckArgs { HeadArgs a; double alpha, eps_rel; float quick; PassOut pass; };
+template <int TEAM, bool INTER, bool ERRORS, bool REF>
+__global__ __launch_bounds__(kCheckThreads) void heads_rows_check(HeadCheckArgs g) {
+    __shared__ unsigned int hist[kBins * kReplicas];
+    __shared__ unsigned int red[kRedWords];
+    __shared__ unsigned int largest;
+    for (int i = threadIdx.x; i < kBins * kReplicas; i += kCheckThreads) hist[i] = 0;
+    if (threadIdx.x == 0) largest = 0;
+    __syncthreads();
+    const HeadArgs& a = g.a;
+    const QuickCheck q(g.quick, g.eps_rel);
+    const bool ordinary = q.eps < INFINITY && q.alpha > 0.f;
+    ThreadAcc acc;
+    Farthest top;
+    unsigned int zeros = 0;
+    const int rep = threadIdx.x & (kReplicas - 1);
+    constexpr int TEAMS = kCheckThreads / TEAM;
+    const int j = threadIdx.x % TEAM;
+    const bool mine = 8 * j < a.d;
+    const unsigned rows = (unsigned)(a.tokens * a.heads);
+    int o[2];
+    item_offsets<INTER>(a, j, o[0], o[1]);
+    for (unsigned row = blockIdx.x * TEAMS + threadIdx.x / TEAM; row < rows; row += gridDim.x * TEAMS) {
+        const HeadPlace at = head_place(a, row);
+        floatv4 x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, c[2], r[2];
+        if (mine) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                x[k] = stream_at(at.x + o[k]);
+                c[k] = stream_at(a.claimed + at.out + o[k]);
+                if (REF) r[k] = stream_at(a.y_ref + at.out + o[k]);
+            }
+        }
+        const HeadCoef h = head_chain<TEAM>(a, x);
+        if (!mine) continue;
+        floatv4 y[2], t[2];
+        head_item<INTER, ERRORS>(a, h, at, j, o, x, y, t);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            floatv4 claim = c[k], ref = REF ? r[k] : y[k], bound = t[k];
+            const float most = fmaxf(fmaxf(fabsf(ref[0]), fabsf(ref[1])), fmaxf(fabsf(ref[2]), fabsf(ref[3])));      // (a NaN among them shows in the error)
+            if (settle_four<true, true>(claim, ref, bound, q, top, &largest, newest(&largest), ordinary && most <= 0x1p90f, acc, zeros,
+                                        [&](unsigned bin) __attribute__((always_inline)) { atomicAdd(&hist[bin * kReplicas + rep], 1u); })) continue;
+#pragma unroll 1
+            for (int e = 0; e < 4; ++e) {
+                check_one(claim[0], ref[0], bound[0], g.alpha, g.eps_rel, hist, rep, acc);
+                claim = claim.yzww; ref = ref.yzww; bound = bound.yzww;
+            }
+        }
+    }
+    if (zeros) atomicAdd(&hist[rep], zeros);
+    settled(top, g.alpha, g.eps_rel, acc);
+    __syncthreads();
+    finish_pass(hist, acc, red, g.pass);
+}
+// Lanes of a head, or 0 for the kernels of any size.  others: the claims' or outputs' addresses
+static int heads_team(const HeadArgs& a, const void* y, const void* tau) {
+    const bool vec = a.d % 8 == 0 && a.rot % 8 == 0 && a.d <= 512 && a.tokens * a.heads < (1L << 31) && aligned(a.x, 16) && aligned(a.gain[0], 16) && aligned(a.gain[1], 16) &&
+                     aligned(a.c, 16) && aligned(a.s, 16) && aligned(a.tc, 16) && aligned(a.ts, 16) && aligned(y, 16) && aligned(tau, 16) &&
+                     a.ldt % 4 == 0 && a.ldh % 4 == 0 && a.ldyt % 4 == 0 && a.ldyh % 4 == 0;
+    return !vec ? 0 : a.d <= 64 ? 8 : a.d <= 128 ? 16 : a.d <= 256 ? 32 : 64;
+}
+template <int TEAM, bool INTER, bool ERRORS>
+static void heads_launch(const HeadArgs& a, hipStream_t st) {
+    const long blocks = (a.tokens * a.heads + 256 / TEAM - 1) / (256 / TEAM);
+    hipLaunchKernelGGL((heads_rows<TEAM, INTER, ERRORS>), dim3((unsigned)(blocks < 256L * 64 ? blocks : 256L * 64)), dim3(256), 0, st, a);
+}
+template <int TEAM, bool INTER, bool ERRORS>
+static void heads_launch_check(const HeadCheckArgs& g, int nblocks, hipStream_t st) {
+    if (g.a.y_ref) hipLaunchKernelGGL((heads_rows_check<TEAM, INTER, ERRORS, true>), dim3(nblocks), dim3(kCheckThreads), 0, st, g);
+    else           hipLaunchKernelGGL((heads_rows_check<TEAM, INTER, ERRORS, false>), dim3(nblocks), dim3(kCheckThreads), 0, st, g);
+}
+// f(team, interleaved, errors) with the constants of a launch
+template <class F> static void heads_dispatch(const HeadArgs& a, int team, F&& f) {
+    using std::integral_constant;
+    using std::bool_constant;
+    auto rest = [&](auto t) {
+        if (a.interleaved) { if (a.tc) f(t, bool_constant<true>(), bool_constant<true>()); else f(t, bool_constant<true>(), bool_constant<false>()); }
+        else               { if (a.tc) f(t, bool_constant<false>(), bool_constant<true>()); else f(t, bool_constant<false>(), bool_constant<false>()); }
+    };
+    switch (team) {
+        case 8:  rest(integral_constant<int, 8>()); break;
+        case 16: rest(integral_constant<int, 16>()); break;
+        case 32: rest(integral_constant<int, 32>()); break;
+        default: rest(integral_constant<int, 64>()); break;
+    }
 }
 
 // Checks the arguments that the two entry points share and fills the kernels'.
@@ -209,7 +413,7 @@ static int heads_setup(int norm, const float* x, const float* gamma_q, const flo
     a.x = x; a.gain[0] = gamma_q; a.gain[1] = gamma_k;
     a.c = cos_table; a.s = sin_table; a.tc = tau_cos; a.ts = tau_sin; a.positions = positions;
     a.tokens = tokens; a.npos = npos; a.ldt = ldt; a.ldh = ldh; a.ldyt = ldyt; a.ldyh = ldyh;
-    a.heads_q = (int)heads_q; a.heads = (int)heads; a.d = (int)d; a.rot = (int)rot; a.interleaved = interleaved != 0;
+    a.heads_q = (int)heads_q; a.heads = (int)heads; a.d = (int)d; a.rot = (int)rot; a.interleaved = interleaved != 0; a.norm = norm == TAO_NORM_RMSNORM;
     return TAO_OK;
 }
 
@@ -243,8 +447,11 @@ int tao_bound_rope_tables(const int64_t* positions, const float* inv_freq, doubl
         a.k1[i] = widen(m * (a.m == 1.0 ? 1.0 + cu : (1.0 + u) * (1.0 + cu)));
         a.k2[i] = widen(m * (a.m == 1.0 ? cu : (1.0 + u) * cu + u));
     }
-    const long blocks = (npos * half + 255) / 256;
-    hipLaunchKernelGGL(rope_tables, dim3((unsigned)(blocks < 256L * 64 ? blocks : 256L * 64)), dim3(256), 0, (hipStream_t)stream, a);
+    const bool vec = half % 4 == 0 && aligned(cos_table, 16) && aligned(sin_table, 16) && aligned(tau_cos, 16) && aligned(tau_sin, 16);
+    const long blocks = (npos * (vec ? half / 4 : half) + 255) / 256;
+    const dim3 grid((unsigned)(blocks < 256L * 64 ? blocks : 256L * 64)), blk(256);
+    if (vec) hipLaunchKernelGGL(rope_tables<4>, grid, blk, 0, (hipStream_t)stream, a);
+    else     hipLaunchKernelGGL(rope_tables<1>, grid, blk, 0, (hipStream_t)stream, a);
     return launch_status();
 }
 
@@ -264,10 +471,12 @@ int tao_bound_norm_rope(int norm, const float* x, const float* gamma_q, const fl
     if (!aligned(y, 4) || !aligned(tau, 4)) return TAO_ERR_ALIGN;
     a.y = y; a.tau = tau;
     hipStream_t st = (hipStream_t)stream;
+    if (const int team = heads_team(a, y, tau)) {
+        heads_dispatch(a, team, [&](auto t, auto inter, auto errors) { heads_launch<t(), inter(), errors()>(a, st); });
+        return launch_status();
+    }
     const long blocks = (rows + 3) / 4;
-    const dim3 grid((unsigned)(blocks < 256L * 64 ? blocks : 256L * 64)), blk(256);
-    if (norm == TAO_NORM_RMSNORM) hipLaunchKernelGGL(heads_any<true>, grid, blk, 0, st, a);
-    else                          hipLaunchKernelGGL(heads_any<false>, grid, blk, 0, st, a);
+    hipLaunchKernelGGL(heads_any, dim3((unsigned)(blocks < 256L * 64 ? blocks : 256L * 64)), dim3(256), 0, st, a);
     return launch_status();
 }
 
@@ -292,12 +501,17 @@ int tao_bound_check_norm_rope(int norm, const float* x, const float* gamma_q, co
     a.y_ref = y_ref; a.claimed = claimed;
     hipStream_t st = (hipStream_t)stream;
     const CheckWorkspace w = carve_check_workspace(ws);
-    const long want = (rows + kCheckThreads / kWave - 1) / (kCheckThreads / kWave);
+    a.tokens = d > 0 ? tokens : 0;
+    const int team = heads_team(a, y_ref, claimed), lanes = team ? team : kWave;
+    const long want = (rows + kCheckThreads / lanes - 1) / (kCheckThreads / lanes);
     const int nblocks = (int)(want < 1 || n <= kAloneElements ? 1 : want > kMaxCheckBlocks ? kMaxCheckBlocks : want);
     const PassOut pass = pass_out(w, nblocks, n, out);
-    a.tokens = d > 0 ? tokens : 0;
-    if (norm == TAO_NORM_RMSNORM) hipLaunchKernelGGL(heads_any_check<true>, dim3(nblocks), dim3(kCheckThreads), 0, st, a, alpha, eps_rel, pass);
-    else                          hipLaunchKernelGGL(heads_any_check<false>, dim3(nblocks), dim3(kCheckThreads), 0, st, a, alpha, eps_rel, pass);
+    if (team) {
+        const HeadCheckArgs g{a, alpha, eps_rel, quick_alpha(alpha, md), pass};
+        heads_dispatch(a, team, [&](auto t, auto inter, auto errors) { heads_launch_check<t(), inter(), errors()>(g, nblocks, st); });
+    } else {
+        hipLaunchKernelGGL(heads_any_check, dim3(nblocks), dim3(kCheckThreads), 0, st, a, alpha, eps_rel, pass);
+    }
     launch_finish(w, nblocks, n, out, st);
     return launch_status();
 }

@@ -20,6 +20,7 @@ struct Int4Args {
     const float* bias;
     float* y; float* tau;
     Int4Sums* part;                                          // [part][M][N], where the reduction is cut into parts or the outputs are checked
+    long part_stride;                                        // outputs of all tokens (a launch may have some of them)
     long M, N, K, lda, ldw, ldy;
     long group; int groups;
     unsigned long per_group;                                 // column / 32 times this over 2^32 is its group (0 for one group; exact up to 2^20 columns)
@@ -78,7 +79,7 @@ __global__ __launch_bounds__(256) void int4_any(Int4Args p) {
         }
     }
 }
-// Whether a tile's sums are not exact enough, or no numbers: a size of 0 is exact (the tiles see to that).
+// Whether a tile's sums are not exact enough, or no numbers.  (A size of 0 is exact: blocks of zeros and scales of 0 add nothing to either, all others add to both.)
 __device__ __forceinline__ bool int4_open(const Int4Sums& v) { return !(v.size < INFINITY) || (v.size > 0.0 && v.err > kInt4Spare * v.size); }
 // The wavefront forms those anew, one lane's after the other's.
 __device__ __forceinline__ void int4_settle(const Int4Args& p, bool mine, int i, int j, Int4Sums& v) {
@@ -93,7 +94,7 @@ __device__ __forceinline__ void int4_settle(const Int4Args& p, bool mine, int i,
     }
 }
 
-// ---- tiles in whole numbers.  Both sums go through v_mfma_i32_32x32x32_i8, which is exact: a weight's q - z and |q - z| are bytes (z up to 127; other columns are formed
+// ---- tiles in whole numbers.  Both sums go through v_mfma_i32_16x16x64_i8, which is exact: a weight's q - z and |q - z| are bytes (z up to 127; other columns are formed
 // in binary64), and 128 activations of a token become whole numbers X = trunc(a 2^(29 - E)), E the exponent of the largest of them, in four digits of base 256 from -128 to
 // 127, of X for the output and of |X| for the bound.  A digit is a row of its own (4 t + digit), so that a lane finds a token's digits in neighbouring registers.  Sums of 128
 // products of a digit stay below 2^21; the digits are put together and scaled in binary64.
@@ -104,24 +105,26 @@ __device__ __forceinline__ void int4_settle(const Int4Args& p, bool mine, int i,
 // For ordinary tokens err is about 0.5u size (largest activation of 128 about 3.5 times the mean, dmax twice the mean of |q - z|).
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 typedef int intx4 __attribute__((ext_vector_type(4)));
-typedef int intx16 __attribute__((ext_vector_type(16)));
 typedef float floatx4_any __attribute__((ext_vector_type(4), aligned(4)));
 constexpr int kInt4Block = 128;                              // columns of a block
 constexpr int kInt4Codes = kInt4Block / 2 + 16;              // bytes of a column's codes of a block in LDS
 constexpr unsigned kInt4Row = kInt4Block + 16;               // bytes of a digit's row in LDS (16 more: the eight rows that are read at a time lie in different banks)
 
-// KW groups of NW wavefronts: a wavefront has 32 columns and the tokens of RT row tiles of OWN each; the groups share out the reduction, their sums are added in LDS.
-template <int OWN_, int RT_, int NW_, int KW_>
+// KW groups of NW wavefronts: a wavefront has CT tiles of 16 columns and the tokens in RT row tiles of four; the groups share out the reduction, their sums are added in LDS.
+// Fewer tokens are there again in the other rows; with two tokens and two tiles of columns the halves of a wavefront have a tile each for putting the digits together.
+template <int TOKENS_, int CT_, int NW_, int KW_, int WAVES_>
 struct Int4Shape {
-    static constexpr int OWN = OWN_, RT = RT_, NW = NW_, KW = KW_, THREADS = NW * KW * kWave, Q = (OWN + 1) / 2;      // Q: tokens of a lane in a row tile
-    static constexpr int TOKENS = OWN * RT, COLUMNS = 32 * NW;
-    static constexpr int BLOCKS = NW * kWave / (TOKENS * kInt4Block / 8);        // of a chunk: a lane brings eight activations
-    static constexpr int SET = TOKENS * 4 * kInt4Row, BLOCK = 2 * SET, DIGITS = BLOCKS * (BLOCK + 4 * TOKENS);     // bytes: digits of X, and of |X|; exponents behind them
-    static constexpr int CODES = 32 * kInt4Codes;            // of a wavefront
-    static constexpr int SUMS = (KW - 1) * NW * RT * Q * kWave * (int)sizeof(Int4Sums);
-    static constexpr int STAGES = KW * (DIGITS + NW * CODES), LDS = (STAGES > SUMS ? STAGES : SUMS) + 16 * ((TOKENS + 3) / 4);
-    static_assert(BLOCKS >= 1 && NW * kWave % (TOKENS * kInt4Block / 8) == 0 && DIGITS % 16 == 0, "whole blocks a chunk");
-    static_assert(LDS <= 80 * 1024, "two workgroups a compute unit");
+    static constexpr int TOKENS = TOKENS_, CT = CT_, NW = NW_, KW = KW_, WAVES = WAVES_, THREADS = NW * KW * kWave, COLUMNS = 16 * CT * NW;
+    static constexpr bool HALVES = TOKENS == 2 && CT == 2;
+    static constexpr int RT = (TOKENS + 3) / 4, ALIKE = TOKENS < 4 ? TOKENS : 4, SLOTS = HALVES ? 1 : RT * CT;       // ALIKE: tokens of a row tile, SLOTS: outputs of a lane
+    static constexpr int PIECES = TOKENS * kInt4Block / 8;   // of eight activations, in a block
+    static constexpr int BLOCKS = PIECES < NW * kWave ? NW * kWave / PIECES : 1, UNITS = BLOCKS * PIECES / (NW * kWave);      // blocks of a chunk, pieces that a lane brings
+    static constexpr int SET = TOKENS * 4 * kInt4Row, BLOCK = 2 * SET, DIGITS = BLOCKS * (BLOCK + 8 * TOKENS);     // bytes: digits of X, and of |X|; their units behind them
+    static constexpr int CODES = 16 * CT * kInt4Codes;            // of a wavefront
+    static constexpr int SUMS = KW * NW * SLOTS * kWave * (int)sizeof(Int4Sums);
+    static constexpr int STAGES = KW * (DIGITS + NW * CODES), LDS = STAGES > SUMS ? STAGES : SUMS;
+    static_assert(BLOCKS * PIECES == UNITS * NW * kWave && DIGITS % 16 == 0, "whole blocks a chunk");
+    static_assert(LDS <= 160 * 1024, "a compute unit's");
 };
 
 // 16 bytes of a row of weights from byte `at` on; bytes from `bytes` on are not touched (the activations there are 0): at the row's end its last 16 bytes, moved down.
@@ -147,22 +150,23 @@ __device__ __forceinline__ uintx4 int4_bytes(const unsigned char* __restrict__ r
     }
     return r;
 }
-// Sixteen codes less their zero point and the magnitudes of that, as bytes: of a word of eight the even ones, then the odd ones.  biased: 128 - z in every byte.  Additions, shifts and bitwise
-// operations of two operands take a SIMD half the time of the others here (2.6 cycles, 4.6).
-__device__ __forceinline__ void int4_codes(unsigned w0, unsigned w1, unsigned biased, intx4& d, intx4& m) {
-    const unsigned half[4] = {w0 & 0x0f0f0f0fu, w0 >> 4 & 0x0f0f0f0fu, w1 & 0x0f0f0f0fu, w1 >> 4 & 0x0f0f0f0fu};
+// Eight codes less their zero point and the magnitudes of that, as bytes: the even ones, then the odd ones.  biased: 127 + z in every byte, so that v = biased - q
+// has its top bit where q < z, is 127 - d elsewhere and 128 + (|d| - 1) there.  (No byte borrows from the next.  Additions, shifts and bitwise operations of two operands take a SIMD half
+// the time of the others here: 2.6 cycles, 4.6.)
+__device__ __forceinline__ void int4_codes(unsigned w, unsigned biased, int* d, int* m) {
+    const unsigned half[2] = {w & 0x0f0f0f0fu, w >> 4 & 0x0f0f0f0fu};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const unsigned v = (half[i] + biased) ^ 0x80808080u, sign = v & 0x80808080u, n = sign >> 7;       // (no byte carries into the next)
-        d[i] = (int)v;
-        m[i] = (int)((v ^ (sign | (sign - n))) + n);
+    for (int i = 0; i < 2; ++i) {
+        const unsigned v = biased - half[i], n = v >> 7 & 0x01010101u;
+        d[i] = (int)(v ^ 0x7f7f7f7fu);
+        m[i] = (int)((v ^ (n + 0x7f7f7f7fu)) + n);
     }
 }
-// Order between the lanes of a wavefront: LDS takes its accesses in order, so only the compiler has to keep it.
-__device__ __forceinline__ void wave_order() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+// A tile of 16 digits' rows by 16 columns, over 64 columns of the reduction or 32 (WORDS 2 or 1): a lane has 16 or 8 bytes of a row and of a column.
+template <int WORDS>
+__device__ __forceinline__ intx4 int4_product(const char* row, const int* d, intx4 sum) {
+    if constexpr (WORDS == 2) return __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const intx4*>(row), intx4{d[0], d[1], d[2], d[3]}, sum, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_i32_16x16x32_i8(*reinterpret_cast<const long*>(row), (long)((unsigned long)(unsigned)d[1] << 32 | (unsigned)d[0]), sum, 0, 0, 0);
 }
 // byte j of four words
 __device__ __forceinline__ void int4_transpose(const unsigned (&w)[4], unsigned (&digit)[4]) {
@@ -171,64 +175,156 @@ __device__ __forceinline__ void int4_transpose(const unsigned (&w)[4], unsigned 
     digit[0] = __builtin_amdgcn_perm(b, a, 0x05040100u); digit[1] = __builtin_amdgcn_perm(b, a, 0x07060302u);
     digit[2] = __builtin_amdgcn_perm(e, c, 0x05040100u); digit[3] = __builtin_amdgcn_perm(e, c, 0x07060302u);
 }
+// Sums over `columns` columns of a column's scale and biased zero point and a token's unit, from the products of their digits.  (The size comes without err, which the end adds.)
+__device__ __forceinline__ void int4_fold(const intx4& y, const intx4& t, float scale, unsigned biased, int columns, double unit, Int4Sums& v) {
+    const int z = (int)(biased & 255u) - 127;
+    const double by = (double)scale * unit, size = fabs(by);
+    v.sum = fma(by, fma((double)(y[2] + (y[3] << 8)), 65536.0, (double)(y[0] + (y[1] << 8))), v.sum);
+    v.size = fma(size, fma((double)(t[2] + (t[3] << 8)), 65536.0, (double)(t[0] + (t[1] << 8))), v.size);
+    v.err = fma(size, (double)(max(z, 15 - z) * columns), v.err);              // (units that truncation may have left off)
+}
+// Eight activations as digits, with the unit of their block (a row of 16 lanes has a block of a token): four times (even ones, odd ones) for X, then for |X|.
+__device__ __forceinline__ double int4_digits_of(const float (&a)[8], uint2 (&digit)[2][4]) {
+    unsigned most = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(a[i]) & 0x7fffffffu);
+    most = wave_all<0, 4>(most, [](unsigned x, unsigned y) { return max(x, y); });
+    const int E = max((int)(most >> 23), 1) - 127;
+    unsigned x[2][2][4];                                     // [set][even or odd]
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const unsigned m = (unsigned)__builtin_amdgcn_ldexpf(fabsf(a[i]), 29 - E), sign = (unsigned)(__float_as_int(a[i]) >> 31);
+        x[0][i & 1][i >> 1] = (((m ^ sign) - sign) + 0x00808080u) ^ 0x00808080u;
+        x[1][i & 1][i >> 1] = (m + 0x00808080u) ^ 0x00808080u;
+    }
+#pragma unroll
+    for (int set = 0; set < 2; ++set) {
+        unsigned even[4], odd[4];
+        int4_transpose(x[set][0], even);
+        int4_transpose(x[set][1], odd);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) digit[set][j] = make_uint2(even[j], odd[j]);
+    }
+    // (0 where all are 0, which is exact; NaN where one is not finite)
+    return most == 0 ? 0.0 : most >= 0x7f800000u ? (double)NAN : ldexp(1.0, E - 29);
+}
+// The values of four rows of 16 lanes, each to all lanes of its column.
+__device__ __forceinline__ void int4_spread(unsigned v, unsigned* to) {
+    const auto pairs = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const auto rows = __builtin_amdgcn_permlane16_swap(pairs[i], pairs[i], false, false);
+        to[2 * i] = rows[0]; to[2 * i + 1] = rows[1];
+    }
+}
+// Order between the lanes of a wavefront: LDS takes its accesses in order, so only the compiler has to keep it.
+__device__ __forceinline__ void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
-// What a lane requests of a chunk: eight activations, of each block two times 16 bytes of weights, and for its column the scales and zero points of the chunk's folds, every other one
-// (the lower half of the wavefront has the even ones).
+// The end of a workgroup: its groups' sums meet in LDS, where every wavefront takes some of the outputs: parts of the reduction, or outputs and bounds.
+template <class SH>
+__device__ __forceinline__ void int4_finish(const Int4Args& p, char* lds, const Int4Sums (&total)[SH::SLOTS], long m0, long n0) {
+    constexpr int NW = SH::NW, KW = SH::KW, SLOTS = SH::SLOTS, CT = SH::CT;
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    constexpr int OUT = SLOTS * kWave;                      // of a wavefront: [output of a lane][lane]
+    __syncthreads();
+    Int4Sums* sums = reinterpret_cast<Int4Sums*>(lds);       // [group][wavefront][output]
+#pragma unroll
+    for (int o = 0; o < SLOTS; ++o) sums[wave * OUT + o * kWave + lane] = total[o];
+    __syncthreads();
+#pragma unroll 1
+    for (int o = threadIdx.x; o < NW * OUT; o += SH::THREADS) {
+        Int4Sums v = sums[o];
+#pragma unroll
+        for (int k = 1; k < KW; ++k) {
+            const Int4Sums& other = sums[k * NW * OUT + o];
+            v.sum += other.sum; v.size += other.size; v.err += other.err;
+        }
+        v.size += v.err;
+        const int slot = o / kWave % SLOTS, q = o >> 4 & 3, t = SH::HALVES ? q & 1 : slot / CT * 4 + q, c = SH::HALVES ? q >> 1 : slot % CT;
+        const long i = m0 + t, j = n0 + (o / OUT * CT + c) * 16 + (o & 15);
+        const bool own = t < SH::TOKENS && i < p.M && j < p.N;
+        if (p.part) {
+            if (own) p.part[blockIdx.y * p.part_stride + i * p.N + j] = v;
+            continue;
+        }
+        int4_settle(p, own, (int)i, (int)j, v);
+        if (own) {
+            const long to = i * p.ldy + j;
+            float out, tau;
+            int4_values(p, j, v, out, tau);
+            if (p.y) p.y[to] = out;
+            if (p.tau) p.tau[to] = tau;
+        }
+    }
+}
+
+// What a lane requests of a chunk: eight activations, of each block CT times 16 bytes of weights, and of the scales and zero points of the chunk's folds every 4 / CT-th for one column (lanes
+// in order of tiles, then of folds).
 template <class SH, int FOLDS>
 struct Int4Chunk {
-    static constexpr int PAIRS = (SH::BLOCKS * FOLDS + 1) / 2;
-    floatx4_any a[2];
-    uintx4 raw[SH::BLOCKS][2];
-    float s[PAIRS];
-    unsigned char z[PAIRS];
+    static constexpr int FACTORS = (SH::BLOCKS * FOLDS * SH::CT + 3) / 4;
+    floatx4_any a[SH::UNITS][2];
+    uintx4 raw[SH::BLOCKS][SH::CT];
+    float s[FACTORS];
+    unsigned char z[FACTORS];
 };
 
 // Weights are read in lines: four lanes a row's 64 bytes of a block, and handed to the lanes of their columns through LDS (a load whose lanes have a row each takes the address
 // unit a cycle or two a lane: with 16 bytes a lane four times as long).
 // FOLDS: how often a block's sums are scaled (1: groups of whole blocks, 2: of halves, 4: of 32 columns)
 template <class SH, int FOLDS>
-__global__ __launch_bounds__(SH::THREADS, SH::RT == 1 ? 4 : 2) void int4_tiles(Int4Args p, Int4Grid grid) {
+__global__ __launch_bounds__(SH::THREADS, SH::WAVES) void int4_tiles(Int4Args p, Int4Grid grid) {
     extern __shared__ __align__(16) char lds[];
-    constexpr int Q = SH::Q, RT = SH::RT, NW = SH::NW, KW = SH::KW, OWN = SH::OWN, BLOCKS = SH::BLOCKS, STEPS = 4 / FOLDS;
+    constexpr int RT = SH::RT, NW = SH::NW, KW = SH::KW, SLOTS = SH::SLOTS, CT = SH::CT, TOKENS = SH::TOKENS, BLOCKS = SH::BLOCKS;
+    constexpr int STEP = FOLDS == 4 ? 32 : 64, STEPS = kInt4Block / STEP, WORDS = STEP / 32;       // columns of a matrix instruction, those of a block, words of a lane's codes for one
     using Chunk = Int4Chunk<SH, FOLDS>;
-    unsigned* marks = reinterpret_cast<unsigned*>(lds + SH::LDS - 16 * ((SH::TOKENS + 3) / 4));       // of a token: 1 not a number, 2 an activation that became 0
     // workgroups of one tile of columns on one die (workgroup modulo 8), whose cache then holds their weights
     const unsigned rest = blockIdx.x >> 3, up = grid.token_blocks == 1 ? rest : rest / grid.token_blocks, tile = up * 8 + (blockIdx.x & 7);
     if (tile >= grid.tiles) return;
-    const int lane = threadIdx.x & (kWave - 1), half = lane >> 5, col = lane & 31;
+    const int lane = threadIdx.x & (kWave - 1), half = lane >> 5, col = lane & 15, piece = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), kg = wave / NW, nw = wave % NW;
-    const long n0 = (long)tile * SH::COLUMNS + 32 * nw, m0 = (long)(rest - up * grid.token_blocks) * SH::TOKENS;
-    if (threadIdx.x < SH::TOKENS) marks[threadIdx.x] = 0;
+    const long n0 = (long)tile * SH::COLUMNS + 16 * CT * nw, m0 = (long)(rest - up * grid.token_blocks) * SH::TOKENS;
     // whole blocks are shared out among the groups of all parts
     const int blocks = grid.blocks, first = min((int)(blockIdx.y * KW + kg) * grid.share, blocks), last = min(first + grid.share, blocks);
     const int trips = (min(grid.share, blocks) + BLOCKS - 1) / BLOCKS, all = trips + (grid.tail == (int)blockIdx.y);
     auto group_of = [&](int k) __attribute__((always_inline)) { return min((int)((unsigned long)(k >> 5) * p.per_group >> 32), p.groups - 1); };
-    const unsigned char* row0 = p.W + min(n0 + lane / 4, p.N - 1) * p.ldw + lane % 4 * 16;
-    const unsigned char* row1 = p.W + min(n0 + 16 + lane / 4, p.N - 1) * p.ldw + lane % 4 * 16;
-    const long n = min(n0 + col, p.N - 1);
+    const long n0w = n0 + lane / 4;
+    const unsigned char* rows_w[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) rows_w[c] = p.W + min(n0w + 16 * c, p.N - 1) * p.ldw + lane % 4 * 16;
+    const long n = min(n0 + (lane & (16 * CT - 1)), p.N - 1);
     const float* scales = p.scale + n * p.groups;
     const bool zeroed = p.zero != nullptr;
-    const unsigned char* zeros = zeroed ? p.zero + n * p.groups : row0;      // (any bytes, where there are none: a load all the same)
+    const unsigned char* zeros = zeroed ? p.zero + n * p.groups : rows_w[0];      // (any bytes, where there are none: a load all the same)
     const int zero_step = zeroed ? 1 : 0;
-    // this lane's eight activations of a chunk
+    // this lane's pieces of eight activations of a chunk
     const int at = (nw * kWave + lane) / 16, own_block = at % BLOCKS, own_token = at / BLOCKS, unit = lane % 16;
-    const float* a_row = p.A + min(m0 + own_token, p.M - 1) * p.lda + unit * 8;
+    const float* a_row[SH::UNITS];
+#pragma unroll
+    for (int u = 0; u < SH::UNITS; ++u) a_row[u] = p.A + min(m0 + own_token + u * (NW * 4 / BLOCKS), p.M - 1) * p.lda + unit * 8;
 
-    Int4Sums total[RT][Q];
+    Int4Sums total[SLOTS];
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int q = 0; q < Q; ++q) total[r][q] = Int4Sums{0.0, 0.0, 0.0};
+    for (int o = 0; o < SLOTS; ++o) total[o] = Int4Sums{0.0, 0.0, 0.0};
     char* digits = lds + kg * SH::DIGITS;
-    const int* exps = reinterpret_cast<const int*>(digits + BLOCKS * SH::BLOCK);
+    double* units = reinterpret_cast<double*>(digits + BLOCKS * SH::BLOCK);
     char* codes = lds + KW * SH::DIGITS + wave * SH::CODES;
-    const unsigned fragment = (((lane >> 2) & (OWN - 1) & 7) * 4 + (lane & 3)) * kInt4Row + half * 16;     // of this lane's row of a row tile
+    const int row = lane & (4 * SH::ALIKE - 1), token = piece & (SH::ALIKE - 1);     // a lane's row of a row tile, its token of the products'
 
     auto meet = [&]() __attribute__((always_inline)) { if constexpr (NW > 1) __syncthreads(); else wave_order(); };
     auto factors = [&](Chunk& w, int block) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < Chunk::PAIRS; ++i) {
-            const int g0 = group_of(block * kInt4Block + 2 * i * (kInt4Block / FOLDS)), g1 = group_of(block * kInt4Block + (2 * i + 1) * (kInt4Block / FOLDS)), g = half ? g1 : g0;
+        for (int i = 0; i < Chunk::FACTORS; ++i) {
+            int g = 0;
+#pragma unroll
+            for (int f = 0; f < 4 / CT; ++f) {
+                const int of = group_of(block * kInt4Block + (i * (4 / CT) + f) * (kInt4Block / FOLDS));
+                g = f == 0 || lane >= f * 16 * CT ? of : g;
+            }
             w.s[i] = scales[g];
             w.z[i] = zeros[g * zero_step];
         }
@@ -238,159 +334,263 @@ __global__ __launch_bounds__(SH::THREADS, SH::RT == 1 ? 4 : 2) void int4_tiles(I
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i) {
             const int b = min(block + i, blocks - 1) * (kInt4Block / 2);
-            __builtin_memcpy(&w.raw[i][0], row0 + b, 16);
-            __builtin_memcpy(&w.raw[i][1], row1 + b, 16);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) __builtin_memcpy(&w.raw[i][c], rows_w[c] + b, 16);
         }
-        const float* a = a_row + min(block + own_block, blocks - 1) * kInt4Block;
-        w.a[0] = *reinterpret_cast<const floatx4_any*>(a); w.a[1] = *reinterpret_cast<const floatx4_any*>(a + 4);
+        const int first_column = min(block + own_block, blocks - 1) * kInt4Block;
+#pragma unroll
+        for (int u = 0; u < SH::UNITS; ++u) {
+            const float* a = a_row[u] + first_column;
+            w.a[u][0] = *reinterpret_cast<const floatx4_any*>(a); w.a[u][1] = *reinterpret_cast<const floatx4_any*>(a + 4);
+        }
         factors(w, block);
     };
-    // activations to digits in LDS, with the exponent of their block: a row of 16 lanes has a block of a token
-    auto write = [&](const floatx4_any (&a)[2]) __attribute__((always_inline)) {
-        unsigned most = 0, least = ~0u;
+    // activations to digits in LDS
+    auto write = [&](const floatx4_any (&a)[2], int token) __attribute__((always_inline)) {
+        const float v[8] = {a[0][0], a[0][1], a[0][2], a[0][3], a[1][0], a[1][1], a[1][2], a[1][3]};
+        uint2 digit[2][4];
+        const double by = int4_digits_of(v, digit);
+        char* to = digits + own_block * SH::BLOCK + token * 4 * kInt4Row + unit * 8;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const unsigned size = __float_as_uint(a[i >> 2][i & 3]) & 0x7fffffffu;
-            most = max(most, size); least = min(least, size - 1u);
-        }
-        most = wave_all<0, 4>(most, [](unsigned x, unsigned y) { return max(x, y); });
-        const int E = max((int)(most >> 23), 1) - 127;
-        const int unit_bits = E - 29 + 127;                  // of 2^(E - 29) as binary32 (where that is subnormal, any subnormal activation counts as gone)
-        const bool gone = least != ~0u && (unit_bits > 0 ? least + 1u < (unsigned)unit_bits << 23 : least < 0x7fffffu);
-        if (most >= 0x7f800000u || gone) atomicOr(&marks[own_token], most >= 0x7f800000u ? 1u : 2u);
-        char* to = digits + own_block * SH::BLOCK + own_token * 4 * kInt4Row + unit * 8;
-        unsigned x[2][2][4];                                 // [set][even or odd]
+        for (int set = 0; set < 2; ++set)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float v = a[i >> 2][i & 3];
-            const unsigned m = (unsigned)__builtin_amdgcn_ldexpf(fabsf(v), 29 - E), sign = (unsigned)(__float_as_int(v) >> 31);
-            x[0][i & 1][i >> 1] = (((m ^ sign) - sign) + 0x00808080u) ^ 0x00808080u;
-            x[1][i & 1][i >> 1] = (m + 0x00808080u) ^ 0x00808080u;
-        }
-#pragma unroll
-        for (int set = 0; set < 2; ++set) {
-            unsigned even[4], odd[4];
-            int4_transpose(x[set][0], even);
-            int4_transpose(x[set][1], odd);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) *reinterpret_cast<uint2*>(to + set * SH::SET + j * kInt4Row) = make_uint2(even[j], odd[j]);
-        }
-        if (unit == 0) reinterpret_cast<int*>(digits + BLOCKS * SH::BLOCK)[own_block * SH::TOKENS + own_token] = E - 29;
+            for (int j = 0; j < 4; ++j) *reinterpret_cast<uint2*>(to + set * SH::SET + j * kInt4Row) = digit[set][j];
+        if (unit == 0) units[own_block * SH::TOKENS + token] = by;
     };
-    // block i of the chunk, whose folds have these scales and biases
-    auto multiply = [&](const uintx4 (&raw)[2], int i, const float* scale, const unsigned* biased) __attribute__((always_inline)) {
+    // block i of the chunk
+    auto multiply = [&](const uintx4 (&raw)[CT], int i, const unsigned (&s_all)[4 * Chunk::FACTORS], const unsigned (&z_all)[4 * Chunk::FACTORS]) __attribute__((always_inline)) {
         wave_order();
         char* to = codes + lane / 4 * kInt4Codes + lane % 4 * 16;
-        *reinterpret_cast<uintx4*>(to) = raw[0];
-        *reinterpret_cast<uintx4*>(to + 16 * kInt4Codes) = raw[1];
+#pragma unroll
+        for (int c = 0; c < CT; ++c) *reinterpret_cast<uintx4*>(to + c * 16 * kInt4Codes) = raw[c];
         wave_order();
-        const char* from = codes + col * kInt4Codes + half * 8;
-        uint2 word[4];
+        const char* from = codes + col * kInt4Codes + piece * (4 * WORDS);
+        const char* rows = digits + i * SH::BLOCK + row * kInt4Row + piece * (8 * WORDS);
+        intx4 y[RT][CT], t[RT][CT];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) word[s] = *reinterpret_cast<const uint2*>(from + 16 * s);
-        intx16 y[RT], t[RT];
+        for (int s = 0; s < STEPS; ++s) {
+            const int f = (i * FOLDS + s * FOLDS / STEPS) * CT;
+            const bool fresh = s % (STEPS / FOLDS) == 0;
+            int d[CT][2 * WORDS], m[CT][2 * WORDS];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int f = s / STEPS;
-            intx4 d, m;
-            int4_codes(word[s].x, word[s].y, biased[f], d, m);
+            for (int c = 0; c < CT; ++c)
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                const char* row = digits + i * SH::BLOCK + fragment + r * OWN * 4 * kInt4Row + s * 32;
-                const intx16 none = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-                y[r] = __builtin_amdgcn_mfma_i32_32x32x32_i8(*reinterpret_cast<const intx4*>(row), d, s % STEPS ? y[r] : none, 0, 0, 0);
-                t[r] = __builtin_amdgcn_mfma_i32_32x32x32_i8(*reinterpret_cast<const intx4*>(row + SH::SET), m, s % STEPS ? t[r] : none, 0, 0, 0);
-            }
-            if (s % STEPS == STEPS - 1) {
-                const int z = 128 - (int)(biased[f] & 255u), left = max(z, 15 - z) * (32 * STEPS);      // units that truncation may have left off
-                const double wide = (double)scale[f];
+                for (int w = 0; w < WORDS; ++w)
+                    int4_codes(*reinterpret_cast<const unsigned*>(from + c * 16 * kInt4Codes + s * (STEP / 2) + 4 * w), z_all[f + c], d[c] + 2 * w, m[c] + 2 * w);
 #pragma unroll
-                for (int r = 0; r < RT; ++r)
+            for (int r = 0; r < RT; ++r)
 #pragma unroll
-                    for (int q = 0; q < Q; ++q) {
-                        Int4Sums& v = total[r][q];
-                        const double by = ldexp(wide, exps[i * SH::TOKENS + r * OWN + (OWN > 1 ? 2 * q + half : 0)]), size = fabs(by);
-                        const int e = 4 * q;
-                        v.sum = fma(by, fma((double)(y[r][e + 2] + (y[r][e + 3] << 8)), 65536.0, (double)(y[r][e] + (y[r][e + 1] << 8))), v.sum);
-                        v.size = fma(size, fma((double)(t[r][e + 2] + (t[r][e + 3] << 8)), 65536.0, (double)(t[r][e] + (t[r][e + 1] << 8) + left)), v.size);
-                        v.err = fma(size, (double)left, v.err);
-                    }
+                for (int c = 0; c < CT; ++c) {
+                    const intx4 none = {0, 0, 0, 0};
+                    y[r][c] = int4_product<WORDS>(rows + r * 16 * kInt4Row + s * STEP, d[c], fresh ? none : y[r][c]);
+                    t[r][c] = int4_product<WORDS>(rows + r * 16 * kInt4Row + s * STEP + SH::SET, m[c], fresh ? none : t[r][c]);
+                }
+            if ((s + 1) % (STEPS / FOLDS) != 0) continue;
+#pragma unroll
+            for (int o = 0; o < SLOTS; ++o) {
+                const int r = o / CT, c = o % CT;
+                intx4 yo = y[r][c], to = t[r][c];
+                unsigned scale = s_all[f + c], biased = z_all[f + c];
+                if constexpr (SH::HALVES) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { yo[e] = half ? y[0][1][e] : yo[e]; to[e] = half ? t[0][1][e] : to[e]; }
+                    scale = half ? s_all[f + 1] : scale; biased = half ? z_all[f + 1] : biased;
+                }
+                int4_fold(yo, to, __uint_as_float(scale), biased, kInt4Block / FOLDS, units[i * TOKENS + r * 4 + token], total[o]);
             }
         }
     };
     Chunk now, next;
     if (trips > 0) request(now, first);
-    __syncthreads();                                         // (the marks)
     for (int trip = 0; trip < all; ++trip) {
         const bool odd = trip == trips;                      // the last block, which is not whole, goes to the last group
         const int block = odd ? blocks : first + trip * BLOCKS, limit = !odd ? last : kg == KW - 1 ? blocks + 1 : 0;
         if (odd) {                                           // (columns that do not exist have activations of 0)
             const int columns = own_block == 0 ? (int)(p.K % kInt4Block) - unit * 8 : 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) now.a[i >> 2][i & 3] = i < columns ? a_row[(long)blocks * kInt4Block + i] : 0.f;
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int u = 0; u < SH::UNITS; ++u) now.a[u][i >> 2][i & 3] = i < columns ? a_row[u][(long)blocks * kInt4Block + i] : 0.f;
             const int from = blocks * (kInt4Block / 2) + lane % 4 * 16, bytes = (int)((p.K + 1) / 2);
-            now.raw[0][0] = int4_bytes(row0 - lane % 4 * 16, from, bytes);
-            now.raw[0][1] = int4_bytes(row1 - lane % 4 * 16, from, bytes);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) now.raw[0][c] = int4_bytes(rows_w[c] - lane % 4 * 16, from, bytes);
             factors(now, block);
         } else if (trip + 1 < trips) {
             request(next, block + BLOCKS);
         }
         meet();
-        write(now.a);
+#pragma unroll
+        for (int u = 0; u < SH::UNITS; ++u) write(now.a[u], own_token + u * (NW * 4 / BLOCKS));
         meet();
         // (a column whose zero point does not fit the bytes gets NaN: its outputs are then formed in binary64)
-        float scale[2 * Chunk::PAIRS];
-        unsigned biased[2 * Chunk::PAIRS];
+        unsigned scale[4 * Chunk::FACTORS], biased[4 * Chunk::FACTORS];          // [fold][tile of columns]
 #pragma unroll
-        for (int i = 0; i < Chunk::PAIRS; ++i) {
-            const unsigned z = zeroed ? now.z[i] : 8u, b = (128u - min(z, 127u)) * 0x01010101u, s = z > 127u ? 0x7fc00000u : __float_as_uint(now.s[i]);
-            const auto bs = __builtin_amdgcn_permlane32_swap(b, b, false, false), ss = __builtin_amdgcn_permlane32_swap(s, s, false, false);
-            biased[2 * i] = bs[0]; biased[2 * i + 1] = bs[1];
-            scale[2 * i] = __uint_as_float(ss[0]); scale[2 * i + 1] = __uint_as_float(ss[1]);
+        for (int i = 0; i < Chunk::FACTORS; ++i) {
+            const unsigned z = zeroed ? now.z[i] : 8u;
+            int4_spread(__builtin_amdgcn_perm(0u, 127u + min(z, 127u), 0u), biased + 4 * i);
+            int4_spread(z > 127u ? 0x7fc00000u : __float_as_uint(now.s[i]), scale + 4 * i);
         }
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i)
-            if (block + i < limit) multiply(now.raw[i], i, scale + i * FOLDS, biased + i * FOLDS);
+            if (block + i < limit) multiply(now.raw[i], i, scale, biased);
         now = next;
     }
-    __syncthreads();                                         // (the stages' memory is that of the sums)
-    Int4Sums* others = reinterpret_cast<Int4Sums*>(lds);     // [group - 1][wavefront][output of a lane][lane]
-    if (kg > 0) {
+    int4_finish<SH>(p, lds, total, m0, (long)tile * SH::COLUMNS);
+}
+// ---- more tokens: digits are formed once, by a kernel of their own, and lie in the workspace as the products want them: of four tokens and a block
+// X, then |X|, of each the steps' 16 rows in the order of the lanes (loads whose lanes have a row each take the address unit a cycle or two a lane: 49 us for 16 x 12288 x 4096).
+constexpr int kInt4Tile = 2 * 16 * kInt4Block;               // bytes
+__global__ __launch_bounds__(256) void int4_digits(Int4Args p, char* digits, double* units, int blocks, long pieces, int step) {
+    const long at = (long)blockIdx.x * 256 + threadIdx.x;
+    if (at >= pieces) return;
+    const int unit = (int)(at & 15), token = (int)(at >> 4 & 3);
+    const long tile = at >> 6, tokens = tile / blocks, block = tile - tokens * blocks, i = tokens * 4 + token, k = block * kInt4Block + unit * 8;
+    float a[8];
+    const float* from = p.A + i * p.lda + k;
+    if (i < p.M && k + 8 <= p.K) {
+        const floatx4_any lo = *reinterpret_cast<const floatx4_any*>(from), hi = *reinterpret_cast<const floatx4_any*>(from + 4);
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
+        for (int e = 0; e < 4; ++e) { a[e] = lo[e]; a[4 + e] = hi[e]; }
+    } else {
 #pragma unroll
-            for (int q = 0; q < Q; ++q) others[(((kg - 1) * NW + nw) * RT * Q + r * Q + q) * kWave + lane] = total[r][q];
+        for (int e = 0; e < 8; ++e) a[e] = i < p.M && k + e < p.K ? from[e] : 0.f;
     }
-    __syncthreads();
-    if (kg > 0) return;
+    uint2 digit[2][4];
+    const double by = int4_digits_of(a, digit);
+    const int lane = step == 64 ? (unit & 7) >> 1 : unit & 3, wide = step / 4, s = unit * 8 / step;             // (of row 0: the wavefront's row of 16 lanes)
+    char* to = digits + tile * kInt4Tile + s * 16 * step + (lane * 16 + token * 4) * wide + (step == 64 ? (unit & 1) * 8 : 0);
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
+    for (int set = 0; set < 2; ++set)
 #pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            Int4Sums v = total[r][q];
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<uint2*>(to + set * 16 * kInt4Block + j * wide) = digit[set][j];
+    if (unit == 0) units[tile * 4 + token] = by;
+}
+template <int TOKENS_, int NW_, int KW_, int WAVES_>
+struct Int4Rows {
+    static constexpr int TOKENS = TOKENS_, CT = 2, NW = NW_, KW = KW_, WAVES = WAVES_, THREADS = NW * KW * kWave, COLUMNS = 16 * CT * NW, RT = TOKENS / 4, SLOTS = RT * CT;
+    static constexpr bool HALVES = false;
+    static constexpr int DIGITS = RT * kInt4Tile, COPIES = DIGITS / 1024 / NW;   // bytes of a block's digits; pieces of 1024 of them that a wavefront brings
+    static constexpr int CODES = 16 * CT * kInt4Codes, STAGES = KW * 2 * DIGITS + NW * KW * CODES;
+    static constexpr int SUMS = KW * NW * SLOTS * kWave * (int)sizeof(Int4Sums), LDS = STAGES > SUMS ? STAGES : SUMS;
+    static_assert(COPIES * NW * 1024 == DIGITS && LDS <= 160 * 1024, "whole pieces; a compute unit's");
+};
+template <class SH, int FOLDS>
+__global__ __launch_bounds__(SH::THREADS, SH::WAVES) void int4_rows(Int4Args p, Int4Grid grid, const char* __restrict__ digits, const double* __restrict__ units) {
+    extern __shared__ __align__(16) char lds[];
+    constexpr int RT = SH::RT, CT = SH::CT, NW = SH::NW, KW = SH::KW, SLOTS = SH::SLOTS;
+    constexpr int STEP = FOLDS == 4 ? 32 : 64, STEPS = kInt4Block / STEP, WORDS = STEP / 32, FACTORS = (FOLDS * CT + 3) / 4;
+    const unsigned rest = blockIdx.x >> 3, up = grid.token_blocks == 1 ? rest : rest / grid.token_blocks, tile = up * 8 + (blockIdx.x & 7);
+    if (tile >= grid.tiles) return;
+    const int lane = threadIdx.x & (kWave - 1), col = lane & 15, piece = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), kg = wave / NW, nw = wave % NW;
+    const long n0 = (long)tile * SH::COLUMNS + 16 * CT * nw, m0 = (long)(rest - up * grid.token_blocks) * SH::TOKENS;
+    const int blocks = grid.blocks, every = blocks + (p.K % kInt4Block != 0);
+    const int first = min((int)(blockIdx.y * KW + kg) * grid.share, blocks), last = min(first + grid.share, blocks);
+    const int trips = min(grid.share, blocks), all = trips + (grid.tail == (int)blockIdx.y);       // (every group's, as they meet at barriers)
+    // the group's block of a trip, or -1: the last one, which is not whole, goes to the last group
+    auto block_of = [&](int trip) __attribute__((always_inline)) {
+        return trip < trips ? (first + trip < last ? first + trip : -1) : trip < all && kg == KW - 1 ? blocks : -1;
+    };
+    auto group_of = [&](int k) __attribute__((always_inline)) { return min((int)((unsigned long)(k >> 5) * p.per_group >> 32), p.groups - 1); };
+    const unsigned char* rows_w[CT];
 #pragma unroll
-            for (int k = 1; k < KW; ++k) {
-                const Int4Sums& o = others[(((k - 1) * NW + nw) * RT * Q + r * Q + q) * kWave + lane];
-                v.sum += o.sum; v.size += o.size; v.err += o.err;
-            }
-            const int t = r * OWN + 2 * q + half;
-            const unsigned mark = marks[min(t, SH::TOKENS - 1)];
-            if (mark & 1u) v.size = NAN;
-            if (mark & 2u) v.size += 0x1p-900;               // (not the 0 that int4_open takes for exact)
-            const bool own = (OWN > 1 || half == 0) && m0 + t < p.M && n0 + col < p.N;
-            if (p.part) {
-                if (own) p.part[((long)blockIdx.y * p.M + m0 + t) * p.N + n0 + col] = v;
-                continue;
-            }
-            int4_settle(p, own, (int)m0 + t, (int)n0 + col, v);
-            if (own) {
-                const long to = (m0 + t) * p.ldy + n0 + col;
-                float out, tau;
-                int4_values(p, n0 + col, v, out, tau);
-                if (p.y) p.y[to] = out;
-                if (p.tau) p.tau[to] = tau;
-            }
+    for (int c = 0; c < CT; ++c) rows_w[c] = p.W + min(n0 + lane / 4 + 16 * c, p.N - 1) * p.ldw + lane % 4 * 16;
+    const long n = min(n0 + (lane & 31), p.N - 1);
+    const float* scales = p.scale + n * p.groups;
+    const bool zeroed = p.zero != nullptr;
+    const unsigned char* zeros = zeroed ? p.zero + n * p.groups : rows_w[0];
+    const int zero_step = zeroed ? 1 : 0;
+    const char* mine = digits + m0 / 4 * every * kInt4Tile;
+    const double* tokens = units + m0 / 4 * every * 4 + piece;
+
+    Int4Sums total[SLOTS];
+#pragma unroll
+    for (int o = 0; o < SLOTS; ++o) total[o] = Int4Sums{0.0, 0.0, 0.0};
+    char* stages = lds + kg * 2 * SH::DIGITS;
+    char* codes = lds + KW * 2 * SH::DIGITS + wave * SH::CODES;
+    const unsigned stages_at = __builtin_amdgcn_readfirstlane((unsigned)(unsigned long)(__attribute__((address_space(3))) char*)stages);
+    uintx4 raw[CT];
+    float s_own[FACTORS];
+    unsigned char z_own[FACTORS];
+    double unit[RT];
+    auto factors = [&](int block) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < FACTORS; ++i) {
+            const int g0 = group_of(block * kInt4Block + 2 * i * (kInt4Block / FOLDS)), g1 = group_of(block * kInt4Block + (2 * i + 1) * (kInt4Block / FOLDS)), g = lane >= 32 ? g1 : g0;
+            s_own[i] = scales[g];
+            z_own[i] = zeros[g * zero_step];
         }
+    };
+    // what a block needs, requested a block ahead and waited for together: digits to LDS, the rest to registers
+    auto fetch = [&](int block, int stage) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < SH::COPIES; ++i) {
+            const int at = nw * SH::COPIES + i, r = at / (kInt4Tile / 1024), part = at % (kInt4Tile / 1024);
+            const char* from = mine + ((long)r * every + block) * kInt4Tile + part * 1024;
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(stages_at + stage * SH::DIGITS + at * 1024), "v"(lane * 16), "s"(from) : "memory");
+        }
+#pragma unroll
+        for (int c = 0; c < CT; ++c) __builtin_memcpy(&raw[c], rows_w[c] + (long)min(block, blocks - 1) * (kInt4Block / 2), 16);
+        factors(block);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) unit[r] = tokens[((long)r * every + block) * 4];
+    };
+    int block = block_of(0);
+    if (block >= 0) fetch(block, 0);
+    for (int trip = 0; trip < all; ++trip) {
+        const int after = block_of(trip + 1);
+        if (block == blocks) {
+            const int from = blocks * (kInt4Block / 2) + lane % 4 * 16, bytes = (int)((p.K + 1) / 2);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) raw[c] = int4_bytes(rows_w[c] - lane % 4 * 16, from, bytes);
+        }
+        __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0)
+        unsigned scale[4 * FACTORS], biased[4 * FACTORS];    // [fold][tile of columns]
+#pragma unroll
+        for (int i = 0; i < FACTORS; ++i) {
+            const unsigned z = zeroed ? z_own[i] : 8u;
+            int4_spread(__builtin_amdgcn_perm(0u, 127u + min(z, 127u), 0u), biased + 4 * i);
+            int4_spread(z > 127u ? 0x7fc00000u : __float_as_uint(s_own[i]), scale + 4 * i);
+        }
+        double by[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) by[r] = unit[r];
+        char* to = codes + lane / 4 * kInt4Codes + lane % 4 * 16;
+#pragma unroll
+        for (int c = 0; c < CT; ++c) *reinterpret_cast<uintx4*>(to + c * 16 * kInt4Codes) = raw[c];
+        __syncthreads();                                     // (the group's digits are there, and nobody reads the stage before any more)
+        if (after >= 0) fetch(after, (trip + 1) & 1);
+        const int now = block;
+        block = after;
+        if (now < 0) continue;
+        const char* rows = stages + (trip & 1) * SH::DIGITS + lane * (8 * WORDS);
+        const char* from = codes + col * kInt4Codes + piece * (4 * WORDS);
+        intx4 y[RT][CT], t[RT][CT];
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            const int f = s * FOLDS / STEPS * CT;
+            const bool fresh = s % (STEPS / FOLDS) == 0;
+            int d[CT][2 * WORDS], m[CT][2 * WORDS];
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int w = 0; w < WORDS; ++w)
+                    int4_codes(*reinterpret_cast<const unsigned*>(from + c * 16 * kInt4Codes + s * (STEP / 2) + 4 * w), biased[f + c], d[c] + 2 * w, m[c] + 2 * w);
+            const intx4 none = {0, 0, 0, 0};
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    y[r][c] = int4_product<WORDS>(rows + r * kInt4Tile + s * 16 * STEP, d[c], fresh ? none : y[r][c]);
+                    t[r][c] = int4_product<WORDS>(rows + r * kInt4Tile + 16 * kInt4Block + s * 16 * STEP, m[c], fresh ? none : t[r][c]);
+                }
+            if ((s + 1) % (STEPS / FOLDS) != 0) continue;
+#pragma unroll
+            for (int o = 0; o < SLOTS; ++o)
+                int4_fold(y[o / CT][o % CT], t[o / CT][o % CT], __uint_as_float(scale[f + o % CT]), biased[f + o % CT], kInt4Block / FOLDS, by[o / CT], total[o]);
+        }
+    }
+    int4_finish<SH>(p, lds, total, m0, (long)tile * SH::COLUMNS);
 }
 // The parts of the reduction added up, in order: outputs and bounds from them.
 __device__ __forceinline__ void int4_joined(const Int4Args& p, int parts, bool own, long at, int& i, int& j, Int4Sums& v) {
@@ -465,7 +665,7 @@ static int int4_setup(const float* A, const uint8_t* W, const float* scale, cons
     }
     Int4Args& p = *out;
     p.A = A; p.W = W; p.scale = scale; p.zero = zero; p.bias = bias; p.y = nullptr; p.tau = nullptr; p.part = nullptr;
-    p.M = M; p.N = N; p.K = K; p.lda = lda; p.ldw = ldw; p.ldy = ldy;
+    p.part_stride = M * N; p.M = M; p.N = N; p.K = K; p.lda = lda; p.ldw = ldw; p.ldy = ldy;
     p.group = group < K || K == 0 ? group : K + (K & 1);     // (one group: its end at an even column)
     p.groups = (int)((K + p.group - 1) / p.group);
     p.per_group = p.groups > 1 ? (1UL << 32) / (unsigned long)(p.group / 32) + 1 : 0;
@@ -474,56 +674,104 @@ static int int4_setup(const float* A, const uint8_t* W, const float* scale, cons
     p.terms = (double)steps;
     return TAO_OK;
 }
-// What a launch does: tiles of up to `tokens` tokens in `parts` parts of the reduction, or the kernel of any size (tokens 0).
-struct Int4Plan { int tokens, parts; };
+// What a call launches: tiles of up to `tokens` tokens in `parts` parts of the reduction (tokens 0: the kernel of any size), with digits formed beforehand for `slab` tokens at a time
+// (0: by the tiles themselves), and of those whether a workgroup has one wavefront's columns or two.
+struct Int4Plan { int tokens, parts; long slab; int nw, kw; };
+constexpr long kInt4Slab = 64L << 20;                        // bytes of digits that are kept at a time (a few tokens', where those are more)
 static Int4Plan int4_plan(long M, long N, long K, bool terms) {
     // (short reductions: a wavefront's lanes are hardly used, and what truncation leaves off would show next to the few roundings that the bound holds)
-    if (K <= 32 || K > (1L << 20) || terms) return {0, 1};
-    const int tokens = M <= 2 ? 2 : M <= 4 ? 4 : M <= 8 ? 8 : 16;
+    if (K <= 32 || K > (1L << 20) || terms) return {0, 1, 0, 1, 1};
+    // (four and fewer tokens, and small products of up to eight: the digits' own launch costs more than forming them again for every tile)
+    const bool rows = K >= kInt4Block && (M > 8 || (M > 4 && N * K >= 1L << 25));
+    const long sixteens = (M + 15) / 16;
+    const int tokens = M <= 1 ? 1 : M <= 2 ? 2 : M <= 4 ? 4 : M <= 8 || !rows || (N + 63) / 64 * sixteens < 160 ? 8 : 16;
+    const long token_blocks = (M + tokens - 1) / tokens, wide = (N + 127) / 128 * token_blocks;
+    // columns and groups of a workgroup: the more columns, the fewer read the same digits; four wavefronts where there are two such workgroups a compute unit
+    const int nw = !rows ? 1 : tokens == 16 && wide >= 256 ? 4 : 2, kw = !rows ? (tokens <= 4 ? 8 : 4) : nw == 2 ? 4 : wide >= 512 ? 1 : 2;
     // parts until there is a workgroup for each of the chip's 256 compute units (written out: the workspace's size is asked for where there may be no device), of four blocks a group
     // at least, as their sums take a launch more
-    const long columns = tokens <= 4 ? 32 : tokens == 8 ? 64 : 128, groups = tokens <= 4 ? 8 : tokens == 8 ? 4 : 2;
-    const long workgroups = (N + columns - 1) / columns * ((M + tokens - 1) / tokens), most = K / kInt4Block / (4 * groups);
+    const long columns = tokens <= 4 ? 16 : 32 * nw;
+    const long workgroups = (N + columns - 1) / columns * token_blocks, most = K / kInt4Block / (4 * kw);
     const long parts = std::max(1L, std::min(256 / std::max(workgroups, 1L), most));
-    return {tokens, (int)parts};
+    const long fit = kInt4Slab / ((K + kInt4Block - 1) / kInt4Block * kInt4Block * 8) / tokens;
+    return {tokens, (int)parts, rows ? tokens * std::min(std::max(fit, 1L), token_blocks) : 0, nw, kw};
 }
-template <class SH, int FOLDS>
-static int int4_launch_tiles(const Int4Args& p, int parts, hipStream_t st) {
+static size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+static size_t part_bytes(long M, long N, const Int4Plan& plan) { return plan.parts > 1 ? padded((size_t)plan.parts * (size_t)(M * N) * sizeof(Int4Sums)) : 0; }
+// Digits, then units.
+static size_t digit_bytes(long K, const Int4Plan& plan) { return (size_t)(plan.slab / 4 * ((K + kInt4Block - 1) / kInt4Block)) * kInt4Tile; }
+static size_t unit_bytes(long K, const Int4Plan& plan) { return padded((size_t)(plan.slab * ((K + kInt4Block - 1) / kInt4Block)) * sizeof(double)); }
+// Shape SH of a kernel for groups of whole blocks, of halves, or of 32 columns and their multiples.
+template <class SH, class... Rest>
+static int int4_launch_shape(void (*whole)(Int4Args, Int4Grid, Rest...), void (*halves)(Int4Args, Int4Grid, Rest...), void (*quarters)(Int4Args, Int4Grid, Rest...),
+                             const Int4Args& p, int parts, hipStream_t st, Rest... rest) {
     const long tiles = (p.N + SH::COLUMNS - 1) / SH::COLUMNS, token_blocks = (p.M + SH::TOKENS - 1) / SH::TOKENS;
     const __int128 grid = (__int128)((tiles + 7) / 8 * 8) * token_blocks;
     if (grid >= (1L << 31)) return TAO_ERR_SHAPE;
     static OncePerDevice once;
-    const hipError_t e = once.run([] { return hipFuncSetAttribute(reinterpret_cast<const void*>(int4_tiles<SH, FOLDS>), hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS); });
+    const hipError_t e = once.run([&] {
+        for (const auto kernel : {whole, halves, quarters}) {
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS);
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    });
     if (e != hipSuccess) { g_last_hip_error = (int)e; return TAO_ERR_LAUNCH; }
     const long blocks = p.K / kInt4Block, sharers = (long)SH::KW * parts;
     const Int4Grid g{(unsigned)tiles, (unsigned)token_blocks, (int)blocks, (int)((blocks + sharers - 1) / sharers), p.K % kInt4Block ? parts - 1 : -1};
-    hipLaunchKernelGGL((int4_tiles<SH, FOLDS>), dim3((unsigned)grid, (unsigned)parts), dim3(SH::THREADS), SH::LDS, st, p, g);
+    const auto kernel = p.groups <= 1 || p.group % kInt4Block == 0 ? whole : p.group % (kInt4Block / 2) == 0 ? halves : quarters;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid, (unsigned)parts), dim3(SH::THREADS), SH::LDS, st, p, g, rest...);
     return launch_status();
 }
 template <class SH>
 static int int4_launch_tiles(const Int4Args& p, int parts, hipStream_t st) {
-    if (p.groups <= 1 || p.group % kInt4Block == 0) return int4_launch_tiles<SH, 1>(p, parts, st);
-    if (p.group % (kInt4Block / 2) == 0) return int4_launch_tiles<SH, 2>(p, parts, st);
-    return int4_launch_tiles<SH, 4>(p, parts, st);
+    return int4_launch_shape<SH>(int4_tiles<SH, 1>, int4_tiles<SH, 2>, int4_tiles<SH, 4>, p, parts, st);
+}
+template <class SH>
+static int int4_launch_rows(const Int4Args& p, int parts, const char* digits, const double* units, hipStream_t st) {
+    return int4_launch_shape<SH>(int4_rows<SH, 1>, int4_rows<SH, 2>, int4_rows<SH, 4>, p, parts, st, digits, units);
+}
+// Slab by slab: digits, then the tiles that read them.
+static int int4_launch_slabs(const Int4Args& p, const Int4Plan& plan, char* ws, hipStream_t st) {
+    const long blocks = (p.K + kInt4Block - 1) / kInt4Block;
+    const int step = p.groups <= 1 || p.group % 64 == 0 ? 64 : 32;         // columns of the products' steps
+    double* units = reinterpret_cast<double*>(ws + digit_bytes(p.K, plan));
+    for (long m = 0; m < p.M; m += plan.slab) {
+        Int4Args q = p;
+        q.M = std::min(plan.slab, p.M - m);
+        q.A += m * p.lda;
+        if (q.y) q.y += m * p.ldy;
+        if (q.tau) q.tau += m * p.ldy;
+        if (q.part) q.part += m * p.N;
+        const long pieces = (q.M + plan.tokens - 1) / plan.tokens * plan.tokens * blocks * 16;
+        hipLaunchKernelGGL(int4_digits, dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, st, q, ws, units, (int)blocks, pieces, step);
+        int rc = launch_status();
+        if (rc != TAO_OK) return rc;
+        if (plan.tokens == 8) rc = int4_launch_rows<Int4Rows<8, 2, 4, 2>>(q, plan.parts, ws, units, st);
+        else if (plan.nw == 2) rc = int4_launch_rows<Int4Rows<16, 2, 4, 2>>(q, plan.parts, ws, units, st);
+        else if (plan.kw == 2) rc = int4_launch_rows<Int4Rows<16, 4, 2, 2>>(q, plan.parts, ws, units, st);
+        else rc = int4_launch_rows<Int4Rows<16, 4, 1, 2>>(q, plan.parts, ws, units, st);
+        if (rc != TAO_OK) return rc;
+    }
+    return TAO_OK;
 }
 // The sums (p.part) or, with one part, the outputs.
-static int int4_launch(const Int4Args& p, const Int4Plan& plan, hipStream_t st) {
+static int int4_launch(const Int4Args& p, const Int4Plan& plan, char* ws, hipStream_t st) {
+    if (plan.slab) return int4_launch_slabs(p, plan, ws, st);
     switch (plan.tokens) {
-        case 2:  return int4_launch_tiles<Int4Shape<2, 1, 1, 8>>(p, plan.parts, st);
-        case 4:  return int4_launch_tiles<Int4Shape<4, 1, 1, 8>>(p, plan.parts, st);
-        case 8:  return int4_launch_tiles<Int4Shape<8, 1, 2, 4>>(p, plan.parts, st);
-        case 16: return int4_launch_tiles<Int4Shape<8, 2, 4, 2>>(p, plan.parts, st);
+        case 1:  return int4_launch_tiles<Int4Shape<1, 1, 1, 8, 2>>(p, plan.parts, st);
+        case 2:  return int4_launch_tiles<Int4Shape<2, 1, 1, 8, 4>>(p, plan.parts, st);
+        case 4:  return int4_launch_tiles<Int4Shape<4, 1, 1, 8, 4>>(p, plan.parts, st);
+        case 8:  return int4_launch_tiles<Int4Shape<8, 2, 1, 4, 2>>(p, plan.parts, st);
     }
     const long blocks = (p.M * p.N + 3) / 4;
     hipLaunchKernelGGL(int4_any, dim3((unsigned)(blocks < 256L * 256 ? blocks : 256L * 256)), dim3(256), 0, st, p);
     return launch_status();
 }
-static size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 static bool int4_sizes_ok(long M, long N, long K) {
     const long most = 1L << 31;
     return M >= 0 && N >= 0 && K >= 0 && M < most && N < most && K < most && (__int128)M * N < ((__int128)1 << 36);
 }
-static size_t part_bytes(long M, long N, int parts) { return padded((size_t)parts * (size_t)(M * N) * sizeof(Int4Sums)); }
 
 }  // namespace tao
 
@@ -533,13 +781,14 @@ size_t tao_linear_int4_workspace_bytes(long M, long N, long K) {
     using namespace tao;
     if (!int4_sizes_ok(M, N, K)) return 0;
     const Int4Plan plan = int4_plan(M, N, K, false);
-    return plan.parts > 1 ? part_bytes(M, N, plan.parts) : 0;
+    return part_bytes(M, N, plan) + digit_bytes(K, plan) + unit_bytes(K, plan);
 }
 
 size_t tao_bound_check_linear_int4_workspace_bytes(long M, long N, long K) {
     using namespace tao;
     if (!int4_sizes_ok(M, N, K)) return 0;
-    return padded(check_workspace_bytes()) + part_bytes(M, N, int4_plan(M, N, K, false).parts);
+    const Int4Plan plan = int4_plan(M, N, K, false);
+    return padded(check_workspace_bytes()) + std::max(part_bytes(M, N, plan), padded((size_t)(M * N) * sizeof(Int4Sums))) + digit_bytes(K, plan) + unit_bytes(K, plan);
 }
 
 int tao_bound_linear_int4(const float* A, const uint8_t* W, const float* scale, const uint8_t* zero, long group, const float* bias,
@@ -558,9 +807,10 @@ int tao_bound_linear_int4(const float* A, const uint8_t* W, const float* scale, 
     const Int4Plan plan = int4_plan(M, N, K, p.uflow != 0.0);
     hipStream_t st = (hipStream_t)stream;
     p.y = y; p.tau = tau;
-    if (plan.parts == 1) return int4_launch(p, plan, st);
+    char* rest = (char*)ws + part_bytes(M, N, plan);
+    if (plan.parts == 1) return int4_launch(p, plan, rest, st);
     p.part = (Int4Sums*)ws;
-    const int rc2 = int4_launch(p, plan, st);
+    const int rc2 = int4_launch(p, plan, rest, st);
     if (rc2 != TAO_OK) return rc2;
     const long blocks = (M * N + 255) / 256;
     hipLaunchKernelGGL(int4_join, dim3((unsigned)(blocks < 256L * 64 ? blocks : 256L * 64)), dim3(256), 0, st, p, plan.parts);
@@ -587,7 +837,7 @@ int tao_bound_check_linear_int4(const float* A, const uint8_t* W, const float* s
     const Int4Plan plan = int4_plan(M, N, K, p.uflow != 0.0);
     p.part = (Int4Sums*)((char*)ws + padded(check_workspace_bytes()));
     if (n > 0) {
-        const int rc2 = int4_launch(p, plan, st);
+        const int rc2 = int4_launch(p, plan, (char*)p.part + std::max(part_bytes(M, N, plan), padded((size_t)n * sizeof(Int4Sums))), st);
         if (rc2 != TAO_OK) return rc2;
     }
     const long want = (n + kCheckThreads - 1) / kCheckThreads;

@@ -110,20 +110,19 @@ constexpr int kInt4Block = 128;                              // columns of a blo
 constexpr int kInt4Codes = kInt4Block / 2 + 16;              // bytes of a column's codes of a block in LDS
 constexpr unsigned kInt4Row = kInt4Block + 16;               // bytes of a digit's row in LDS (16 more: the eight rows that are read at a time lie in different banks)
 
-// KW groups of NW wavefronts: a wavefront has CT tiles of 16 columns and the tokens in RT row tiles of four; the groups share out the reduction, their sums are added in LDS.
-// Fewer tokens are there again in the other rows; with two tokens and two tiles of columns the halves of a wavefront have a tile each for putting the digits together.
-template <int TOKENS_, int CT_, int NW_, int KW_, int WAVES_>
+// Up to eight tokens: a workgroup has 16 columns, its KW wavefronts share out the reduction, and each forms the digits of its blocks by itself.  A wavefront has the tokens in RT row tiles
+// of four; fewer tokens are there again in the other rows.
+template <int TOKENS_, int WAVES_>
 struct Int4Shape {
-    static constexpr int TOKENS = TOKENS_, CT = CT_, NW = NW_, KW = KW_, WAVES = WAVES_, THREADS = NW * KW * kWave, COLUMNS = 16 * CT * NW;
-    static constexpr bool HALVES = TOKENS == 2 && CT == 2;
-    static constexpr int RT = (TOKENS + 3) / 4, ALIKE = TOKENS < 4 ? TOKENS : 4, SLOTS = HALVES ? 1 : RT * CT;       // ALIKE: tokens of a row tile, SLOTS: outputs of a lane
+    static constexpr int TOKENS = TOKENS_, CT = 1, NW = 1, KW = 8, WAVES = WAVES_, THREADS = KW * kWave, COLUMNS = 16;
+    static constexpr int RT = (TOKENS + 3) / 4, ALIKE = TOKENS < 4 ? TOKENS : 4, SLOTS = RT;       // ALIKE: tokens of a row tile, SLOTS: outputs of a lane
     static constexpr int PIECES = TOKENS * kInt4Block / 8;   // of eight activations, in a block
-    static constexpr int BLOCKS = PIECES < NW * kWave ? NW * kWave / PIECES : 1, UNITS = BLOCKS * PIECES / (NW * kWave);      // blocks of a chunk, pieces that a lane brings
+    static constexpr int BLOCKS = PIECES < kWave ? kWave / PIECES : 1, UNITS = BLOCKS * PIECES / kWave;      // blocks of a chunk, pieces that a lane brings
     static constexpr int SET = TOKENS * 4 * kInt4Row, BLOCK = 2 * SET, DIGITS = BLOCKS * (BLOCK + 8 * TOKENS);     // bytes: digits of X, and of |X|; their units behind them
-    static constexpr int CODES = 16 * CT * kInt4Codes;            // of a wavefront
-    static constexpr int SUMS = KW * NW * SLOTS * kWave * (int)sizeof(Int4Sums);
-    static constexpr int STAGES = KW * (DIGITS + NW * CODES), LDS = STAGES > SUMS ? STAGES : SUMS;
-    static_assert(BLOCKS * PIECES == UNITS * NW * kWave && DIGITS % 16 == 0, "whole blocks a chunk");
+    static constexpr int CODES = 16 * kInt4Codes;            // of a wavefront
+    static constexpr int SUMS = KW * SLOTS * kWave * (int)sizeof(Int4Sums);
+    static constexpr int STAGES = KW * (DIGITS + CODES), LDS = STAGES > SUMS ? STAGES : SUMS;
+    static_assert(BLOCKS * PIECES == UNITS * kWave && DIGITS % 16 == 0, "whole blocks a chunk");
     static_assert(LDS <= 160 * 1024, "a compute unit's");
 };
 
@@ -217,6 +216,14 @@ __device__ __forceinline__ void int4_spread(unsigned v, unsigned* to) {
         to[2 * i] = rows[0]; to[2 * i + 1] = rows[1];
     }
 }
+// A column's scale and biased zero point of four folds, or of two for two tiles of columns, from the rows of 16 lanes that read them.  (A column whose zero point does not fit the
+// bytes gets NaN: its outputs are then formed in binary64.)
+__device__ __forceinline__ void int4_factors(bool zeroed, float s, unsigned char own_z, unsigned* scale, unsigned* biased) {
+    const unsigned z = zeroed ? own_z : 8u;
+    int4_spread(__builtin_amdgcn_perm(0u, 127u + min(z, 127u), 0u), biased);
+    int4_spread(z > 127u ? 0x7fc00000u : __float_as_uint(s), scale);
+}
+__device__ __forceinline__ int int4_group(const Int4Args& p, int column) { return min((int)((unsigned long)(column >> 5) * p.per_group >> 32), p.groups - 1); }
 // Order between the lanes of a wavefront: LDS takes its accesses in order, so only the compiler has to keep it.
 __device__ __forceinline__ void wave_order() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -244,7 +251,7 @@ __device__ __forceinline__ void int4_finish(const Int4Args& p, char* lds, const 
             v.sum += other.sum; v.size += other.size; v.err += other.err;
         }
         v.size += v.err;
-        const int slot = o / kWave % SLOTS, q = o >> 4 & 3, t = SH::HALVES ? q & 1 : slot / CT * 4 + q, c = SH::HALVES ? q >> 1 : slot % CT;
+        const int slot = o / kWave % SLOTS, q = o >> 4 & 3, t = slot / CT * 4 + q, c = slot % CT;
         const long i = m0 + t, j = n0 + (o / OUT * CT + c) * 16 + (o & 15);
         const bool own = t < SH::TOKENS && i < p.M && j < p.N;
         if (p.part) {
@@ -262,13 +269,12 @@ __device__ __forceinline__ void int4_finish(const Int4Args& p, char* lds, const 
     }
 }
 
-// What a lane requests of a chunk: eight activations, of each block CT times 16 bytes of weights, and of the scales and zero points of the chunk's folds every 4 / CT-th for one column (lanes
-// in order of tiles, then of folds).
+// What a lane requests of a chunk: pieces of eight activations, of each block 16 bytes of weights, and of the scales and zero points of the chunk's folds every fourth for one column.
 template <class SH, int FOLDS>
 struct Int4Chunk {
-    static constexpr int FACTORS = (SH::BLOCKS * FOLDS * SH::CT + 3) / 4;
+    static constexpr int FACTORS = (SH::BLOCKS * FOLDS + 3) / 4;
     floatx4_any a[SH::UNITS][2];
-    uintx4 raw[SH::BLOCKS][SH::CT];
+    uintx4 raw[SH::BLOCKS];
     float s[FACTORS];
     unsigned char z[FACTORS];
 };
@@ -279,51 +285,45 @@ struct Int4Chunk {
 template <class SH, int FOLDS>
 __global__ __launch_bounds__(SH::THREADS, SH::WAVES) void int4_tiles(Int4Args p, Int4Grid grid) {
     extern __shared__ __align__(16) char lds[];
-    constexpr int RT = SH::RT, NW = SH::NW, KW = SH::KW, SLOTS = SH::SLOTS, CT = SH::CT, TOKENS = SH::TOKENS, BLOCKS = SH::BLOCKS;
+    constexpr int RT = SH::RT, KW = SH::KW, SLOTS = SH::SLOTS, TOKENS = SH::TOKENS, BLOCKS = SH::BLOCKS;
     constexpr int STEP = FOLDS == 4 ? 32 : 64, STEPS = kInt4Block / STEP, WORDS = STEP / 32;       // columns of a matrix instruction, those of a block, words of a lane's codes for one
     using Chunk = Int4Chunk<SH, FOLDS>;
     // workgroups of one tile of columns on one die (workgroup modulo 8), whose cache then holds their weights
     const unsigned rest = blockIdx.x >> 3, up = grid.token_blocks == 1 ? rest : rest / grid.token_blocks, tile = up * 8 + (blockIdx.x & 7);
     if (tile >= grid.tiles) return;
-    const int lane = threadIdx.x & (kWave - 1), half = lane >> 5, col = lane & 15, piece = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), kg = wave / NW, nw = wave % NW;
-    const long n0 = (long)tile * SH::COLUMNS + 16 * CT * nw, m0 = (long)(rest - up * grid.token_blocks) * SH::TOKENS;
-    // whole blocks are shared out among the groups of all parts
-    const int blocks = grid.blocks, first = min((int)(blockIdx.y * KW + kg) * grid.share, blocks), last = min(first + grid.share, blocks);
-    const int trips = (min(grid.share, blocks) + BLOCKS - 1) / BLOCKS, all = trips + (grid.tail == (int)blockIdx.y);
-    auto group_of = [&](int k) __attribute__((always_inline)) { return min((int)((unsigned long)(k >> 5) * p.per_group >> 32), p.groups - 1); };
-    const long n0w = n0 + lane / 4;
-    const unsigned char* rows_w[CT];
-#pragma unroll
-    for (int c = 0; c < CT; ++c) rows_w[c] = p.W + min(n0w + 16 * c, p.N - 1) * p.ldw + lane % 4 * 16;
-    const long n = min(n0 + (lane & (16 * CT - 1)), p.N - 1);
+    const int lane = threadIdx.x & (kWave - 1), col = lane & 15, piece = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const long n0 = (long)tile * SH::COLUMNS, m0 = (long)(rest - up * grid.token_blocks) * SH::TOKENS;
+    // whole blocks are shared out among the wavefronts of all parts
+    const int blocks = grid.blocks, first = min((int)(blockIdx.y * KW + wave) * grid.share, blocks), last = min(first + grid.share, blocks);
+    const int trips = (last - first + BLOCKS - 1) / BLOCKS, all = trips + (grid.tail == (int)blockIdx.y && wave == KW - 1);
+    const unsigned char* row_w = p.W + min(n0 + lane / 4, p.N - 1) * p.ldw + lane % 4 * 16;
+    const long n = min(n0 + col, p.N - 1);
     const float* scales = p.scale + n * p.groups;
     const bool zeroed = p.zero != nullptr;
-    const unsigned char* zeros = zeroed ? p.zero + n * p.groups : rows_w[0];      // (any bytes, where there are none: a load all the same)
+    const unsigned char* zeros = zeroed ? p.zero + n * p.groups : row_w;     // (any bytes, where there are none: a load all the same)
     const int zero_step = zeroed ? 1 : 0;
     // this lane's pieces of eight activations of a chunk
-    const int at = (nw * kWave + lane) / 16, own_block = at % BLOCKS, own_token = at / BLOCKS, unit = lane % 16;
+    const int at = lane / 16, own_block = at % BLOCKS, own_token = at / BLOCKS, unit = lane % 16;
     const float* a_row[SH::UNITS];
 #pragma unroll
-    for (int u = 0; u < SH::UNITS; ++u) a_row[u] = p.A + min(m0 + own_token + u * (NW * 4 / BLOCKS), p.M - 1) * p.lda + unit * 8;
+    for (int u = 0; u < SH::UNITS; ++u) a_row[u] = p.A + min(m0 + own_token + u * (4 / BLOCKS), p.M - 1) * p.lda + unit * 8;
 
     Int4Sums total[SLOTS];
 #pragma unroll
     for (int o = 0; o < SLOTS; ++o) total[o] = Int4Sums{0.0, 0.0, 0.0};
-    char* digits = lds + kg * SH::DIGITS;
+    char* digits = lds + wave * SH::DIGITS;
     double* units = reinterpret_cast<double*>(digits + BLOCKS * SH::BLOCK);
     char* codes = lds + KW * SH::DIGITS + wave * SH::CODES;
     const int row = lane & (4 * SH::ALIKE - 1), token = piece & (SH::ALIKE - 1);     // a lane's row of a row tile, its token of the products'
 
-    auto meet = [&]() __attribute__((always_inline)) { if constexpr (NW > 1) __syncthreads(); else wave_order(); };
     auto factors = [&](Chunk& w, int block) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < Chunk::FACTORS; ++i) {
             int g = 0;
 #pragma unroll
-            for (int f = 0; f < 4 / CT; ++f) {
-                const int of = group_of(block * kInt4Block + (i * (4 / CT) + f) * (kInt4Block / FOLDS));
-                g = f == 0 || lane >= f * 16 * CT ? of : g;
+            for (int f = 0; f < 4; ++f) {
+                const int of = int4_group(p, block * kInt4Block + (i * 4 + f) * (kInt4Block / FOLDS));
+                g = f == 0 || lane >= f * 16 ? of : g;
             }
             w.s[i] = scales[g];
             w.z[i] = zeros[g * zero_step];
@@ -332,11 +332,7 @@ __global__ __launch_bounds__(SH::THREADS, SH::WAVES) void int4_tiles(Int4Args p,
     // (nothing here branches, so that what is on its way is known where it is waited for: blocks behind the last one repeat it)
     auto request = [&](Chunk& w, int block) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < BLOCKS; ++i) {
-            const int b = min(block + i, blocks - 1) * (kInt4Block / 2);
-#pragma unroll
-            for (int c = 0; c < CT; ++c) __builtin_memcpy(&w.raw[i][c], rows_w[c] + b, 16);
-        }
+        for (int i = 0; i < BLOCKS; ++i) __builtin_memcpy(&w.raw[i], row_w + min(block + i, blocks - 1) * (kInt4Block / 2), 16);
         const int first_column = min(block + own_block, blocks - 1) * kInt4Block;
 #pragma unroll
         for (int u = 0; u < SH::UNITS; ++u) {
@@ -358,85 +354,61 @@ __global__ __launch_bounds__(SH::THREADS, SH::WAVES) void int4_tiles(Int4Args p,
         if (unit == 0) units[own_block * SH::TOKENS + token] = by;
     };
     // block i of the chunk
-    auto multiply = [&](const uintx4 (&raw)[CT], int i, const unsigned (&s_all)[4 * Chunk::FACTORS], const unsigned (&z_all)[4 * Chunk::FACTORS]) __attribute__((always_inline)) {
+    auto multiply = [&](const uintx4& raw, int i, const unsigned (&scale)[4 * Chunk::FACTORS], const unsigned (&biased)[4 * Chunk::FACTORS]) __attribute__((always_inline)) {
         wave_order();
-        char* to = codes + lane / 4 * kInt4Codes + lane % 4 * 16;
-#pragma unroll
-        for (int c = 0; c < CT; ++c) *reinterpret_cast<uintx4*>(to + c * 16 * kInt4Codes) = raw[c];
+        *reinterpret_cast<uintx4*>(codes + lane / 4 * kInt4Codes + lane % 4 * 16) = raw;
         wave_order();
         const char* from = codes + col * kInt4Codes + piece * (4 * WORDS);
         const char* rows = digits + i * SH::BLOCK + row * kInt4Row + piece * (8 * WORDS);
-        intx4 y[RT][CT], t[RT][CT];
+        intx4 y[RT], t[RT];
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            const int f = (i * FOLDS + s * FOLDS / STEPS) * CT;
+            const int f = i * FOLDS + s * FOLDS / STEPS;
             const bool fresh = s % (STEPS / FOLDS) == 0;
-            int d[CT][2 * WORDS], m[CT][2 * WORDS];
+            int d[2 * WORDS], m[2 * WORDS];
 #pragma unroll
-            for (int c = 0; c < CT; ++c)
+            for (int w = 0; w < WORDS; ++w) int4_codes(*reinterpret_cast<const unsigned*>(from + s * (STEP / 2) + 4 * w), biased[f], d + 2 * w, m + 2 * w);
 #pragma unroll
-                for (int w = 0; w < WORDS; ++w)
-                    int4_codes(*reinterpret_cast<const unsigned*>(from + c * 16 * kInt4Codes + s * (STEP / 2) + 4 * w), z_all[f + c], d[c] + 2 * w, m[c] + 2 * w);
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int c = 0; c < CT; ++c) {
-                    const intx4 none = {0, 0, 0, 0};
-                    y[r][c] = int4_product<WORDS>(rows + r * 16 * kInt4Row + s * STEP, d[c], fresh ? none : y[r][c]);
-                    t[r][c] = int4_product<WORDS>(rows + r * 16 * kInt4Row + s * STEP + SH::SET, m[c], fresh ? none : t[r][c]);
-                }
+            for (int r = 0; r < RT; ++r) {
+                const intx4 none = {0, 0, 0, 0};
+                y[r] = int4_product<WORDS>(rows + r * 16 * kInt4Row + s * STEP, d, fresh ? none : y[r]);
+                t[r] = int4_product<WORDS>(rows + r * 16 * kInt4Row + s * STEP + SH::SET, m, fresh ? none : t[r]);
+            }
             if ((s + 1) % (STEPS / FOLDS) != 0) continue;
 #pragma unroll
-            for (int o = 0; o < SLOTS; ++o) {
-                const int r = o / CT, c = o % CT;
-                intx4 yo = y[r][c], to = t[r][c];
-                unsigned scale = s_all[f + c], biased = z_all[f + c];
-                if constexpr (SH::HALVES) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) { yo[e] = half ? y[0][1][e] : yo[e]; to[e] = half ? t[0][1][e] : to[e]; }
-                    scale = half ? s_all[f + 1] : scale; biased = half ? z_all[f + 1] : biased;
-                }
-                int4_fold(yo, to, __uint_as_float(scale), biased, kInt4Block / FOLDS, units[i * TOKENS + r * 4 + token], total[o]);
-            }
+            for (int r = 0; r < RT; ++r) int4_fold(y[r], t[r], __uint_as_float(scale[f]), biased[f], kInt4Block / FOLDS, units[i * TOKENS + r * 4 + token], total[r]);
         }
     };
     Chunk now, next;
     if (trips > 0) request(now, first);
     for (int trip = 0; trip < all; ++trip) {
-        const bool odd = trip == trips;                      // the last block, which is not whole, goes to the last group
-        const int block = odd ? blocks : first + trip * BLOCKS, limit = !odd ? last : kg == KW - 1 ? blocks + 1 : 0;
+        const bool odd = trip == trips;                      // the last block, which is not whole, goes to the last wavefront
+        const int block = odd ? blocks : first + trip * BLOCKS, limit = odd ? blocks + 1 : last;
         if (odd) {                                           // (columns that do not exist have activations of 0)
             const int columns = own_block == 0 ? (int)(p.K % kInt4Block) - unit * 8 : 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int u = 0; u < SH::UNITS; ++u) now.a[u][i >> 2][i & 3] = i < columns ? a_row[u][(long)blocks * kInt4Block + i] : 0.f;
-            const int from = blocks * (kInt4Block / 2) + lane % 4 * 16, bytes = (int)((p.K + 1) / 2);
-#pragma unroll
-            for (int c = 0; c < CT; ++c) now.raw[0][c] = int4_bytes(rows_w[c] - lane % 4 * 16, from, bytes);
+            now.raw[0] = int4_bytes(row_w - lane % 4 * 16, blocks * (kInt4Block / 2) + lane % 4 * 16, (int)((p.K + 1) / 2));
             factors(now, block);
         } else if (trip + 1 < trips) {
             request(next, block + BLOCKS);
         }
-        meet();
+        wave_order();
 #pragma unroll
-        for (int u = 0; u < SH::UNITS; ++u) write(now.a[u], own_token + u * (NW * 4 / BLOCKS));
-        meet();
-        // (a column whose zero point does not fit the bytes gets NaN: its outputs are then formed in binary64)
-        unsigned scale[4 * Chunk::FACTORS], biased[4 * Chunk::FACTORS];          // [fold][tile of columns]
+        for (int u = 0; u < SH::UNITS; ++u) write(now.a[u], own_token + u * (4 / BLOCKS));
+        unsigned scale[4 * Chunk::FACTORS], biased[4 * Chunk::FACTORS];          // of the folds
 #pragma unroll
-        for (int i = 0; i < Chunk::FACTORS; ++i) {
-            const unsigned z = zeroed ? now.z[i] : 8u;
-            int4_spread(__builtin_amdgcn_perm(0u, 127u + min(z, 127u), 0u), biased + 4 * i);
-            int4_spread(z > 127u ? 0x7fc00000u : __float_as_uint(now.s[i]), scale + 4 * i);
-        }
+        for (int i = 0; i < Chunk::FACTORS; ++i) int4_factors(zeroed, now.s[i], now.z[i], scale + 4 * i, biased + 4 * i);
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i)
             if (block + i < limit) multiply(now.raw[i], i, scale, biased);
         now = next;
     }
-    int4_finish<SH>(p, lds, total, m0, (long)tile * SH::COLUMNS);
+    int4_finish<SH>(p, lds, total, m0, n0);
 }
+
 // ---- more tokens: digits are formed once, by a kernel of their own, and lie in the workspace as the products want them: of four tokens and a block
 // X, then |X|, of each the steps' 16 rows in the order of the lanes (loads whose lanes have a row each take the address unit a cycle or two a lane: 49 us for 16 x 12288 x 4096).
 constexpr int kInt4Tile = 2 * 16 * kInt4Block;               // bytes
@@ -468,7 +440,6 @@ __global__ __launch_bounds__(256) void int4_digits(Int4Args p, char* digits, dou
 template <int TOKENS_, int NW_, int KW_, int WAVES_>
 struct Int4Rows {
     static constexpr int TOKENS = TOKENS_, CT = 2, NW = NW_, KW = KW_, WAVES = WAVES_, THREADS = NW * KW * kWave, COLUMNS = 16 * CT * NW, RT = TOKENS / 4, SLOTS = RT * CT;
-    static constexpr bool HALVES = false;
     static constexpr int DIGITS = RT * kInt4Tile, COPIES = DIGITS / 1024 / NW;   // bytes of a block's digits; pieces of 1024 of them that a wavefront brings
     static constexpr int CODES = 16 * CT * kInt4Codes, STAGES = KW * 2 * DIGITS + NW * KW * CODES;
     static constexpr int SUMS = KW * NW * SLOTS * kWave * (int)sizeof(Int4Sums), LDS = STAGES > SUMS ? STAGES : SUMS;
@@ -491,7 +462,6 @@ __global__ __launch_bounds__(SH::THREADS, SH::WAVES) void int4_rows(Int4Args p, 
     auto block_of = [&](int trip) __attribute__((always_inline)) {
         return trip < trips ? (first + trip < last ? first + trip : -1) : trip < all && kg == KW - 1 ? blocks : -1;
     };
-    auto group_of = [&](int k) __attribute__((always_inline)) { return min((int)((unsigned long)(k >> 5) * p.per_group >> 32), p.groups - 1); };
     const unsigned char* rows_w[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) rows_w[c] = p.W + min(n0 + lane / 4 + 16 * c, p.N - 1) * p.ldw + lane % 4 * 16;
@@ -516,7 +486,7 @@ __global__ __launch_bounds__(SH::THREADS, SH::WAVES) void int4_rows(Int4Args p, 
     auto factors = [&](int block) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < FACTORS; ++i) {
-            const int g0 = group_of(block * kInt4Block + 2 * i * (kInt4Block / FOLDS)), g1 = group_of(block * kInt4Block + (2 * i + 1) * (kInt4Block / FOLDS)), g = lane >= 32 ? g1 : g0;
+            const int g = int4_group(p, block * kInt4Block + (2 * i + lane / 32) * (kInt4Block / FOLDS));
             s_own[i] = scales[g];
             z_own[i] = zeros[g * zero_step];
         }
@@ -547,11 +517,7 @@ __global__ __launch_bounds__(SH::THREADS, SH::WAVES) void int4_rows(Int4Args p, 
         __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0)
         unsigned scale[4 * FACTORS], biased[4 * FACTORS];    // [fold][tile of columns]
 #pragma unroll
-        for (int i = 0; i < FACTORS; ++i) {
-            const unsigned z = zeroed ? z_own[i] : 8u;
-            int4_spread(__builtin_amdgcn_perm(0u, 127u + min(z, 127u), 0u), biased + 4 * i);
-            int4_spread(z > 127u ? 0x7fc00000u : __float_as_uint(s_own[i]), scale + 4 * i);
-        }
+        for (int i = 0; i < FACTORS; ++i) int4_factors(zeroed, s_own[i], z_own[i], scale + 4 * i, biased + 4 * i);
         double by[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) by[r] = unit[r];
@@ -687,10 +653,10 @@ static Int4Plan int4_plan(long M, long N, long K, bool terms) {
     const int tokens = M <= 1 ? 1 : M <= 2 ? 2 : M <= 4 ? 4 : M <= 8 || !rows || (N + 63) / 64 * sixteens < 160 ? 8 : 16;
     const long token_blocks = (M + tokens - 1) / tokens, wide = (N + 127) / 128 * token_blocks;
     // columns and groups of a workgroup: the more columns, the fewer read the same digits; four wavefronts where there are two such workgroups a compute unit
-    const int nw = !rows ? 1 : tokens == 16 && wide >= 256 ? 4 : 2, kw = !rows ? (tokens <= 4 ? 8 : 4) : nw == 2 ? 4 : wide >= 512 ? 1 : 2;
+    const int nw = !rows ? 1 : tokens == 16 && wide >= 256 ? 4 : 2, kw = !rows ? 8 : nw == 2 ? 4 : wide >= 512 ? 1 : 2;
     // parts until there is a workgroup for each of the chip's 256 compute units (written out: the workspace's size is asked for where there may be no device), of four blocks a group
     // at least, as their sums take a launch more
-    const long columns = tokens <= 4 ? 16 : 32 * nw;
+    const long columns = rows ? 32 * nw : 16;
     const long workgroups = (N + columns - 1) / columns * token_blocks, most = K / kInt4Block / (4 * kw);
     const long parts = std::max(1L, std::min(256 / std::max(workgroups, 1L), most));
     const long fit = kInt4Slab / ((K + kInt4Block - 1) / kInt4Block * kInt4Block * 8) / tokens;
@@ -759,10 +725,10 @@ static int int4_launch_slabs(const Int4Args& p, const Int4Plan& plan, char* ws, 
 static int int4_launch(const Int4Args& p, const Int4Plan& plan, char* ws, hipStream_t st) {
     if (plan.slab) return int4_launch_slabs(p, plan, ws, st);
     switch (plan.tokens) {
-        case 1:  return int4_launch_tiles<Int4Shape<1, 1, 1, 8, 2>>(p, plan.parts, st);
-        case 2:  return int4_launch_tiles<Int4Shape<2, 1, 1, 8, 4>>(p, plan.parts, st);
-        case 4:  return int4_launch_tiles<Int4Shape<4, 1, 1, 8, 4>>(p, plan.parts, st);
-        case 8:  return int4_launch_tiles<Int4Shape<8, 2, 1, 4, 2>>(p, plan.parts, st);
+        case 1:  return int4_launch_tiles<Int4Shape<1, 2>>(p, plan.parts, st);
+        case 2:  return int4_launch_tiles<Int4Shape<2, 4>>(p, plan.parts, st);
+        case 4:  return int4_launch_tiles<Int4Shape<4, 4>>(p, plan.parts, st);
+        case 8:  return int4_launch_tiles<Int4Shape<8, 2>>(p, plan.parts, st);
     }
     const long blocks = (p.M * p.N + 3) / 4;
     hipLaunchKernelGGL(int4_any, dim3((unsigned)(blocks < 256L * 256 ? blocks : 256L * 256)), dim3(256), 0, st, p);

@@ -17,23 +17,25 @@ struct TableArgs {
     long npos; int half;
     double m, e1, e2, whole;         // Gamma(1), Gamma(2); positions up to `whole` are not rounded
     double k1[2], k2[2];             // of cos, of sin
+    float q1[2], q2[2];              // the same in binary32, where `quick`: they and Gamma(d) are far from its range's ends
+    bool quick;
 };
 
 // cos and sin of |t| < 2^50: t less the nearest multiple k of pi/2 (two parts of pi/2 in fused steps: the first difference is exact, as t and k times the
-// first part are multiples of 2^-52 where k is not 0, the second rounds once: 2^-53 absolutely), then Taylor polynomials on |r| <= pi/4 of degree 13 and 14,
-// whose remainders are below 2^-45 relatively.
+// first part are multiples of 2^-52 where k is not 0, the second rounds once: 2^-53 absolutely), then polynomials on |r| <= pi/4 of degree 11 and 12,
+// for (sin r / r - 1) / r^2 and (cos r - 1 + r^2/2) / r^4 fitted in extended precision at 400 Chebyshev points of r^2 with weights that even out the largest errors: 2^-45 relatively
+// (Taylor's of that degree 2^-37; two terms more take 28.7 us for 27.7 at 131072 x 64).
 __device__ __forceinline__ void cos_sin(double t, double& c, double& s) {
-    const double k = rint(t * 0x1.45f306dc9c883p-1);
+    const double at = fma(t, 0x1.45f306dc9c883p-1, 0x1.8p52), k = at - 0x1.8p52;         // (k in the last bits of the sum)
     const double r = fma(-k, 0x1.1a62633145c07p-54, fma(-k, 0x1.921fb54442d18p+0, t)), z = r * r;
-    double ps = 1.0 / 6227020800.0, pc = -1.0 / 87178291200.0;
-    ps = fma(ps, z, -1.0 / 39916800.0);  pc = fma(pc, z, 1.0 / 479001600.0);
-    ps = fma(ps, z, 1.0 / 362880.0);     pc = fma(pc, z, -1.0 / 3628800.0);
-    ps = fma(ps, z, -1.0 / 5040.0);      pc = fma(pc, z, 1.0 / 40320.0);
-    ps = fma(ps, z, 1.0 / 120.0);        pc = fma(pc, z, -1.0 / 720.0);
-    ps = fma(ps, z, -1.0 / 6.0);         pc = fma(pc, z, 1.0 / 24.0);
+    double ps = -0x1.aa288026d8c33p-26, pc = 0x1.1c81d7955fe06p-29;
+    ps = fma(ps, z, 0x1.71d9aa58557b2p-19);   pc = fma(pc, z, -0x1.27e25f7db439cp-22);
+    ps = fma(ps, z, -0x1.a019fd9bd07dap-13);  pc = fma(pc, z, 0x1.a019ff53f3bf3p-16);
+    ps = fma(ps, z, 0x1.1111110fd4207p-7);    pc = fma(pc, z, -0x1.6c16c16b6175dp-10);
+    ps = fma(ps, z, -0x1.555555555516dp-3);   pc = fma(pc, z, 0x1.5555555555437p-5);
     const double sr = fma(ps * z, r, r);
     const double cr = fma(fma(pc, z, -0.5), z, 1.0);
-    const int q = (int)(long long)k & 3;
+    const int q = __double2loint(at) & 3;
     s = q & 1 ? cr : sr; c = q & 1 ? sr : cr;
     if (q & 2) s = -s;
     if ((q + 1) & 2) c = -c;
@@ -42,13 +44,22 @@ __device__ __forceinline__ void table_element(const TableArgs& a, double p, doub
     const double t = p * f, e = (fabs(p) > a.whole ? a.e2 : a.e1) * fabs(t);
     double c, s;
     cos_sin(t, c, s);
-    const double ac = fabs(c), as = fabs(s), e2 = 0.5 * e * e;
-    const double bc = fmin(fmin(fma(as, e, e2), e), 1.0 + ac), bs = fmin(fmin(fma(ac, e, e2), e), 1.0 + as);
     v[0] = (float)(a.m * c); v[1] = (float)(a.m * s);
-    v[2] = up32g(fma(a.k1[0], bc, a.k2[0] * ac)); v[3] = up32g(fma(a.k1[1], bs, a.k2[1] * as));
+    if (a.quick && (fabs(t) >= 0x1p-60 || t == 0.0)) {
+        // in binary32, whose operations take half the time of binary64's: from E, c and s, an u each off, the sums of positive terms are 6u off at most; (1 + 8u) above them they
+        // are at or above their formulas and less than 16u < 1e-6 from them (131072 x 64: 28.7 us, 32.6 in binary64 with the argument's multiple of pi/2 converted to a whole number)
+        const float ac = fabsf((float)c), as = fabsf((float)s), E = (float)e, e2 = 0.5f * E * E;
+        const float bc = fminf(fminf(fmaf(as, E, e2), E), 1.f + ac), bs = fminf(fminf(fmaf(ac, E, e2), E), 1.f + as);
+        v[2] = fmaf(a.q1[0], bc, a.q2[0] * ac) * (1.f + 0x1p-21f); v[3] = fmaf(a.q1[1], bs, a.q2[1] * as) * (1.f + 0x1p-21f);
+    } else {
+        const double ac = fabs(c), as = fabs(s), e2 = 0.5 * e * e;
+        const double bc = fmin(fmin(fma(as, e, e2), e), 1.0 + ac), bs = fmin(fmin(fma(ac, e, e2), e), 1.0 + as);
+        v[2] = up32g(fma(a.k1[0], bc, a.k2[0] * ac)); v[3] = up32g(fma(a.k1[1], bs, a.k2[1] * as));
+    }
     if (!(fabs(t) < 0x1p50)) { v[0] = v[1] = v[2] = v[3] = NAN; }
 }
-// A thread has VEC neighbouring frequencies of a position: 16-byte stores where rows are whole vectors.  What bounds it: the tables' bytes (16 an element) for long ones.
+// A thread has VEC neighbouring frequencies of a position: 16-byte stores where rows are whole vectors.  What bounds long tables: their bytes (16 an element)
+// and, hardly less, 35 binary64 operations an element: 131072 x 64 in 27.7 us, 4.8 TB/s; one frequency a thread 46.
 template <int VEC>
 __global__ __launch_bounds__(256) void rope_tables(TableArgs a) {
     const unsigned per = (unsigned)a.half / VEC;
@@ -446,6 +457,11 @@ int tao_bound_rope_tables(const int64_t* positions, const float* inv_freq, doubl
         const double cu = c_lib[i] * u;
         a.k1[i] = widen(m * (a.m == 1.0 ? 1.0 + cu : (1.0 + u) * (1.0 + cu)));
         a.k2[i] = widen(m * (a.m == 1.0 ? cu : (1.0 + u) * cu + u));
+    }
+    a.quick = m >= 0x1p-40 && m <= 0x1p40 && a.e1 >= 0x1p-60;
+    for (int i = 0; i < 2; ++i) {
+        a.q1[i] = (float)a.k1[i]; a.q2[i] = (float)a.k2[i];
+        a.quick = a.quick && a.k1[i] <= 0x1p60 && a.k2[i] <= 0x1p60 && (a.k2[i] == 0.0 || a.k2[i] >= 0x1p-100);
     }
     const bool vec = half % 4 == 0 && aligned(cos_table, 16) && aligned(sin_table, 16) && aligned(tau_cos, 16) && aligned(tau_sin, 16);
     const long blocks = (npos * (vec ? half / 4 : half) + 255) / 256;

@@ -300,7 +300,7 @@ __global__ __launch_bounds__(SH::THREADS, SH::WAVES) void int4_tiles(Int4Args p,
     const long n = min(n0 + col, p.N - 1);
     const float* scales = p.scale + n * p.groups;
     const bool zeroed = p.zero != nullptr;
-    const unsigned char* zeros = zeroed ? p.zero + n * p.groups : row_w;     // (any bytes, where there are none: a load all the same)
+    const unsigned char* zeros = zeroed ? p.zero + n * p.groups : reinterpret_cast<const unsigned char*>(scales);        // (bytes that are there, where there are none: a load all the same)
     const int zero_step = zeroed ? 1 : 0;
     // this lane's pieces of eight activations of a chunk
     const int at = lane / 16, own_block = at % BLOCKS, own_token = at / BLOCKS, unit = lane % 16;
@@ -468,7 +468,7 @@ __global__ __launch_bounds__(SH::THREADS, SH::WAVES) void int4_rows(Int4Args p, 
     const long n = min(n0 + (lane & 31), p.N - 1);
     const float* scales = p.scale + n * p.groups;
     const bool zeroed = p.zero != nullptr;
-    const unsigned char* zeros = zeroed ? p.zero + n * p.groups : rows_w[0];
+    const unsigned char* zeros = zeroed ? p.zero + n * p.groups : reinterpret_cast<const unsigned char*>(scales);
     const int zero_step = zeroed ? 1 : 0;
     const char* mine = digits + m0 / 4 * every * kInt4Tile;
     const double* tokens = units + m0 / 4 * every * 4 + piece;

@@ -234,6 +234,23 @@ def test_offsets_beyond_32_bits(tao, M, N, K):
         assert torch.equal(got[0], expect[0]) and torch.equal(got[1], expect[1])
 
 
+def at_the_end(a):
+    """A copy whose last byte is the last one of an allocation of whole pages."""
+    store = torch.empty(20 << 20, dtype=torch.uint8, device="cuda")
+    return store[len(store) - a.nbytes:].view(torch.from_numpy(a).dtype).view(a.shape).copy_(torch.from_numpy(a))
+
+
+@pytest.mark.parametrize("M", [1, 3, 7, 30])
+@pytest.mark.parametrize("K", [31, 33, 48, 66, 95, 128, 130, 288])
+@pytest.mark.parametrize("zero", [False, True])
+def test_operands_that_end_where_their_memory_ends(tao, M, K, zero):
+    """Nothing behind an operand is read, not even to be thrown away (rows shorter than the bytes that a tile brings, tiles beyond the last row, no zero points)."""
+    for group in (32, 64, K):
+        A, q, s, _, z, b = operands(M, 21, K, group, K, zero, True)
+        W, k = int4.pack(q), dict(zero=None if z is None else at_the_end(z), bias=at_the_end(b))
+        assert_product(tao.tao_bound_linear_int4(at_the_end(A), at_the_end(W), at_the_end(s), group, **k), A, q, s, group, z, b)
+
+
 def test_refusals_of_the_binding(tao):
     A, q, s, group, z, b = operands(8, 16, 64, 32, 0, True, True)
     A, W, s, z, b = cuda(A, int4.pack(q), s, z, b)

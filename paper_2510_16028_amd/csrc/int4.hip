@@ -10,8 +10,9 @@ namespace tao {
 
 // The two sums of an output, and how far a tile's may be off (0 for those of binary64).
 struct Int4Sums { double sum, size, err; };
-// Tiles of columns and of tokens, whole blocks of the reduction and those of a group of wavefronts, and the last part if a block that is not whole follows (else -1).
-struct Int4Grid { unsigned tiles, token_blocks; int blocks, share, tail; };
+// Tiles of columns and of tokens, whole blocks of the reduction and those of a group of wavefronts, and the last part if a block that is not whole follows (else -1), first workgroup
+// of the launch (a grid has fewer than 2^32 threads).
+struct Int4Grid { unsigned tiles, token_blocks; int blocks, share, tail; unsigned from; };
 constexpr double kInt4Spare = 14.0 * 0x1p-24;                // ... relative to the size, for the output to be taken
 
 struct Int4Args {
@@ -289,7 +290,7 @@ __global__ __launch_bounds__(SH::THREADS, SH::WAVES) void int4_tiles(Int4Args p,
     constexpr int STEP = FOLDS == 4 ? 32 : 64, STEPS = kInt4Block / STEP, WORDS = STEP / 32;       // columns of a matrix instruction, those of a block, words of a lane's codes for one
     using Chunk = Int4Chunk<SH, FOLDS>;
     // workgroups of one tile of columns on one die (workgroup modulo 8), whose cache then holds their weights
-    const unsigned rest = blockIdx.x >> 3, up = grid.token_blocks == 1 ? rest : rest / grid.token_blocks, tile = up * 8 + (blockIdx.x & 7);
+    const unsigned rest = (grid.from + blockIdx.x) >> 3, up = grid.token_blocks == 1 ? rest : rest / grid.token_blocks, tile = up * 8 + (blockIdx.x & 7);
     if (tile >= grid.tiles) return;
     const int lane = threadIdx.x & (kWave - 1), col = lane & 15, piece = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const long n0 = (long)tile * SH::COLUMNS, m0 = (long)(rest - up * grid.token_blocks) * SH::TOKENS;
@@ -450,7 +451,7 @@ __global__ __launch_bounds__(SH::THREADS, SH::WAVES) void int4_rows(Int4Args p, 
     extern __shared__ __align__(16) char lds[];
     constexpr int RT = SH::RT, CT = SH::CT, NW = SH::NW, KW = SH::KW, SLOTS = SH::SLOTS;
     constexpr int STEP = FOLDS == 4 ? 32 : 64, STEPS = kInt4Block / STEP, WORDS = STEP / 32, FACTORS = (FOLDS * CT + 3) / 4;
-    const unsigned rest = blockIdx.x >> 3, up = grid.token_blocks == 1 ? rest : rest / grid.token_blocks, tile = up * 8 + (blockIdx.x & 7);
+    const unsigned rest = (grid.from + blockIdx.x) >> 3, up = grid.token_blocks == 1 ? rest : rest / grid.token_blocks, tile = up * 8 + (blockIdx.x & 7);
     if (tile >= grid.tiles) return;
     const int lane = threadIdx.x & (kWave - 1), col = lane & 15, piece = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), kg = wave / NW, nw = wave % NW;
@@ -684,10 +685,16 @@ static int int4_launch_shape(void (*whole)(Int4Args, Int4Grid, Rest...), void (*
     });
     if (e != hipSuccess) { g_last_hip_error = (int)e; return TAO_ERR_LAUNCH; }
     const long blocks = p.K / kInt4Block, sharers = (long)SH::KW * parts;
-    const Int4Grid g{(unsigned)tiles, (unsigned)token_blocks, (int)blocks, (int)((blocks + sharers - 1) / sharers), p.K % kInt4Block ? parts - 1 : -1};
+    Int4Grid g{(unsigned)tiles, (unsigned)token_blocks, (int)blocks, (int)((blocks + sharers - 1) / sharers), p.K % kInt4Block ? parts - 1 : -1, 0};
     const auto kernel = p.groups <= 1 || p.group % kInt4Block == 0 ? whole : p.group % (kInt4Block / 2) == 0 ? halves : quarters;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid, (unsigned)parts), dim3(SH::THREADS), SH::LDS, st, p, g, rest...);
-    return launch_status();
+    constexpr long most = 1L << 22;                          // workgroups of a launch (whole eights, 2^31 threads)
+    for (long from = 0; from < (long)grid; from += most) {
+        g.from = (unsigned)from;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min((long)grid - from, most), (unsigned)parts), dim3(SH::THREADS), SH::LDS, st, p, g, rest...);
+        const int rc = launch_status();
+        if (rc != TAO_OK) return rc;
+    }
+    return TAO_OK;
 }
 template <class SH>
 static int int4_launch_tiles(const Int4Args& p, int parts, hipStream_t st) {

@@ -234,6 +234,23 @@ def test_offsets_beyond_32_bits(tao, M, N, K):
         assert torch.equal(got[0], expect[0]) and torch.equal(got[1], expect[1])
 
 
+@pytest.mark.parametrize("M,N,K", [(70000000, 3, 40), (3, 140000000, 33)])
+def test_more_tiles_than_a_launch_has(tao, M, N, K):
+    """Outputs whose tiles would have 2^32 threads and more: the first and last of them, and those next to the seams, against the same product in part."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    A, s = torch.randn((M, K), generator=g, device="cuda"), torch.rand((N, 2), generator=g, device="cuda")
+    W = torch.randint(0, 256, (N, (K + 1) // 2), generator=g, device="cuda", dtype=torch.uint8)
+    y, tau = tao.tao_bound_linear_int4(A, W, s, 32)
+    long, seam = max(M, N), (1 << 22) * (1 if M > N else 16)
+    for at in {0, seam - 50, seam, 2 * seam - 50, long - 100}:
+        if at + 100 > long:
+            continue
+        rows, cols = (slice(at, at + 100), slice(None)) if M > N else (slice(None), slice(at, at + 100))
+        a, w, sc = A[rows].contiguous(), W[cols].contiguous(), s[cols].contiguous()
+        q = torch.stack([w & 15, w >> 4], dim=2).flatten(1)[:, :K]
+        assert_product((y[rows, cols], tau[rows, cols]), a.cpu().numpy(), q.cpu().numpy(), sc.cpu().numpy(), 32, None, None)
+
+
 def at_the_end(a):
     """A copy whose last byte is the last one of an allocation of whole pages."""
     store = torch.empty(20 << 20, dtype=torch.uint8, device="cuda")

@@ -331,6 +331,21 @@ def test_offsets_beyond_32_bits(tao, d, rot):
     assert rc == 0 and torch.equal(view, plain[0])
 
 
+@pytest.mark.parametrize("T,H,d,rot", [(3, 2, 8, 8), (5, 3, 90, 26), (7, 5, 128, 64), (1, 1, 24, 0), (9, 1, 136, 136)])
+def test_operands_that_end_where_their_memory_ends(tao, T, H, d, rot):
+    def at_the_end(a):
+        store = torch.empty(20 << 20, dtype=torch.uint8, device="cuda")
+        return store[len(store) - a.nbytes:].view(torch.from_numpy(a).dtype).view(a.shape).copy_(torch.from_numpy(a))
+    x, c, s, k = heads(T, H, d, rot, errors=True)
+    plain, _, _ = both(tao, x, c, s, k)
+    g = {n: at_the_end(k[n]) for n in ("positions", "tau_cos", "tau_sin")}
+    got = tao.tao_bound_norm_rope(at_the_end(x), at_the_end(c), at_the_end(s), gamma=at_the_end(k["gamma_q"]), **g)
+    assert torch.equal(got[0], plain[0]) and torch.equal(got[1], plain[1])
+    p, f = k["positions"], frequencies(rot // 2)
+    for a, b in zip(tao.tao_bound_rope_tables(*cuda(f, p)), tao.tao_bound_rope_tables(at_the_end(f), at_the_end(p))):
+        assert torch.equal(a, b)
+
+
 def test_refusals_of_the_binding(tao):
     x, c, s, k = heads(4, 3, 16, 16, npos=4)
     xd, cd, sd = cuda(x, c, s)

@@ -677,8 +677,9 @@ _ws_cache = {}
 def _scratch(device, need):
     """One scratch tensor per (device, stream); calls on one stream are ordered, so sharing is safe."""
     torch = _torch()
-    key = (device.index if device.index is not None else torch.cuda.current_device(),
-           torch.cuda.current_stream().cuda_stream)
+    here = _current_device()
+    # (the current stream, also where the tensors are on another device)
+    key = (here if device.index is None else device.index, _raw_stream(here))
     ws = _ws_cache.get(key)
     if ws is None or ws.numel() < need:
         ws = torch.empty(max(int(need), 256), dtype=torch.uint8, device=device)
@@ -918,21 +919,30 @@ def _profile_and_scratch(out, ws, like, here, need):
     return out, ws
 
 
-def _vector(t, n, here, name):
-    """A contiguous [n] tensor, or None."""
+def _dense(t, dtype, shape, here, name):
+    """The address of a contiguous tensor of this type and shape on the current device, or None for None.  (Most calls of a decode step
+    are as long as what Python does before them: one level of calls, the tests in one expression, the refusals apart.)"""
     if t is None:
         return None
-    shape = _on(t, _float32, here, name)
-    if len(shape) != 1 or shape[0] != n or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous [%d] tensor" % (name, n))
-    return t.data_ptr()
+    if isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == here and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    _on(t, dtype, here, name)
+    if len(shape) == 1:
+        raise ValueError("%s must be a contiguous [%d] tensor" % (name, shape[0]))
+    raise ValueError("%s must be contiguous and of shape %s" % (name, tuple(shape)))
 
 
 def _output(t, shape, here, name):
-    """The address of a contiguous tensor of this shape."""
-    if _on(t, _float32, here, name) != shape or not t.is_contiguous():
-        raise ValueError("%s must be contiguous and of shape %s" % (name, tuple(shape)))
-    return t.data_ptr()
+    """... that has to be there."""
+    if isinstance(t, _Tensor) and t.dtype is _float32 and t.get_device() == here and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    _on(t, _float32, here, name)
+    raise ValueError("%s must be contiguous and of shape %s" % (name, tuple(shape)))
+
+
+def _made(shape, like):
+    """A float32 tensor on like's device (new_empty takes 1.7 us, empty with a type and a device 2.1, empty_like 1.1)."""
+    return like.new_empty(shape) if like.dtype is _float32 else _torch_module.empty(shape, dtype=_float32, device=like.device)
 
 
 def _reexecuted(y, tau, with_y, with_tau, shape, like, here):
@@ -940,14 +950,16 @@ def _reexecuted(y, tau, with_y, with_tau, shape, like, here):
     if not (with_y or with_tau):
         raise ValueError("neither y nor tau is asked for")
     if not with_y:
-        y = None
-    elif y is None:
-        y = _torch_module.empty(shape, dtype=_float32, device=like.device)
+        y = yp = None
+    else:
+        if y is None:
+            y = _made(shape, like)
+        yp = _output(y, shape, here, "y")
     if not with_tau:
-        tau = None
-    elif tau is None:
-        tau = _torch_module.empty(shape, dtype=_float32, device=like.device)
-    return y, tau, None if y is None else _output(y, shape, here, "y"), None if tau is None else _output(tau, shape, here, "tau")
+        return y, None, yp, None
+    if tau is None:
+        tau = _made(shape, like) if y is None else _torch_module.empty_like(y)
+    return y, tau, yp, _output(tau, shape, here, "tau")
 
 
 def tao_quantize_rows(x, q=None, scale=None):
@@ -1008,7 +1020,7 @@ def _int8_args(A, scale_a, W, scale_w, bias):
     elif Wd == 3 and batch > 1:
         sW = 1                                           # (0 would share scale_w)
     ldy = N or 1
-    return (here, As[:-1] + Ws[-2:-1], (A.data_ptr(), scale_a.data_ptr(), W.data_ptr(), scale_w.data_ptr(), _vector(bias, N, here, "bias")),
+    return (here, As[:-1] + Ws[-2:-1], (A.data_ptr(), scale_a.data_ptr(), W.data_ptr(), scale_w.data_ptr(), _dense(bias, _float32, (N,), here, "bias")),
             (M, N, K, lda, ldw, ldy, batch, sA, sW, M * ldy))
 
 
@@ -1076,7 +1088,7 @@ def _int4_args(A, W, scale, group, zero, bias):
             raise ValueError("W: last dimension must be contiguous")
         if N > 1:
             ldw = t[0]                                   # (rows that overlap are refused below, those of A too)
-    return (here, As[:-1] + Ws[:1], (A.data_ptr(), W.data_ptr(), scale.data_ptr(), _ptr(zero), group, _vector(bias, N, here, "bias")),
+    return (here, As[:-1] + Ws[:1], (A.data_ptr(), W.data_ptr(), scale.data_ptr(), _ptr(zero), group, _dense(bias, _float32, (N,), here, "bias")),
             (M, N, K, lda if M > 1 else K, ldw, N or 1))
 
 
@@ -1106,22 +1118,7 @@ def tao_bound_check_linear_int4(A, W, scale, group, claimed, zero=None, bias=Non
     return read_profile(out) if readback else out
 
 
-def _table(t, shape, here, name):
-    """The address of a contiguous table, or None."""
-    if t is None:
-        return None
-    if _on(t, _float32, here, name) != shape or not t.is_contiguous():
-        raise ValueError("%s must be contiguous and of shape %s" % (name, tuple(shape)))
-    return t.data_ptr()
-
-
-def _positions(t, n, here):
-    if t is None:
-        return None
-    shape = _on(t, _int64, here, "positions")
-    if len(shape) != 1 or (n is not None and shape[0] != n) or not t.is_contiguous():
-        raise ValueError("positions must be a contiguous int64 vector" + ("" if n is None else " of %d" % n))
-    return t.data_ptr()
+_TABLES = ("cos", "sin", "tau_cos", "tau_sin")
 
 
 def tao_bound_rope_tables(inv_freq, positions=None, npos=None, scale=1.0, model=None, cos=None, sin=None, tau_cos=None, tau_sin=None, with_tau=True):
@@ -1132,8 +1129,9 @@ def tao_bound_rope_tables(inv_freq, positions=None, npos=None, scale=1.0, model=
     fs = _on(inv_freq, _float32, here, "inv_freq")
     if len(fs) != 1 or not inv_freq.is_contiguous():
         raise ValueError("inv_freq must be a contiguous vector")
-    pp = _positions(positions, None, here)
     if positions is not None:
+        if len(_on(positions, _int64, here, "positions")) != 1:
+            raise ValueError("positions must be a contiguous int64 vector")
         if npos is not None and npos != positions.shape[0]:
             raise ValueError("npos is not the number of positions")
         npos = positions.shape[0]
@@ -1143,9 +1141,9 @@ def tao_bound_rope_tables(inv_freq, positions=None, npos=None, scale=1.0, model=
     outs = [cos, sin] + ([tau_cos, tau_sin] if with_tau else [None, None])
     for i in range(4 if with_tau else 2):
         if outs[i] is None:
-            outs[i] = _torch_module.empty(shape, dtype=_float32, device=inv_freq.device)
-    ptrs = [_table(t, shape, here, name) for t, name in zip(outs, ("cos", "sin", "tau_cos", "tau_sin"))]
-    rc = (_lib or lib()).tao_bound_rope_tables(pp, inv_freq.data_ptr(), float(scale), *ptrs, shape[0], shape[1], _mref(model), _raw_stream(here))
+            outs[i] = inv_freq.new_empty(shape)
+    ptrs = [_dense(t, _float32, shape, here, name) for t, name in zip(outs, _TABLES)]
+    rc = (_lib or lib()).tao_bound_rope_tables(_dense(positions, _int64, shape[:1], here, "positions"), inv_freq.data_ptr(), float(scale), *ptrs, shape[0], shape[1], _mref(model), _raw_stream(here))
     _check(rc, "tao_bound_rope_tables")
     return tuple(outs)
 
@@ -1172,10 +1170,10 @@ def _heads_args(x, cos, sin, norm, gamma, gamma_k, heads_k, eps, tau_cos, tau_si
     table = _on(cos, _float32, here, "cos")
     if len(table) != 2:
         raise ValueError("cos and sin must be [npos, rot / 2]")
-    tables = [_table(t, table, here, name) for t, name in ((cos, "cos"), (sin, "sin"), (tau_cos, "tau_cos"), (tau_sin, "tau_sin"))]
+    tables = [_dense(t, _float32, table, here, name) for t, name in zip((cos, sin, tau_cos, tau_sin), _TABLES)]
     if sin is None or (tau_cos is None) != (tau_sin is None):
         raise ValueError("cos and sin, and tau_cos and tau_sin, come together")
-    return (here, shape, (int(norm), x.data_ptr(), _vector(gamma, d, here, "gamma"), _vector(gamma_k, d, here, "gamma_k"), float(eps), *tables, _positions(positions, tokens, here)),
+    return (here, shape, (int(norm), x.data_ptr(), _dense(gamma, _float32, (d,), here, "gamma"), _dense(gamma_k, _float32, (d,), here, "gamma_k"), float(eps), *tables, _dense(positions, _int64, (tokens,), here, "positions")),
             (tokens, heads - heads_k, heads_k, d, 2 * table[1], table[0], ldt, ldh, heads * d, d, int(bool(interleaved))))
 
 
@@ -1242,7 +1240,7 @@ def _groupnorm_act_args(x, groups, gamma, beta):
     here = _current_device()
     shape = _on(x, _float32, here, "x")
     batch, positions, C, ld = _pixels_view(x, shape, "x")
-    return here, shape, (x.data_ptr(), _vector(gamma, C, here, "gamma"), _vector(beta, C, here, "beta")), (batch, positions, C, int(groups), ld, C or 1)
+    return here, shape, (x.data_ptr(), _dense(gamma, _float32, (C,), here, "gamma"), _dense(beta, _float32, (C,), here, "beta")), (batch, positions, C, int(groups), ld, C or 1)
 
 
 def tao_bound_groupnorm_act(x, groups, gamma=None, beta=None, eps=1e-5, act=ACT_SILU, model=None, y=None, tau=None,

@@ -1118,7 +1118,11 @@ def tao_bound_check_linear_int4(A, W, scale, group, claimed, zero=None, bias=Non
     return read_profile(out) if readback else out
 
 
-_TABLES = ("cos", "sin", "tau_cos", "tau_sin")
+def _table(t, like, shape, here, name):
+    """The address of a table, and the table, made where it is not given."""
+    if t is None:
+        t = like.new_empty(shape)
+    return _output(t, shape, here, name), t
 
 
 def tao_bound_rope_tables(inv_freq, positions=None, npos=None, scale=1.0, model=None, cos=None, sin=None, tau_cos=None, tau_sin=None, with_tau=True):
@@ -1138,14 +1142,14 @@ def tao_bound_rope_tables(inv_freq, positions=None, npos=None, scale=1.0, model=
     elif npos is None:
         raise ValueError("positions or npos must be given")
     shape = _torch_module.Size((int(npos), fs[0]))
-    outs = [cos, sin] + ([tau_cos, tau_sin] if with_tau else [None, None])
-    for i in range(4 if with_tau else 2):
-        if outs[i] is None:
-            outs[i] = inv_freq.new_empty(shape)
-    ptrs = [_dense(t, _float32, shape, here, name) for t, name in zip(outs, _TABLES)]
-    rc = (_lib or lib()).tao_bound_rope_tables(_dense(positions, _int64, shape[:1], here, "positions"), inv_freq.data_ptr(), float(scale), *ptrs, shape[0], shape[1], _mref(model), _raw_stream(here))
+    cp, cos = _table(cos, inv_freq, shape, here, "cos")
+    sp, sin = _table(sin, inv_freq, shape, here, "sin")
+    tcp, tau_cos = _table(tau_cos, inv_freq, shape, here, "tau_cos") if with_tau else (None, None)
+    tsp, tau_sin = _table(tau_sin, inv_freq, shape, here, "tau_sin") if with_tau else (None, None)
+    rc = (_lib or lib()).tao_bound_rope_tables(_dense(positions, _int64, shape[:1], here, "positions"), inv_freq.data_ptr(), float(scale), cp, sp, tcp, tsp,
+                                               shape[0], shape[1], _mref(model), _raw_stream(here))
     _check(rc, "tao_bound_rope_tables")
-    return tuple(outs)
+    return cos, sin, tau_cos, tau_sin
 
 
 def _heads_args(x, cos, sin, norm, gamma, gamma_k, heads_k, eps, tau_cos, tau_sin, positions, interleaved):
@@ -1162,19 +1166,24 @@ def _heads_args(x, cos, sin, norm, gamma, gamma_k, heads_k, eps, tau_cos, tau_si
     if gamma_k is not None and heads_k == 0:
         raise ValueError("gamma_k needs heads_k")
     ldt, ldh = heads * d, d
-    if x.numel() > 0:
-        t = x.stride()
-        if d > 1 and t[2] != 1:
+    if tokens and heads and d:
+        ldt, ldh, step = x.stride()
+        if step != 1 and d > 1:
             raise ValueError("x: last dimension must be contiguous")
-        ldt, ldh = t[0] if tokens > 1 else 0, t[1] if heads > 1 else 0
+        if tokens == 1:
+            ldt = 0
+        if heads == 1:
+            ldh = 0
     table = _on(cos, _float32, here, "cos")
     if len(table) != 2:
         raise ValueError("cos and sin must be [npos, rot / 2]")
-    tables = [_dense(t, _float32, table, here, name) for t, name in zip((cos, sin, tau_cos, tau_sin), _TABLES)]
     if sin is None or (tau_cos is None) != (tau_sin is None):
         raise ValueError("cos and sin, and tau_cos and tau_sin, come together")
-    return (here, shape, (int(norm), x.data_ptr(), _dense(gamma, _float32, (d,), here, "gamma"), _dense(gamma_k, _float32, (d,), here, "gamma_k"), float(eps), *tables, _dense(positions, _int64, (tokens,), here, "positions")),
-            (tokens, heads - heads_k, heads_k, d, 2 * table[1], table[0], ldt, ldh, heads * d, d, int(bool(interleaved))))
+    npos, half = table
+    return (here, shape, (int(norm), x.data_ptr(), _dense(gamma, _float32, (d,), here, "gamma"), _dense(gamma_k, _float32, (d,), here, "gamma_k"), float(eps),
+                          _output(cos, table, here, "cos"), _output(sin, table, here, "sin"), _dense(tau_cos, _float32, table, here, "tau_cos"),
+                          _dense(tau_sin, _float32, table, here, "tau_sin"), _dense(positions, _int64, (tokens,), here, "positions")),
+            (tokens, heads - heads_k, heads_k, d, 2 * half, npos, ldt, ldh, heads * d, d, 1 if interleaved else 0))
 
 
 def tao_bound_norm_rope(x, cos, sin, norm=NORM_RMSNORM, gamma=None, gamma_k=None, heads_k=0, eps=1e-6, positions=None, tau_cos=None, tau_sin=None,

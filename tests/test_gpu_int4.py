@@ -154,6 +154,22 @@ def test_strides_and_addresses(tao, M, N, K, group, pad, at, pada, ata):
     assert_product(got, A, q, s, group, z, b)
 
 
+@pytest.mark.parametrize("K,group", [(7, 32), (40, 32), (257, 64), (1030, 1030)])
+@pytest.mark.parametrize("at,pad", [(0, 0), (1, 0), (3, 5), (2, 2)])
+def test_any_size_at_any_address(tao, K, group, at, pad):
+    """The kernel of any size (models with underflow terms take it) with rows from any address; then tiles that leave outputs open: an activation far above the others of its block."""
+    A, q, s, _, z, b = operands(3, 20, K, group, K + at, True, True)
+    W, m = int4.pack(q), tao.FpModel(flags=1)
+    Ad, sd, zd, bd = cuda(A, s, z, b)
+    store = torch.full((at + 20 * (W.shape[1] + pad),), 255, dtype=torch.uint8, device="cuda")
+    Wd = store[at:].view(20, W.shape[1] + pad)[:, :W.shape[1]].copy_(torch.from_numpy(W))
+    assert_product(tao.tao_bound_linear_int4(Ad, Wd, sd, group, zero=zd, bias=bd, model=m), A, q, s, group, z, b, model=m)
+    A[:, K // 2] *= 1e6
+    q[::2, K // 2] = z[::2, K // 2 // group]
+    Wd.copy_(torch.from_numpy(int4.pack(q)))
+    assert_product(tao.tao_bound_linear_int4(cuda(A)[0], Wd, sd, group, zero=zd, bias=bd), A, q, s, group, z, b)
+
+
 def test_wide_output_rows_keep_what_lies_between_them(tao):
     for M, N, K in ((5, 33, 64), (30, 257, 128), (2, 64, 31)):
         A, q, s, group, z, _ = operands(M, N, K, 32, 3)

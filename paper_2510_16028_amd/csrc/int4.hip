@@ -306,7 +306,6 @@ __global__ __launch_bounds__(SH::THREADS, SH::WAVES) void int4_tiles(Int4Args p,
     const long n0 = (long)tile * SH::COLUMNS, m0 = (long)(rest - up * grid.token_blocks) * SH::TOKENS;
     // whole blocks are shared out among the wavefronts of all parts
     const int blocks = grid.blocks, first = min((int)(blockIdx.y * KW + wave) * grid.share, blocks), last = min(first + grid.share, blocks);
-    const int trips = (last - first + BLOCKS - 1) / BLOCKS, all = trips + (grid.tail == (int)blockIdx.y && wave == KW - 1);
     const unsigned char* row_w = p.W + min(n0 + lane / 4, p.N - 1) * p.ldw + lane % 4 * 16;
     const long n = min(n0 + col, p.N - 1);
     const float* scales = p.scale + n * p.groups;
@@ -340,11 +339,11 @@ __global__ __launch_bounds__(SH::THREADS, SH::WAVES) void int4_tiles(Int4Args p,
             w.z[i] = zeros[g * zero_step];
         }
     };
-    // (nothing here branches, so that what is on its way is known where it is waited for: blocks behind the last one repeat it)
+    // (nothing here branches, so that what is on its way is known where it is waited for: blocks behind the wavefront's last one repeat it)
     auto request = [&](Chunk& w, int block) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < BLOCKS; ++i) __builtin_memcpy(&w.raw[i], row_w + min(block + i, blocks - 1) * (kInt4Block / 2), 16);
-        const int first_column = min(block + own_block, blocks - 1) * kInt4Block;
+        for (int i = 0; i < BLOCKS; ++i) __builtin_memcpy(&w.raw[i], row_w + min(block + i, last - 1) * (kInt4Block / 2), 16);
+        const int first_column = min(block + own_block, last - 1) * kInt4Block;
 #pragma unroll
         for (int u = 0; u < SH::UNITS; ++u) {
             const float* a = a_row[u] + first_column;
@@ -390,22 +389,7 @@ __global__ __launch_bounds__(SH::THREADS, SH::WAVES) void int4_tiles(Int4Args p,
             for (int r = 0; r < RT; ++r) int4_fold(y[r], t[r], __uint_as_float(scale[f]), biased[f], kInt4Block / FOLDS, units[i * TOKENS + r * 4 + token], total[r]);
         }
     };
-    Chunk now, next;
-    if (trips > 0) request(now, first);
-    for (int trip = 0; trip < all; ++trip) {
-        const bool odd = trip == trips;                      // the last block, which is not whole, goes to the last wavefront
-        const int block = odd ? blocks : first + trip * BLOCKS, limit = odd ? blocks + 1 : last;
-        if (odd) {                                           // (columns that do not exist have activations of 0)
-            const int columns = own_block == 0 ? (int)(p.K % kInt4Block) - unit * 8 : 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int u = 0; u < SH::UNITS; ++u) now.a[u][i >> 2][i & 3] = i < columns ? a_row[u][(long)blocks * kInt4Block + i] : 0.f;
-            now.raw[0] = int4_bytes(row_w - lane % 4 * 16, blocks * (kInt4Block / 2) + lane % 4 * 16, (int)((p.K + 1) / 2));
-            factors(now, block);
-        } else if (trip + 1 < trips) {
-            request(next, block + BLOCKS);
-        }
+    auto chunk = [&](const Chunk& now, int block, int limit) __attribute__((always_inline)) {
         wave_order();
 #pragma unroll
         for (int u = 0; u < SH::UNITS; ++u) write(now.a[u], own_token + u * (4 / BLOCKS));
@@ -415,7 +399,28 @@ __global__ __launch_bounds__(SH::THREADS, SH::WAVES) void int4_tiles(Int4Args p,
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i)
             if (block + i < limit) multiply(now.raw[i], i, scale, biased);
-        now = next;
+    };
+    if (first < last) {
+        Chunk now, next;
+        request(now, first);
+        for (int block = first;;) {
+            if (block + BLOCKS < last) request(next, block + BLOCKS);
+            chunk(now, block, last);
+            block += BLOCKS;
+            if (block >= last) break;
+            now = next;
+        }
+    }
+    if (grid.tail == (int)blockIdx.y && wave == KW - 1) {    // the last block, which is not whole, goes to the last wavefront (columns that do not exist have activations of 0)
+        Chunk odd;
+        const int columns = own_block == 0 ? (int)(p.K % kInt4Block) - unit * 8 : 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int u = 0; u < SH::UNITS; ++u) odd.a[u][i >> 2][i & 3] = i < columns ? a_row[u][(long)blocks * kInt4Block + i] : 0.f;
+        odd.raw[0] = int4_bytes(row_w - lane % 4 * 16, blocks * (kInt4Block / 2) + lane % 4 * 16, (int)((p.K + 1) / 2));
+        factors(odd, blocks);
+        chunk(odd, blocks, blocks + 1);
     }
     int4_finish<SH>(p, lds, total, m0, n0);
 }

@@ -148,7 +148,7 @@ __device__ __forceinline__ void plain_element(const HeadCoef& h, double hx, floa
 // Sums over TEAM lanes, in every one of them.
 template <int TEAM>
 __device__ __forceinline__ double team_sum(double v) {
-    constexpr int STEPS = TEAM == 8 ? 3 : TEAM == 16 ? 4 : TEAM == 32 ? 5 : 6;
+    constexpr int STEPS = TEAM == 4 ? 2 : TEAM == 8 ? 3 : TEAM == 16 ? 4 : TEAM == 32 ? 5 : 6;
     return wave_all<0, STEPS>(v, [](double p, double q) { return p + q; });
 }
 
@@ -163,7 +163,7 @@ struct HeadCheck {
     const float* y_ref; const float* claimed; double alpha, eps_rel; unsigned int* hist; int rep; ThreadAcc acc;
     __device__ __forceinline__ void put1(long i, float yv, float tv) { check_one(claimed[i], y_ref ? y_ref[i] : yv, tv, alpha, eps_rel, hist, rep, acc); }
 };
-// Any size, stride and layout: a wavefront a head, element by element, x read twice.
+// Any size, stride and layout: a wavefront a head, element by element, x read twice.  (For heads of more than 512 elements, and 2^31 heads and more.)
 template <class Sink>
 __device__ __forceinline__ void head_any(const HeadArgs& a, long row, Sink& sink) {
     const int lane = threadIdx.x & (kWave - 1), half = a.rot >> 1;
@@ -213,7 +213,8 @@ __global__ __launch_bounds__(kCheckThreads) void heads_any_check(HeadArgs a, dou
 }
 
 // ---- heads of whole vectors: d and rot multiples of 8, on 16-byte addresses, up to 512 elements.  TEAM lanes a head; lane j has two vectors of four elements: those from 4 j and from rot / 2 + 4 j on
-// of the rotated ones (8 j and 8 j + 4 where pairs are neighbours), with entries 4 j of the tables; from lane rot / 8 on those from 8 j and 8 j + 4 on.  A head stays in registers, so x is read once.
+// of the rotated ones, with entries 4 j of the tables; lanes from rot / 8 on have those of the two halves of the rest.  Where pairs are neighbours any vectors do: those of the head's two halves.  So
+// neighbouring lanes have neighbouring vectors (two vectors of one lane next to each other, every store fills half a line: 2048 x 40 heads of 128 with neighbouring pairs 45 us, 23 so).  A head stays in registers, so x is read once.
 // What bounds it: HBM for many heads (12 bytes an element), launches for few.
 struct HeadPlace { const float* x; const float* g; long out, table; bool inside; };
 __device__ __forceinline__ HeadPlace head_place(const HeadArgs& a, unsigned row) {
@@ -224,11 +225,14 @@ __device__ __forceinline__ HeadPlace head_place(const HeadArgs& a, unsigned row)
 }
 template <bool INTER>
 __device__ __forceinline__ void item_offsets(const HeadArgs& a, int j, int& first, int& second) {
-    const bool apart = !INTER && 8 * j < a.rot;
-    first = apart ? 4 * j : 8 * j;
-    second = apart ? first + (a.rot >> 1) : first + 4;
+    const int plain = a.d - a.rot;
+    if (INTER)              { first = 4 * j; second = first + (a.d >> 1); }
+    else if (8 * j < a.rot) { first = 4 * j; second = first + (a.rot >> 1); }
+    else                    { first = (a.rot >> 1) + 4 * j; second = first + (plain >> 1); }
 }
 __device__ __forceinline__ floatv4 vector_at(const float* p) { return *reinterpret_cast<const floatv4*>(p); }
+typedef float floatv2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ floatv2 two_at(const float* p) { return *reinterpret_cast<const floatv2*>(p); }
 __device__ __forceinline__ floatv4 stream_at(const float* p) { return __builtin_nontemporal_load(reinterpret_cast<const floatv4*>(p)); }
 // One item's outputs and bounds from its elements (x) and what it looks up.
 template <bool INTER, bool ERRORS>
@@ -241,7 +245,33 @@ __device__ __forceinline__ void head_item(const HeadArgs& a, const HeadCoef& h, 
 #pragma unroll
         for (int e = 0; e < 4; ++e) hx[k][e] = (double)x[k][e] * (double)g[e];
     }
-    if (8 * j < a.rot) {
+    auto plain = [&](int k) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float yv, tv;
+            plain_element(h, hx[k][e], yv, tv);
+            y[k][e] = yv; t[k][e] = tv;
+        }
+    };
+    auto turn = [&](int ka, int ea, int kb, int eb, float c, float s, float tc, float ts) __attribute__((always_inline)) {
+        float ya, yb, ta, tb;
+        rotate_pair<ERRORS>(a, h, hx[ka][ea], hx[kb][eb], c, s, tc, ts, ya, yb, ta, tb);
+        y[ka][ea] = ya; y[kb][eb] = yb; t[ka][ea] = ta; t[kb][eb] = tb;
+    };
+    if constexpr (INTER) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (o[k] >= a.rot) { plain(k); continue; }
+            const long entry = at.table + (o[k] >> 1);
+            floatv2 c = {NAN, NAN}, s = c, tc = {0.f, 0.f}, ts = tc;
+            if (at.inside) {
+                c = two_at(a.c + entry); s = two_at(a.s + entry);
+                if (ERRORS) { tc = two_at(a.tc + entry); ts = two_at(a.ts + entry); }
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) turn(k, 2 * e, k, 2 * e + 1, c[e], s[e], tc[e], ts[e]);
+        }
+    } else if (8 * j < a.rot) {
         const floatv4 none = {0.f, 0.f, 0.f, 0.f}, bad = {NAN, NAN, NAN, NAN};
         floatv4 c = bad, s = bad, tc = none, ts = none;
         if (at.inside) {
@@ -249,22 +279,9 @@ __device__ __forceinline__ void head_item(const HeadArgs& a, const HeadCoef& h, 
             if (ERRORS) { tc = vector_at(a.tc + at.table + 4 * j); ts = vector_at(a.ts + at.table + 4 * j); }
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            // the pair's places: element e of both vectors, or neighbours
-            const int ka = INTER ? e >> 1 : 0, ea = INTER ? 2 * (e & 1) : e, kb = INTER ? ka : 1, eb = INTER ? ea + 1 : e;
-            float ya, yb, ta, tb;
-            rotate_pair<ERRORS>(a, h, hx[ka][ea], hx[kb][eb], c[e], s[e], tc[e], ts[e], ya, yb, ta, tb);
-            y[ka][ea] = ya; y[kb][eb] = yb; t[ka][ea] = ta; t[kb][eb] = tb;
-        }
+        for (int e = 0; e < 4; ++e) turn(0, e, 1, e, c[e], s[e], tc[e], ts[e]);
     } else {
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float yv, tv;
-                plain_element(h, hx[k][e], yv, tv);
-                y[k][e] = yv; t[k][e] = tv;
-            }
+        plain(0); plain(1);
     }
 }
 template <int TEAM>
@@ -358,7 +375,153 @@ __global__ __launch_bounds__(kCheckThreads) void heads_rows_check(HeadCheckArgs 
     __syncthreads();
     finish_pass(hist, acc, red, g.pass);
 }
-// Lanes of a head, or 0 for the kernels of any size.  others: the claims' or outputs' addresses
+// ---- heads of up to 512 elements of any kind, stride and address: TEAM lanes a head, each with up to PAIRS pairs of elements, TEAM apart: those of the rotation, then those of the two halves of the rest.
+// All of a head is requested before the first of it is used, and stays in registers.  (A wavefront a head, x read twice: 2048 x 40 heads of 126 51 us, 40 so, checked 87 and 53; 8000 x 40 of 18 149 and 36.)
+template <int TEAM, int PAIRS>
+struct HeadPairs {
+    int ja[PAIRS], jb[PAIRS], entry[PAIRS];                  // places, -1 where there is none; entry of the tables, -1 where the pair is not rotated
+    float x[PAIRS][2];
+    __device__ __forceinline__ HeadPairs(const HeadArgs& a, int lane) {
+        const int half = a.rot >> 1, rest = (a.d - a.rot + 1) >> 1;
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            const int j = lane + i * TEAM, k = j - half;
+            entry[i] = k < 0 ? j : -1;
+            ja[i] = k < 0 ? (a.interleaved ? 2 * j : j) : k < rest ? a.rot + k : -1;
+            jb[i] = k < 0 ? (a.interleaved ? 2 * j + 1 : j + half) : k < rest && a.rot + rest + k < a.d ? a.rot + rest + k : -1;
+        }
+    }
+    // One head's outputs and bounds.
+    __device__ __forceinline__ void head(const HeadArgs& a, const HeadPlace& at, float (&y)[PAIRS][2], float (&t)[PAIRS][2]) {
+        float g[PAIRS][2], c[PAIRS], s[PAIRS], tc[PAIRS], ts[PAIRS];
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            x[i][0] = ja[i] >= 0 ? at.x[ja[i]] : 0.f; x[i][1] = jb[i] >= 0 ? at.x[jb[i]] : 0.f;
+            g[i][0] = at.g && ja[i] >= 0 ? at.g[ja[i]] : 1.f; g[i][1] = at.g && jb[i] >= 0 ? at.g[jb[i]] : 1.f;
+            const bool turned = entry[i] >= 0 && at.inside;
+            const long e = at.table + entry[i];
+            c[i] = turned ? a.c[e] : NAN; s[i] = turned ? a.s[e] : NAN;
+            tc[i] = turned && a.tc ? a.tc[e] : 0.f; ts[i] = turned && a.tc ? a.ts[e] : 0.f;
+        }
+        if (a.norm) {
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) sum = fma((double)x[i][1], (double)x[i][1], fma((double)x[i][0], (double)x[i][0], sum));
+            sum = team_sum<TEAM>(sum);
+        }
+        const HeadCoef h = head_coef(a, sum);
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            const double ha = (double)x[i][0] * (double)g[i][0], hb = (double)x[i][1] * (double)g[i][1];
+            if (entry[i] >= 0) {
+                rotate_pair<true>(a, h, ha, hb, c[i], s[i], tc[i], ts[i], y[i][0], y[i][1], t[i][0], t[i][1]);
+            } else {
+                plain_element(h, ha, y[i][0], t[i][0]);
+                plain_element(h, hb, y[i][1], t[i][1]);
+            }
+        }
+    }
+};
+template <int TEAM, int PAIRS>
+__global__ __launch_bounds__(256) void heads_pairs(HeadArgs a) {
+    constexpr int TEAMS = 256 / TEAM;
+    HeadPairs<TEAM, PAIRS> p(a, threadIdx.x % TEAM);
+    const unsigned rows = (unsigned)(a.tokens * a.heads);
+    for (unsigned row = blockIdx.x * TEAMS + threadIdx.x / TEAM; row < rows; row += gridDim.x * TEAMS) {
+        const HeadPlace at = head_place(a, row);
+        float y[PAIRS][2], t[PAIRS][2];
+        p.head(a, at, y, t);
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            if (p.ja[i] >= 0) {
+                if (a.y) a.y[at.out + p.ja[i]] = y[i][0];
+                if (a.tau) a.tau[at.out + p.ja[i]] = t[i][0];
+            }
+            if (p.jb[i] >= 0) {
+                if (a.y) a.y[at.out + p.jb[i]] = y[i][1];
+                if (a.tau) a.tau[at.out + p.jb[i]] = t[i][1];
+            }
+        }
+    }
+}
+template <int TEAM, int PAIRS, bool REF>
+__global__ __launch_bounds__(kCheckThreads) void heads_pairs_check(HeadCheckArgs g) {
+    __shared__ unsigned int hist[kBins * kReplicas];
+    __shared__ unsigned int red[kRedWords];
+    __shared__ unsigned int largest;
+    for (int i = threadIdx.x; i < kBins * kReplicas; i += kCheckThreads) hist[i] = 0;
+    if (threadIdx.x == 0) largest = 0;
+    __syncthreads();
+    const HeadArgs& a = g.a;
+    const QuickCheck q(g.quick, g.eps_rel);
+    const bool ordinary = q.eps < INFINITY && q.alpha > 0.f;
+    ThreadAcc acc;
+    Farthest top;
+    unsigned int zeros = 0;
+    const int rep = threadIdx.x & (kReplicas - 1);
+    constexpr int TEAMS = kCheckThreads / TEAM;
+    HeadPairs<TEAM, PAIRS> p(a, threadIdx.x % TEAM);
+    const unsigned rows = (unsigned)(a.tokens * a.heads);
+    for (unsigned row = blockIdx.x * TEAMS + threadIdx.x / TEAM; row < rows; row += gridDim.x * TEAMS) {
+        const HeadPlace at = head_place(a, row);
+        float y[PAIRS][2], t[PAIRS][2], c[PAIRS][2], f[PAIRS][2];
+        // (what does not exist: a claim of 1 for an output of 1, taken out of the count again)
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            c[i][0] = p.ja[i] >= 0 ? a.claimed[at.out + p.ja[i]] : 1.f; c[i][1] = p.jb[i] >= 0 ? a.claimed[at.out + p.jb[i]] : 1.f;
+            if (REF) { f[i][0] = p.ja[i] >= 0 ? a.y_ref[at.out + p.ja[i]] : 1.f; f[i][1] = p.jb[i] >= 0 ? a.y_ref[at.out + p.jb[i]] : 1.f; }
+        }
+        p.head(a, at, y, t);
+#pragma unroll
+        for (int k = 0; k < PAIRS; k += 2) {
+            floatv4 claim, ref, bound;
+            unsigned none = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = k + e / 2;
+                const bool there = (e & 1 ? p.jb[i] : p.ja[i]) >= 0;
+                claim[e] = c[i][e & 1];
+                ref[e] = REF ? f[i][e & 1] : there ? y[i][e & 1] : 1.f;
+                bound[e] = there ? t[i][e & 1] : 0.f;
+                none += there ? 0u : 1u << (8 * e);
+            }
+            if (p.ja[k] < 0) continue;
+            const float most = fmaxf(fmaxf(fabsf(ref[0]), fabsf(ref[1])), fmaxf(fabsf(ref[2]), fabsf(ref[3])));      // (a NaN among them shows in the error)
+            if (settle_four<true, true>(claim, ref, bound, q, top, &largest, newest(&largest), ordinary && most <= 0x1p90f, acc, zeros,
+                                        [&](unsigned bin) __attribute__((always_inline)) { atomicAdd(&hist[bin * kReplicas + rep], 1u); })) {
+                zeros -= __popc(none);
+                continue;
+            }
+#pragma unroll 1
+            for (int e = 0; e < 4; ++e) {
+                if (!(none & 1u)) check_one(claim[0], ref[0], bound[0], g.alpha, g.eps_rel, hist, rep, acc);
+                claim = claim.yzww; ref = ref.yzww; bound = bound.yzww;
+                none >>= 8;
+            }
+        }
+    }
+    if (zeros) atomicAdd(&hist[rep], zeros);
+    settled(top, g.alpha, g.eps_rel, acc);
+    __syncthreads();
+    finish_pass(hist, acc, red, g.pass);
+}
+// Lanes of a head in those kernels, or 0 for the ones of any size.
+static int pairs_team(const HeadArgs& a) {
+    return a.d > 512 || a.tokens * a.heads >= (1L << 31) ? 0 : a.d <= 16 ? 4 : a.d <= 32 ? 8 : a.d <= 64 ? 16 : a.d <= 128 ? 32 : 64;
+}
+// f(team, pairs) with the constants of a launch
+template <class F> static void pairs_dispatch(const HeadArgs& a, int team, F&& f) {
+    using std::integral_constant;
+    const integral_constant<int, 2> two;
+    switch (team) {
+        case 4:  f(integral_constant<int, 4>(), two); break;
+        case 8:  f(integral_constant<int, 8>(), two); break;
+        case 16: f(integral_constant<int, 16>(), two); break;
+        case 32: f(integral_constant<int, 32>(), two); break;
+        default: if (a.d <= 256) f(integral_constant<int, 64>(), two); else f(integral_constant<int, 64>(), integral_constant<int, 4>()); break;
+    }
+}
+// Lanes of a head of whole vectors, or 0.  y, tau: the claims' or outputs' addresses
 static int heads_team(const HeadArgs& a, const void* y, const void* tau) {
     const bool vec = a.d % 8 == 0 && a.rot % 8 == 0 && a.d <= 512 && a.tokens * a.heads < (1L << 31) && aligned(a.x, 16) && aligned(a.gain[0], 16) && aligned(a.gain[1], 16) &&
                      aligned(a.c, 16) && aligned(a.s, 16) && aligned(a.tc, 16) && aligned(a.ts, 16) && aligned(y, 16) && aligned(tau, 16) &&
@@ -491,6 +654,11 @@ int tao_bound_norm_rope(int norm, const float* x, const float* gamma_q, const fl
         heads_dispatch(a, team, [&](auto t, auto inter, auto errors) { heads_launch<t(), inter(), errors()>(a, st); });
         return launch_status();
     }
+    if (const int team = pairs_team(a)) {
+        const long blocks = (rows + 256 / team - 1) / (256 / team);
+        pairs_dispatch(a, team, [&](auto t, auto pairs) { hipLaunchKernelGGL((heads_pairs<t(), pairs()>), dim3((unsigned)(blocks < 256L * 64 ? blocks : 256L * 64)), dim3(256), 0, st, a); });
+        return launch_status();
+    }
     const long blocks = (rows + 3) / 4;
     hipLaunchKernelGGL(heads_any, dim3((unsigned)(blocks < 256L * 64 ? blocks : 256L * 64)), dim3(256), 0, st, a);
     return launch_status();
@@ -518,13 +686,18 @@ int tao_bound_check_norm_rope(int norm, const float* x, const float* gamma_q, co
     hipStream_t st = (hipStream_t)stream;
     const CheckWorkspace w = carve_check_workspace(ws);
     a.tokens = d > 0 ? tokens : 0;
-    const int team = heads_team(a, y_ref, claimed), lanes = team ? team : kWave;
+    const int team = heads_team(a, y_ref, claimed), pairs = team ? 0 : pairs_team(a), lanes = team ? team : pairs ? pairs : kWave;
     const long want = (rows + kCheckThreads / lanes - 1) / (kCheckThreads / lanes);
     const int nblocks = (int)(want < 1 || n <= kAloneElements ? 1 : want > kMaxCheckBlocks ? kMaxCheckBlocks : want);
     const PassOut pass = pass_out(w, nblocks, n, out);
+    const HeadCheckArgs g{a, alpha, eps_rel, quick_alpha(alpha, md), pass};
     if (team) {
-        const HeadCheckArgs g{a, alpha, eps_rel, quick_alpha(alpha, md), pass};
         heads_dispatch(a, team, [&](auto t, auto inter, auto errors) { heads_launch_check<t(), inter(), errors()>(g, nblocks, st); });
+    } else if (pairs) {
+        pairs_dispatch(a, pairs, [&](auto t, auto n) {
+            if (y_ref) hipLaunchKernelGGL((heads_pairs_check<t(), n(), true>), dim3(nblocks), dim3(kCheckThreads), 0, st, g);
+            else       hipLaunchKernelGGL((heads_pairs_check<t(), n(), false>), dim3(nblocks), dim3(kCheckThreads), 0, st, g);
+        });
     } else {
         hipLaunchKernelGGL(heads_any_check, dim3(nblocks), dim3(kCheckThreads), 0, st, a, alpha, eps_rel, pass);
     }

@@ -375,7 +375,7 @@ __global__ __launch_bounds__(kCheckThreads) void heads_rows_check(HeadCheckArgs 
     __syncthreads();
     finish_pass(hist, acc, red, g.pass);
 }
-// ---- heads of up to 512 elements of any kind, stride and address: TEAM lanes a head, each with up to PAIRS pairs of elements, TEAM apart: those of the rotation, then those of the two halves of the rest.
+// ---- heads of up to 512 elements of any kind, stride and address: TEAM lanes a head, each with up to PAIRS pairs of elements (two; four pairs and half the lanes 44 us for 40 at 2048 x 40 heads of 126), TEAM apart: those of the rotation, then those of the two halves of the rest.
 // All of a head is requested before the first of it is used, and stays in registers.  (A wavefront a head, x read twice: 2048 x 40 heads of 126 51 us, 40 so, checked 87 and 53; 8000 x 40 of 18 149 and 36.)
 template <int TEAM, int PAIRS>
 struct HeadPairs {
@@ -526,7 +526,7 @@ static int heads_team(const HeadArgs& a, const void* y, const void* tau) {
     const bool vec = a.d % 8 == 0 && a.rot % 8 == 0 && a.d <= 512 && a.tokens * a.heads < (1L << 31) && aligned(a.x, 16) && aligned(a.gain[0], 16) && aligned(a.gain[1], 16) &&
                      aligned(a.c, 16) && aligned(a.s, 16) && aligned(a.tc, 16) && aligned(a.ts, 16) && aligned(y, 16) && aligned(tau, 16) &&
                      a.ldt % 4 == 0 && a.ldh % 4 == 0 && a.ldyt % 4 == 0 && a.ldyh % 4 == 0;
-    return !vec ? 0 : a.d <= 64 ? 8 : a.d <= 128 ? 16 : a.d <= 256 ? 32 : 64;
+    return !vec ? 0 : a.d <= 32 ? 4 : a.d <= 64 ? 8 : a.d <= 128 ? 16 : a.d <= 256 ? 32 : 64;
 }
 template <int TEAM, bool INTER, bool ERRORS>
 static void heads_launch(const HeadArgs& a, hipStream_t st) {
@@ -547,6 +547,7 @@ template <class F> static void heads_dispatch(const HeadArgs& a, int team, F&& f
         else               { if (a.tc) f(t, bool_constant<false>(), bool_constant<true>()); else f(t, bool_constant<false>(), bool_constant<false>()); }
     };
     switch (team) {
+        case 4:  rest(integral_constant<int, 4>()); break;
         case 8:  rest(integral_constant<int, 8>()); break;
         case 16: rest(integral_constant<int, 16>()); break;
         case 32: rest(integral_constant<int, 32>()); break;

@@ -299,6 +299,36 @@ def test_check_is_the_streaming_check_of_the_stored_bound(tao, T, H, d, rot, ref
     assert honest["accept"] == 1 and honest["max_rel"] == 0.0 and honest["n"] == T * H * d
 
 
+@pytest.mark.parametrize("d", [2, 3, 15, 16, 17, 31, 32, 33, 63, 65, 66, 127, 129, 130, 255, 257, 258, 511, 513])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_heads_of_any_length(tao, d, interleaved):
+    """Lengths at the borders of the lanes that a head has: whole heads rotated, half of them, and none; outputs, bounds and the checks of claims at and around their bounds."""
+    for rot in {d // 2 * 2, d // 4 * 2, 0}:
+        x, c, s, k = heads(21, 3, d, rot, errors=rot % 4 == 0, heads_k=1)
+        got, e, g = both(tao, x, c, s, k, interleaved=interleaved)
+        assert_heads(got, e, x, rot)
+        y, tau = got
+        f = torch.tensor([0.0, 0.5, -0.99, 1.01, 0.0, -3.0], device="cuda")[torch.arange(y.numel(), device="cuda") % 6].view(y.shape)
+        claimed = (y.double() + f.double() * tau.double()).float()
+        for y_ref in (None, (y * (1 + 2.0 ** -22)).contiguous()):
+            pf = tao.tao_bound_check_norm_rope(cuda(x)[0], *cuda(c, s), claimed, y_ref=y_ref, interleaved=interleaved, **g)
+            other = y if y_ref is None else y_ref
+            assert_profile_equal(pf, oracle.check_and_profile(claimed.cpu().numpy(), other.cpu().numpy(), tau.cpu().numpy(), 1.0, 1e-12))
+
+
+@pytest.mark.parametrize("d,rot", [(24, 8), (32, 32), (64, 24), (136, 128), (512, 256)])
+@pytest.mark.parametrize("errors", [False, True])
+def test_vectors_of_neighbouring_pairs(tao, d, rot, errors):
+    """Interleaved pairs in whole vectors, some of whose lanes have a rotated vector and one that is not."""
+    x, c, s, k = heads(50, 5, d, rot, errors=errors, heads_k=2)
+    k["positions"][[3, 40]] = [-1, 10 ** 9]
+    got, e, g = both(tao, x, c, s, k, interleaved=True)
+    assert_heads(got, e, x, rot)
+    pf = tao.tao_bound_check_norm_rope(cuda(x)[0], *cuda(c, s), got[0].clone(), interleaved=True, **g)
+    y, tau = (t.cpu().numpy() for t in got)
+    assert_profile_equal(pf, oracle.check_and_profile(y, y, tau))
+
+
 @pytest.mark.parametrize("T,H,d,rot", [(20, 5, 128, 128), (600, 40, 128, 128), (300, 7, 50, 20)])
 def test_the_largest_error_among_many(tao, T, H, d, rot):
     """Claims whose largest error is one of many almost as large, the last of a rising row, the first of a falling one, or the only one."""

@@ -1061,9 +1061,13 @@ def _int4_args(A, W, scale, group, zero, bias):
     """The current device, the output's shape, and the operands' addresses and the sizes and strides of the C call, checked."""
     _torch_module or _torch()
     here = _current_device()
-    As, Ws, Ss = _on(A, _float32, here, "A"), _on(W, _uint8, here, "W"), _on(scale, _float32, here, "scale")
-    if A.numel() > 0:
+    As, Ws = _on(A, _float32, here, "A"), _on(W, _uint8, here, "W")
+    if len(As) == 2 and A.is_contiguous():
+        M, K = As
+        lda = K
+    elif A.numel() > 0:
         M, K, lda = _rows_view(A, "A")
+        lda = lda if M > 1 else K
     elif len(As) > 0:                                    # (a tensor without elements has no strides to speak of)
         M, K = 1, As[-1]
         for n in As[:-1]:
@@ -1073,23 +1077,19 @@ def _int4_args(A, W, scale, group, zero, bias):
         raise ValueError("A: need at least one dimension")
     if len(Ws) != 2 or Ws[1] != (K + 1) // 2:
         raise ValueError("W must be [N, %d]: two weights to a byte of a row" % ((K + 1) // 2))
-    N, ldw = Ws[0], Ws[1]
+    N, ldw = Ws
     group = int(group)
     if group < 1:
         raise ValueError("group must be positive")
-    G = -(-K // group)
-    if tuple(Ss) != (N, G) or not scale.is_contiguous():
-        raise ValueError("scale must be contiguous and of shape (%d, %d)" % (N, G))
-    if zero is not None and (_on(zero, _uint8, here, "zero") != Ss or not zero.is_contiguous()):
-        raise ValueError("zero must be contiguous and shaped like scale")
-    if W.numel() > 0:
+    groups = (N, -(-K // group))
+    if not W.is_contiguous():
         t = W.stride()
         if ldw > 1 and t[1] != 1:
             raise ValueError("W: last dimension must be contiguous")
         if N > 1:
             ldw = t[0]                                   # (rows that overlap are refused below, those of A too)
-    return (here, As[:-1] + Ws[:1], (A.data_ptr(), W.data_ptr(), scale.data_ptr(), _ptr(zero), group, _dense(bias, _float32, (N,), here, "bias")),
-            (M, N, K, lda if M > 1 else K, ldw, N or 1))
+    return (here, As[:-1] + Ws[:1], (A.data_ptr(), W.data_ptr(), _output(scale, groups, here, "scale"), _dense(zero, _uint8, groups, here, "zero"), group,
+                                     _dense(bias, _float32, (N,), here, "bias")), (M, N, K, lda, ldw, N or 1))
 
 
 def tao_bound_linear_int4(A, W, scale, group, zero=None, bias=None, model=None, y=None, tau=None, with_y=True, with_tau=True, ws=None):

@@ -79,6 +79,36 @@ __global__ __launch_bounds__(256) void rope_tables(TableArgs a) {
         }
     }
 }
+// Rows of other lengths: four neighbouring elements of the whole table a thread, over the ends of rows (131072 x 63 29.0 us, one element a thread 35.7; 2^23 x 1 34.4, 39.2).
+__global__ __launch_bounds__(256) void rope_tables_flat(TableArgs a) {
+    const long n = a.npos * a.half, stride = (long)gridDim.x * 1024;
+    for (long i = ((long)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += stride) {
+        long r = n < (1L << 32) ? (long)((unsigned)i / (unsigned)a.half) : i / a.half;
+        int j = (int)(i - r * a.half);
+        double p = (double)(a.positions ? a.positions[r] : r);
+        float v[4][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (e > 0 && ++j == a.half) {
+                j = 0;
+                ++r;
+                if (r < a.npos) p = (double)(a.positions ? a.positions[r] : r);         // (what lies behind the last row is not stored)
+            }
+            table_element(a, p, (double)a.inv_freq[j], v[e]);
+        }
+#pragma unroll
+        for (int o = 0; o < 4; ++o) {
+            if (!a.out[o]) continue;
+            if (i + 4 <= n) {
+                ntstore4(reinterpret_cast<float4*>(a.out[o] + i), make_float4(v[0][o], v[1][o], v[2][o], v[3][o]));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (i + e < n) a.out[o][i + e] = v[e][o];
+            }
+        }
+    }
+}
 
 // ---- norm and rotation of heads
 struct HeadArgs {
@@ -627,11 +657,13 @@ int tao_bound_rope_tables(const int64_t* positions, const float* inv_freq, doubl
         a.q1[i] = (float)a.k1[i]; a.q2[i] = (float)a.k2[i];
         a.quick = a.quick && a.k1[i] <= 0x1p60 && a.k2[i] <= 0x1p60 && (a.k2[i] == 0.0 || a.k2[i] >= 0x1p-100);
     }
-    const bool vec = half % 4 == 0 && aligned(cos_table, 16) && aligned(sin_table, 16) && aligned(tau_cos, 16) && aligned(tau_sin, 16);
-    const long blocks = (npos * (vec ? half / 4 : half) + 255) / 256;
+    // (tables of less than one element for each of the chip's threads: one a thread; 16640 x 63 8.9 us, four a thread 8.4, 2080 x 63 3.5 and 4.7)
+    const bool vec = (half % 4 == 0 || npos * half >= 1L << 19) && aligned(cos_table, 16) && aligned(sin_table, 16) && aligned(tau_cos, 16) && aligned(tau_sin, 16);
+    const long blocks = ((vec ? (npos * half + 3) / 4 : npos * half) + 255) / 256;
     const dim3 grid((unsigned)(blocks < 256L * 64 ? blocks : 256L * 64)), blk(256);
-    if (vec) hipLaunchKernelGGL(rope_tables<4>, grid, blk, 0, (hipStream_t)stream, a);
-    else     hipLaunchKernelGGL(rope_tables<1>, grid, blk, 0, (hipStream_t)stream, a);
+    if (vec && half % 4 == 0) hipLaunchKernelGGL(rope_tables<4>, grid, blk, 0, (hipStream_t)stream, a);
+    else if (vec)             hipLaunchKernelGGL(rope_tables_flat, grid, blk, 0, (hipStream_t)stream, a);
+    else                      hipLaunchKernelGGL(rope_tables<1>, grid, blk, 0, (hipStream_t)stream, a);
     return launch_status();
 }
 

@@ -105,6 +105,23 @@ def test_tables_in_part(tao):
         assert tao.tao_bound_rope_tables(cuda(frequencies(half))[0], npos=npos)[0].shape == (npos, half)
 
 
+@pytest.mark.parametrize("npos,half", [(1, 1), (1, 2), (1, 3), (2, 3), (5, 1), (7, 5), (3, 7), (129, 63), (2000, 3), (11, 130), (8323, 63), (174763, 3), (524289, 1), (262145, 2)])
+@pytest.mark.parametrize("at", [0, 1])
+def test_tables_of_any_length(tao, npos, half, at):
+    """Rows that are no whole vectors, with what lies before and behind the tables left as it was, from aligned and other addresses, in both kernels; positions that end where their memory ends."""
+    store = torch.empty(20 << 20, dtype=torch.uint8, device="cuda")
+    p = np.random.default_rng(npos + half).integers(0, 100000, npos)
+    pd = store[len(store) - p.nbytes:].view(torch.int64).copy_(torch.from_numpy(p))
+    f = frequencies(half, 1e4)
+    whole = [torch.full((npos * half + 8,), 7.0, device="cuda") for _ in range(4)]
+    views = [w[at:at + npos * half].view(npos, half) for w in whole]
+    got = tao.tao_bound_rope_tables(cuda(f)[0], pd, cos=views[0], sin=views[1], tau_cos=views[2], tau_sin=views[3])
+    rows = np.arange(npos) if npos < 3000 else np.unique(np.concatenate([np.arange(40), np.arange(npos - 700, npos), np.random.default_rng(0).integers(0, npos, 500)]))
+    assert_tables([t[torch.from_numpy(rows).cuda()] for t in got], p[rows], f)
+    for w in whole:
+        assert bool((w[:at] == 7).all()) and bool((w[at + npos * half:] == 7).all())
+
+
 def test_tables_that_are_long(tao):
     f = frequencies(64)
     got = tao.tao_bound_rope_tables(cuda(f)[0], npos=131072)

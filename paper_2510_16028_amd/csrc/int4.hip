@@ -663,8 +663,11 @@ constexpr long kInt4Slab = 64L << 20;                        // bytes of digits 
 static Int4Plan int4_plan(long M, long N, long K, bool terms) {
     // (short reductions: a wavefront's lanes are hardly used, and what truncation leaves off would show next to the few roundings that the bound holds)
     if (K <= 32 || K > (1L << 20) || terms) return {0, 1, 0, 1, 1};
-    // (four and fewer tokens, and small products of up to eight: the digits' own launch costs more than forming them again for every tile)
-    const bool rows = K >= kInt4Block && (M > 8 || (M > 4 && N * K >= 1L << 25));
+    // (four and fewer tokens, and small products of up to eight: the digits' own launch costs more than forming them again for every tile.  Of eight tokens, us by tiles of 16 columns that form
+    // them and with digits formed once: 1024 x 8192 7.7 and 8.7, 4096 x 4096 10.5 and 14.9, 16384 x 1024 13.5 and 17.9; where there are more than two such tiles a compute unit, 512 x 16384 10.9 and 7.3;
+    // more than one that is long, 4096 x 6144 19.2 and 15.6; 4096 x 12288 28 and 18; 12288 x 4096 25 and 20.  Four tokens over 4096 x 12288 15.5 and 18.3.)
+    const long sixteenths = (N + 15) / 16;
+    const bool rows = K >= kInt4Block && (M > 8 || (M > 4 && (sixteenths > 512 || (sixteenths > 256 && K > 2048) || N * K >= 1L << 25)));
     const long sixteens = (M + 15) / 16;
     const int tokens = M <= 1 ? 1 : M <= 2 ? 2 : M <= 4 ? 4 : M <= 8 || !rows || (N + 63) / 64 * sixteens < 160 ? 8 : 16;
     const long token_blocks = (M + tokens - 1) / tokens, wide = (N + 127) / 128 * token_blocks;

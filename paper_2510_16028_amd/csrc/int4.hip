@@ -121,7 +121,7 @@ constexpr int kInt4Block = 128;                              // columns of a blo
 constexpr int kInt4Codes = kInt4Block / 2 + 16;              // bytes of a column's codes of a block in LDS
 constexpr unsigned kInt4Row = kInt4Block + 16;               // bytes of a digit's row in LDS (16 more: the eight rows that are read at a time lie in different banks)
 
-// Up to eight tokens: a workgroup has 16 columns, its KW wavefronts share out the reduction, and each forms the digits of its blocks by itself.  A wavefront has the tokens in RT row tiles
+// Few tiles of up to eight tokens: a workgroup has 16 columns, its KW wavefronts share out the reduction, and each forms the digits of its blocks by itself.  A wavefront has the tokens in RT row tiles
 // of four; fewer tokens are there again in the other rows.
 template <int TOKENS_, int WAVES_>
 struct Int4Shape {
@@ -663,11 +663,11 @@ constexpr long kInt4Slab = 64L << 20;                        // bytes of digits 
 static Int4Plan int4_plan(long M, long N, long K, bool terms) {
     // (short reductions: a wavefront's lanes are hardly used, and what truncation leaves off would show next to the few roundings that the bound holds)
     if (K <= 32 || K > (1L << 20) || terms) return {0, 1, 0, 1, 1};
-    // (four and fewer tokens, and small products of up to eight: the digits' own launch costs more than forming them again for every tile.  Of eight tokens, us by tiles of 16 columns that form
-    // them and with digits formed once: 1024 x 8192 7.7 and 8.7, 4096 x 4096 10.5 and 14.9, 16384 x 1024 13.5 and 17.9; where there are more than two such tiles a compute unit, 512 x 16384 10.9 and 7.3;
-    // more than one that is long, 4096 x 6144 19.2 and 15.6; 4096 x 12288 28 and 18; 12288 x 4096 25 and 20.  Four tokens over 4096 x 12288 15.5 and 18.3.)
-    const long sixteenths = (N + 15) / 16;
-    const bool rows = K >= kInt4Block && (M > 8 || (M > 4 && (sixteenths > 512 || (sixteenths > 256 && K > 2048) || N * K >= 1L << 25)));
+    // (Digits formed anew by every tile of 16 columns and eight tokens, or once, by a launch of their own.  us: 8 x 1024 over 8192 7.7 and 8.7, 8 x 4096 over 4096 10.5 and 14.9, 16 x 1024 over 2048 4.8 and 8.7,
+    // 16 x 512 over 4096 6.9 and 8.8; where there are more than two tiles a compute unit, 8 x 512 over 16384 10.9 and 7.3; more than one of long reductions, 8 x 4096 over 6144 19.2 and 15.6,
+    // 16 x 4096 over 4096 19.3 and 16.4; in long enough ones, 5 x 12288 over 4096 25.5 and 20.5.  Four tokens and fewer by tiles of theirs: 4096 over 12288 15.5 and 18.3.)
+    const long work = (N + 15) / 16 * ((M + 7) / 8);
+    const bool rows = K >= kInt4Block && M > 4 && (work > 512 || (work > 256 && K > 2048) || work * K >= 1L << 21);
     const long sixteens = (M + 15) / 16;
     const int tokens = M <= 1 ? 1 : M <= 2 ? 2 : M <= 4 ? 4 : M <= 8 || !rows || (N + 63) / 64 * sixteens < 160 ? 8 : 16;
     const long token_blocks = (M + tokens - 1) / tokens, wide = (N + 127) / 128 * token_blocks;

@@ -64,6 +64,47 @@ def test_reduction_lengths(tao, K):
         assert_product(run(tao, *o), *o)
 
 
+# products of so many tiles that digits are formed once: eight tokens a tile, sixteen over 64 columns, over 128 with two and with one group of wavefronts, and parts of the reduction
+ONCE = [(5, 8300, 130, 32), (9, 4200, 257, 64), (8, 8209, 128, 128), (16, 10300, 200, 128), (15, 10250, 384, 96), (40, 11000, 130, 32), (33, 11001, 192, 64), (100, 10000, 129, 128), (81, 10013, 160, 160), (5, 4200, 6200, 160)]
+
+
+@pytest.mark.filterwarnings("ignore:invalid value")
+@pytest.mark.parametrize("M,N,K,group", ONCE)
+@pytest.mark.parametrize("zero", [False, True])
+def test_products_of_many_tiles(tao, M, N, K, group, zero):
+    """... ordinary ones; rows of A and W further apart than they are long, from any address, with tokens and scales that are no numbers, an activation far above the others, and zero points
+    outside the codes; then the check of claims at and around their bounds."""
+    A, q, s, _, z, b = o = operands(M, N, K, group, 1, zero, not zero)
+    assert_product(run(tao, *o), *o)
+    A[1, 5], A[2, K // 2], A[3, 0] = np.nan, np.inf, 1e7
+    s[7, 0], s[N - 1, -1] = np.nan, 0.0
+    q[::3, 0] = 8 if z is None else z[::3, 0]
+    if zero:
+        z[5::200, 0] = 255
+    W = int4.pack(q)
+    Ad, Wd = torch.full((M, K + 3), float("nan"), device="cuda")[:, 1:K + 1], torch.full((N, W.shape[1] + 5), 255, dtype=torch.uint8, device="cuda")[:, 3:W.shape[1] + 3]
+    Ad.copy_(torch.from_numpy(A))
+    Wd.copy_(torch.from_numpy(W))
+    sd, zd, bd = cuda(s, z, b)
+    y, tau = tao.tao_bound_linear_int4(Ad, Wd, sd, group, zero=zd, bias=bd)
+    assert_product((y, tau), A, q, s, group, z, b)
+    f = torch.tensor([0.0, 0.5, -0.99, 1.01, -3.0, 0.0, 0.0], device="cuda")[torch.arange(M * N, device="cuda") % 7].view(M, N)
+    claimed = (y.double() + f.double() * tau.double()).float()
+    pf = tao.tao_bound_check_linear_int4(Ad, Wd, sd, group, claimed, zero=zd, bias=bd)
+    assert_profile_equal(pf, oracle.check_and_profile(claimed.cpu().numpy(), y.cpu().numpy(), tau.cpu().numpy()))
+
+
+def test_more_tokens_than_digits_are_kept_of(tao):
+    """A product whose digits take more than the workspace keeps of them at a time: the tokens go through in slabs."""
+    M, N, K, group = 20000, 48, 1000, 64
+    need = tao.tao_linear_int4_workspace_bytes(M, N, K)
+    assert need < 8 * M * K                                  # (eight bytes of digits an activation)
+    A, q, s, _, z, b = operands(M, N, K, group, 2, True, True)
+    got = run(tao, A, q, s, group, z, b)
+    for rows in (slice(0, 40), slice(8000, 8300), slice(16200, 16500), slice(M - 40, M)):
+        assert_product([t[rows] for t in got], A[rows], q, s, group, z, b)
+
+
 @pytest.mark.parametrize("M", [1, 2, 3, 5, 8, 9, 16, 24, 25, 32, 40, 100])
 def test_numbers_of_tokens(tao, M):
     o = operands(M, 100, 300, 64, M, True, False, spread=3.0)

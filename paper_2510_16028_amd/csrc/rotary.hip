@@ -17,7 +17,7 @@ struct TableArgs {
     long npos; int half;
     double m, e1, e2, whole;         // Gamma(1), Gamma(2); positions up to `whole` are not rounded
     double k1[2], k2[2];             // of cos, of sin
-    float q1[2], q2[2];              // the same in binary32, where `quick`: they and Gamma(d) are far from its range's ends
+    float q1[2], q2[2];              // the same in binary32, where `quick`: they are far from the upper end of its range
     bool quick;
 };
 
@@ -45,13 +45,13 @@ __device__ __forceinline__ void table_element(const TableArgs& a, double p, doub
     double c, s;
     cos_sin(t, c, s);
     v[0] = (float)(a.m * c); v[1] = (float)(a.m * s);
-    if (a.quick && (fabs(t) >= 0x1p-60 || t == 0.0)) {
-        // in binary32, whose operations take half the time of binary64's: from E, c and s, an u each off, the sums of positive terms are 6u off at most; (1 + 8u) above them they
-        // are at or above their formulas and less than 16u < 1e-6 from them (131072 x 64: 28.7 us, 32.6 in binary64 with the argument's multiple of pi/2 converted to a whole number)
-        const float ac = fabsf((float)c), as = fabsf((float)s), E = (float)e, e2 = 0.5f * E * E;
-        const float bc = fminf(fminf(fmaf(as, E, e2), E), 1.f + ac), bs = fminf(fminf(fmaf(ac, E, e2), E), 1.f + as);
-        v[2] = fmaf(a.q1[0], bc, a.q2[0] * ac) * (1.f + 0x1p-21f); v[3] = fmaf(a.q1[1], bs, a.q2[1] * as) * (1.f + 0x1p-21f);
-    } else {
+    // in binary32, whose operations take half the time of binary64's: from E, c and s, an u each off, the sums of positive terms are 6u off at most; (1 + 8u) above them they
+    // are at or above their formulas and less than 16u < 1e-6 from them (131072 x 64: 28.7 us, 32.6 in binary64 with the argument's multiple of pi/2 converted to a whole number).  From 2^-60 on
+    // (factors up to 2^60), where what is lost below 2^-126 on the way is less than 2^-28 of them; smaller ones, of angles next to 0 where c_cos or c_sin is 0 or u or m small, in binary64.
+    const float ac = fabsf((float)c), as = fabsf((float)s), E = (float)e, e2 = 0.5f * E * E;
+    const float bc = fminf(fminf(fmaf(as, E, e2), E), 1.f + ac), bs = fminf(fminf(fmaf(ac, E, e2), E), 1.f + as);
+    v[2] = fmaf(a.q1[0], bc, a.q2[0] * ac) * (1.f + 0x1p-21f); v[3] = fmaf(a.q1[1], bs, a.q2[1] * as) * (1.f + 0x1p-21f);
+    if (!(a.quick && fminf(v[2], v[3]) >= 0x1p-60f)) {
         const double ac = fabs(c), as = fabs(s), e2 = 0.5 * e * e;
         const double bc = fmin(fmin(fma(as, e, e2), e), 1.0 + ac), bs = fmin(fmin(fma(ac, e, e2), e), 1.0 + as);
         v[2] = up32g(fma(a.k1[0], bc, a.k2[0] * ac)); v[3] = up32g(fma(a.k1[1], bs, a.k2[1] * as));
@@ -652,10 +652,10 @@ int tao_bound_rope_tables(const int64_t* positions, const float* inv_freq, doubl
         a.k1[i] = widen(m * (a.m == 1.0 ? 1.0 + cu : (1.0 + u) * (1.0 + cu)));
         a.k2[i] = widen(m * (a.m == 1.0 ? cu : (1.0 + u) * cu + u));
     }
-    a.quick = m >= 0x1p-40 && m <= 0x1p40 && a.e1 >= 0x1p-60;
+    a.quick = true;
     for (int i = 0; i < 2; ++i) {
         a.q1[i] = (float)a.k1[i]; a.q2[i] = (float)a.k2[i];
-        a.quick = a.quick && a.k1[i] <= 0x1p60 && a.k2[i] <= 0x1p60 && (a.k2[i] == 0.0 || a.k2[i] >= 0x1p-100);
+        a.quick = a.quick && a.k1[i] <= 0x1p60 && a.k2[i] <= 0x1p60;
     }
     // (tables of less than one element for each of the chip's threads: one a thread; 16640 x 63 8.9 us, four a thread 8.4, 2080 x 63 3.5 and 4.7)
     const bool vec = (half % 4 == 0 || npos * half >= 1L << 19) && aligned(cos_table, 16) && aligned(sin_table, 16) && aligned(tau_cos, 16) && aligned(tau_sin, 16);

@@ -93,6 +93,17 @@ def test_table_models(tao, model):
     assert_tables(tao.tao_bound_rope_tables(*cuda(f, p), scale=1.1, model=m), p, f, 1.1, m)
 
 
+@pytest.mark.parametrize("model,scale", [(dict(c_sin=0.0, c_cos=0.0), 1.0), (dict(c_sin=4.0, c_cos=0.0), 1.0), (dict(c_sin=0.0, c_cos=0.0, u=2.0 ** -11), 1.0), (dict(u=2.0 ** -40), 2.0 ** -40),
+                                         (dict(c_sin=1e-20, c_cos=1e-20, u=2.0 ** -40), 2.0 ** -40), (dict(c_sin=1e4, c_cos=0.0), 2.0 ** -100), (dict(), 2.0 ** -120), (dict(c_cos=0.0), 1e30)])
+def test_table_bounds_next_to_nothing(tao, model, scale):
+    """Angles next to 0 under models and amplitudes that leave hardly any bound: its terms, or it, fall below binary32's smallest normal numbers."""
+    rng = np.random.default_rng(5)
+    f = np.concatenate([2.0 ** rng.uniform(-75, -20, 400), 2.0 ** -np.arange(40, 62), [1.0, 0.1, 3e-7, 1e-30, 0.0]]).astype(F)
+    p = np.array([0, 1, 3, 1001, 70001])
+    m = tao.FpModel(**model)
+    assert_tables(tao.tao_bound_rope_tables(*cuda(f, p), scale=scale, model=m), p, f, scale, m)
+
+
 def test_tables_in_part(tao):
     f = cuda(frequencies(8))[0]
     whole = tao.tao_bound_rope_tables(f, npos=9)

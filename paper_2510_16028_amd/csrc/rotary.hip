@@ -17,17 +17,18 @@ struct TableArgs {
     long npos; int half;
     double m, e1, e2, whole;         // Gamma(1), Gamma(2); positions up to `whole` are not rounded
     double k1[2], k2[2];             // of cos, of sin
-    float q1[2], q2[2];              // the same in binary32, where `quick`: they are far from the upper end of its range
-    bool quick;
+    float q1[2], q2[2];              // the same in binary32
+    float near;                      // E up to which bounds are formed from those: Gamma(1) 2^20, or 0
 };
 
-// cos and sin of |t| < 2^50: t less the nearest multiple k of pi/2 (two parts of pi/2 in fused steps: the first difference is exact, as t and k times the
-// first part are multiples of 2^-52 where k is not 0, the second rounds once: 2^-53 absolutely), then polynomials on |r| <= pi/4 of degree 11 and 12,
+// cos and sin of t + lost, |t| < 2^50, lost what t's own rounding left off: t less the nearest multiple k of pi/2 (two parts of pi/2 in fused steps: the first difference is exact, as t
+// and k times the first part are multiples of 2^-52 where k is not 0), then lost, which next to a multiple of pi/2 may be most of what remains; then polynomials on |r| <= pi/4 of degree 11 and 12,
 // for (sin r / r - 1) / r^2 and (cos r - 1 + r^2/2) / r^4 fitted in extended precision at 400 Chebyshev points of r^2 with weights that even out the largest errors: 2^-45 relatively
-// (Taylor's of that degree 2^-37; two terms more take 28.7 us for 27.7 at 131072 x 64).
-__device__ __forceinline__ void cos_sin(double t, double& c, double& s) {
+// (Taylor's of that degree 2^-37; two terms more take 28.7 us for 27.7 at 131072 x 64).  k is the nearest to t (1 + 2^-53.8) / (pi/2), and lost lies outside: |r| <= pi/4 + 2^-53.8 |t| + |lost|, below 0.8
+// up to angles of 2^45 (2^-43.7 there) and 1.05 at 2^50 (2^-34).
+__device__ __forceinline__ void cos_sin(double t, double lost, double& c, double& s) {
     const double at = fma(t, 0x1.45f306dc9c883p-1, 0x1.8p52), k = at - 0x1.8p52;         // (k in the last bits of the sum)
-    const double r = fma(-k, 0x1.1a62633145c07p-54, fma(-k, 0x1.921fb54442d18p+0, t)), z = r * r;
+    const double r = fma(-k, 0x1.1a62633145c07p-54, fma(-k, 0x1.921fb54442d18p+0, t)) + lost, z = r * r;
     double ps = -0x1.aa288026d8c33p-26, pc = 0x1.1c81d7955fe06p-29;
     ps = fma(ps, z, 0x1.71d9aa58557b2p-19);   pc = fma(pc, z, -0x1.27e25f7db439cp-22);
     ps = fma(ps, z, -0x1.a019fd9bd07dap-13);  pc = fma(pc, z, 0x1.a019ff53f3bf3p-16);
@@ -40,26 +41,57 @@ __device__ __forceinline__ void cos_sin(double t, double& c, double& s) {
     if (q & 2) s = -s;
     if ((q + 1) & 2) c = -c;
 }
-__device__ __forceinline__ void table_element(const TableArgs& a, double p, double f, float (&v)[4]) {
-    const double t = p * f, e = (fabs(p) > a.whole ? a.e2 : a.e1) * fabs(t);
+// An element from the rounded angle t = p f, with bounds in binary32, whose operations take half the time of binary64's: from E, c and s, an u each off, the sums of positive terms are 6u off at most; (1 + 8u)
+// above them they are at or above their formulas and less than 16u < 1e-6 from them (131072 x 64: 26 us, 32.6 in binary64 with the argument's multiple of pi/2 converted to a whole number).
+// False where that does not hold, and table_element has to form the element:
+//  - bounds below 2^-60 (angles next to 0 where c_cos or c_sin is 0 or u or m small): what is lost below 2^-126 on the way is less than 2^-28 of the others (factors up to 2^60);
+//  - angles from about 2^20 on: what the product left off, 2^-53 |t|, moves a table by as much, and a bound by as much of 1 + |cos| or 1 + |sin| (2^-33);
+//  - Gamma(1) below 2^-27: it moves a bound by 2 2^-53 |t| of E next to a multiple of pi/2 (2^-25 of E otherwise).
+__device__ __forceinline__ bool table_element_near(const TableArgs& a, int64_t n, double f, float (&v)[4]) {
+    const double p = (double)n, t = p * f, e = (fabs(p) > a.whole ? a.e2 : a.e1) * fabs(t);
     double c, s;
-    cos_sin(t, c, s);
+    cos_sin(t, 0.0, c, s);
     v[0] = (float)(a.m * c); v[1] = (float)(a.m * s);
-    // in binary32, whose operations take half the time of binary64's: from E, c and s, an u each off, the sums of positive terms are 6u off at most; (1 + 8u) above them they
-    // are at or above their formulas and less than 16u < 1e-6 from them (131072 x 64: 28.7 us, 32.6 in binary64 with the argument's multiple of pi/2 converted to a whole number).  From 2^-60 on
-    // (factors up to 2^60), where what is lost below 2^-126 on the way is less than 2^-28 of them; smaller ones, of angles next to 0 where c_cos or c_sin is 0 or u or m small, in binary64.
     const float ac = fabsf((float)c), as = fabsf((float)s), E = (float)e, e2 = 0.5f * E * E;
     const float bc = fminf(fminf(fmaf(as, E, e2), E), 1.f + ac), bs = fminf(fminf(fmaf(ac, E, e2), E), 1.f + as);
     v[2] = fmaf(a.q1[0], bc, a.q2[0] * ac) * (1.f + 0x1p-21f); v[3] = fmaf(a.q1[1], bs, a.q2[1] * as) * (1.f + 0x1p-21f);
-    if (!(a.quick && fminf(v[2], v[3]) >= 0x1p-60f)) {
-        const double ac = fabs(c), as = fabs(s), e2 = 0.5 * e * e;
-        const double bc = fmin(fmin(fma(as, e, e2), e), 1.0 + ac), bs = fmin(fmin(fma(ac, e, e2), e), 1.0 + as);
-        v[2] = up32g(fma(a.k1[0], bc, a.k2[0] * ac)); v[3] = up32g(fma(a.k1[1], bs, a.k2[1] * as));
+    return fminf(v[2], v[3]) >= 0x1p-60f && E < a.near;
+}
+__device__ __forceinline__ void table_element(const TableArgs& a, int64_t n, double f, float (&v)[4]) {
+    double p = (double)n, low = 0.0;                         // the position is p + low exactly
+    if (fabs(p) >= 0x1p53) {
+        if (p >= 0x1p63) p = 0x1.fffffffffffffp62;           // (2^63 is no int64)
+        low = (double)(n - (int64_t)p);
     }
+    const double t = p * f, e = (fabs(p) > a.whole || (fabs(p) == a.whole && p * low > 0.0) ? a.e2 : a.e1) * fabs(t);
+    double c, s;
+    cos_sin(t, fma(low, f, fma(p, f, -t)), c, s);
+    const double ac = fabs(c), as = fabs(s), e2 = 0.5 * e * e;
+    const double bc = fmin(fmin(fma(as, e, e2), e), 1.0 + ac), bs = fmin(fmin(fma(ac, e, e2), e), 1.0 + as);
+    v[0] = (float)(a.m * c); v[1] = (float)(a.m * s);
+    v[2] = up32g(fma(a.k1[0], bc, a.k2[0] * ac)); v[3] = up32g(fma(a.k1[1], bs, a.k2[1] * as));
     if (!(fabs(t) < 0x1p50)) { v[0] = v[1] = v[2] = v[3] = NAN; }
 }
+// The elements whose bits are set in `left` of VEC, one after the other (in line for each, they cost the common way registers: 2^20 x 16 48.6 us, 42.3 so); at(e, n, f): element e's position and frequency.
+template <int VEC, class At>
+__device__ __forceinline__ void table_elements_left(const TableArgs& a, unsigned left, float (&v)[VEC][4], At&& at) {
+#pragma unroll 1
+    while (left) {
+        const int e = __builtin_ctz(left);
+        left &= left - 1;
+        int64_t n;
+        double f;
+        at(e, n, f);
+        float w[4];
+        table_element(a, n, f, w);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k)
+#pragma unroll
+            for (int o = 0; o < 4; ++o) v[k][o] = k == e ? w[o] : v[k][o];
+    }
+}
 // A thread has VEC neighbouring frequencies of a position: 16-byte stores where rows are whole vectors.  What bounds long tables: their bytes (16 an element)
-// and, hardly less, 35 binary64 operations an element: 131072 x 64 in 27.7 us, 4.8 TB/s; one frequency a thread 46.
+// and, hardly less, 35 binary64 operations an element: 131072 x 64 in 26 us, 5.2 TB/s; one frequency a thread 46.
 template <int VEC>
 __global__ __launch_bounds__(256) void rope_tables(TableArgs a) {
     const unsigned per = (unsigned)a.half / VEC;
@@ -67,10 +99,12 @@ __global__ __launch_bounds__(256) void rope_tables(TableArgs a) {
     for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += stride) {
         const long r = n < (1L << 32) ? (long)((unsigned)i / per) : i / per;
         const int j = (int)(i - r * per) * VEC;
-        const double p = (double)(a.positions ? a.positions[r] : r);
+        const int64_t p = a.positions ? a.positions[r] : r;
         float v[VEC][4];
+        unsigned left = 0;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) table_element(a, p, (double)a.inv_freq[j + e], v[e]);
+        for (int e = 0; e < VEC; ++e) left |= table_element_near(a, p, (double)a.inv_freq[j + e], v[e]) ? 0u : 1u << e;
+        table_elements_left<VEC>(a, left, v, [&](int e, int64_t& at, double& f) __attribute__((always_inline)) { at = p; f = (double)a.inv_freq[j + e]; });
 #pragma unroll
         for (int o = 0; o < 4; ++o) {
             if (!a.out[o]) continue;
@@ -85,17 +119,23 @@ __global__ __launch_bounds__(256) void rope_tables_flat(TableArgs a) {
     for (long i = ((long)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += stride) {
         long r = n < (1L << 32) ? (long)((unsigned)i / (unsigned)a.half) : i / a.half;
         int j = (int)(i - r * a.half);
-        double p = (double)(a.positions ? a.positions[r] : r);
+        int64_t p = a.positions ? a.positions[r] : r;
         float v[4][4];
+        unsigned left = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (e > 0 && ++j == a.half) {
                 j = 0;
                 ++r;
-                if (r < a.npos) p = (double)(a.positions ? a.positions[r] : r);         // (what lies behind the last row is not stored)
+                if (r < a.npos) p = a.positions ? a.positions[r] : r;             // (what lies behind the last row is not stored)
             }
-            table_element(a, p, (double)a.inv_freq[j], v[e]);
+            left |= table_element_near(a, p, (double)a.inv_freq[j], v[e]) ? 0u : 1u << e;
         }
+        table_elements_left<4>(a, left, v, [&](int e, int64_t& at, double& f) __attribute__((always_inline)) {
+            const long k = i + e < n ? i + e : 0, row = k / a.half;
+            at = a.positions ? a.positions[row] : row;
+            f = (double)a.inv_freq[k - row * a.half];
+        });
 #pragma unroll
         for (int o = 0; o < 4; ++o) {
             if (!a.out[o]) continue;
@@ -652,11 +692,12 @@ int tao_bound_rope_tables(const int64_t* positions, const float* inv_freq, doubl
         a.k1[i] = widen(m * (a.m == 1.0 ? 1.0 + cu : (1.0 + u) * (1.0 + cu)));
         a.k2[i] = widen(m * (a.m == 1.0 ? cu : (1.0 + u) * cu + u));
     }
-    a.quick = true;
+    bool quick = a.e1 >= 0x1p-27;
     for (int i = 0; i < 2; ++i) {
         a.q1[i] = (float)a.k1[i]; a.q2[i] = (float)a.k2[i];
-        a.quick = a.quick && a.k1[i] <= 0x1p60 && a.k2[i] <= 0x1p60;
+        quick = quick && a.k1[i] <= 0x1p60 && a.k2[i] <= 0x1p60;
     }
+    a.near = quick ? (float)a.e1 * 0x1p20f : 0.f;
     // (tables of less than one element for each of the chip's threads: one a thread; 16640 x 63 8.9 us, four a thread 8.4, 2080 x 63 3.5 and 4.7)
     const bool vec = (half % 4 == 0 || npos * half >= 1L << 19) && aligned(cos_table, 16) && aligned(sin_table, 16) && aligned(tau_cos, 16) && aligned(tau_sin, 16);
     const long blocks = ((vec ? (npos * half + 3) / 4 : npos * half) + 255) / 256;

@@ -79,6 +79,44 @@ def test_tables_next_to_the_zeros(tao):
     assert_tables(tao.tao_bound_rope_tables(*cuda(f, p)), p, f)
 
 
+def test_tables_of_angles_whose_products_round(tao):
+    """Odd far positions and frequencies of 24 bits, so that p f has more than 53: what the product leaves off is part of every table and bound; positions that binary64 does not hold, up to the ends of int64."""
+    rng = np.random.default_rng(7)
+    f = np.array([1.0, 0.1, 1 / 3, 0.731, 0.999, -0.25], F)
+    for bits in (24, 28, 32, 34, 36, 40, 44, 45, 48, 49):
+        p = np.concatenate([rng.integers(2 ** (bits - 1), 2 ** bits, 24) | 1, [2 ** bits + 1, 2 ** bits - 3, -2 ** bits + 1]])
+        assert_tables_closely(tao, p, f)
+    k = np.arange(1, 200)
+    near = np.concatenate([(k * np.pi / 2).astype(F), (k * np.pi / 4).astype(F)])         # one of the two functions is next to 0 at p = 1, 3, 5
+    assert_tables_closely(tao, np.array([1, 3, 5, 999999999, 2 ** 36 + 1, 2 ** 40 - 3]), near)
+    for bits in (54, 58, 63):
+        p = rng.integers(2 ** (bits - 1), 2 ** bits - 1, 20) | 1
+        p = np.concatenate([p, -p])
+        assert_tables_closely(tao, p, (f[1:] * 2.0 ** (48 - bits)).astype(F))
+        assert_tables_closely(tao, p, (f[1:] * 2.0 ** (20 - bits)).astype(F))
+    ends = np.array([2 ** 63 - 1, 2 ** 63 - 512, 2 ** 63 - 513, 2 ** 63 - 1025, -2 ** 63, -2 ** 63 + 1, 2 ** 53, 2 ** 53 + 1, -2 ** 53 - 1])
+    assert_tables_closely(tao, ends, np.array([2.0 ** -14, 0.7 * 2.0 ** -14, 1e-10, 1e-19], F))
+
+
+def assert_tables_closely(tao, p, f, scale=1.0, model=None):
+    """As the header has it: the formula to |m| (2^-44 + 2^-53 |p f|), from angles of 2^20 on to |m| 2^-34, rounded once; bounds as everywhere."""
+    got, exact = tao.tao_bound_rope_tables(*cuda(f, p), scale=scale, model=model), rotary.rope_tables(p, f, scale, model)
+    far = np.abs(p.astype(L)[:, None] * f.astype(L)[None, :])
+    for g, e in zip(got[:2], exact[:2]):
+        assert_rounded(g.cpu().numpy(), e, abs(L(F(scale))) * np.where(far >= 2.0 ** 20, L(2) ** -34, L(2) ** -44 + L(2) ** -53 * far))
+    for g, e in zip(got[2:], exact[2:]):
+        assert_bound(g.cpu().numpy(), e)
+
+
+@pytest.mark.parametrize("u", [2.0 ** -30, 2.0 ** -53])
+def test_tables_of_finer_models(tao, u):
+    """Roundoffs far below binary32's: the angle's own rounding in binary64 would be as large as E."""
+    m = tao.FpModel(u=u)
+    p = np.array([0, 1, 5, 1001, 70001, 2 ** 24 + 1, 2 ** 31 - 1, 2 ** 40 + 1])
+    assert_tables_closely(tao, p, frequencies(40, 1e4), 1.1, m)
+    assert_tables_closely(tao, p, frequencies(40, 1e4), 1.0, m)
+
+
 def test_tables_beyond_their_range(tao):
     f = np.array([1.0, np.inf, np.nan, 3e38, -np.inf, 2.0 ** 50, 2.0 ** 49], F)
     c, s, tc, ts = (t.cpu().numpy() for t in tao.tao_bound_rope_tables(*cuda(f, np.array([1, 2]))))

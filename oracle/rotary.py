@@ -18,12 +18,14 @@ def _reduced(p, f):
     if not np.isfinite(f):
         return L(np.nan)
     num, den = float(f).as_integer_ratio()
-    t = (int(p) * num << 252) // den if den > 1 else int(p) * num << 252
+    num *= int(p)
+    t = (abs(num) << 252) // den                             # (of magnitudes: below 0 the two parts at the end would take from each other, and a small angle's bits with them)
     r = t % _TWO_PI
+    sign = 1 if num >= 0 else -1
     if r > _TWO_PI // 2:
-        r -= _TWO_PI
+        r, sign = _TWO_PI - r, -sign
     hi = r >> 190                                            # 64 bits at a time
-    return L(hi) * L(2) ** -62 + L(r - (hi << 190)) * L(2) ** -252
+    return sign * (L(hi) * L(2) ** -62 + L(r - (hi << 190)) * L(2) ** -252)
 
 
 def rope_tables(positions, inv_freq, scale=1.0, model=None):

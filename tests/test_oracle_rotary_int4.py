@@ -20,6 +20,21 @@ def test_reduction_of_far_angles():
     assert np.abs(c * c + s * s - 1).max() < 1e-17
 
 
+def test_small_negative_angles():
+    """The sine is odd, and next to 0 it is the angle, to all bits of an angle of any size and sign."""
+    f = np.array([1e-45, 1e-40, 1e-30, 2.0 ** -70, 1e-19, 3e-10, 0.25], F)
+    c, s, tc, ts = rotary.rope_tables([7, 70001], f)
+    c2, s2, tc2, ts2 = rotary.rope_tables([-7, -70001], f)
+    for a, b in ((c, c2), (s, -s2), (tc, tc2), (ts, ts2)):
+        assert np.array_equal(a, b)
+    angle = -np.array([[7], [70001]]).astype(L) * f[None, :5].astype(L)
+    assert (np.abs(s2[:, :5] / angle - 1) < 2.0 ** -60).all()
+    # angles a little below a multiple of 2 pi
+    near = np.nextafter((2 * np.pi * np.arange(1, 50)).astype(F), F(0))
+    s3 = rotary.rope_tables([1], near)[1]
+    assert (np.abs(s3 - np.sin(near.astype(L))) < 2.0 ** -58).all() and np.array_equal(s3, -rotary.rope_tables([-1], near)[1])
+
+
 @pytest.mark.parametrize("scale", [1.0, 1.25, -0.7])
 def test_tables_cover_executions(scale):
     rng = np.random.default_rng(3)

@@ -296,8 +296,9 @@ int tao_quantize_rows(const float *x, int8_t *q, float *scale, long rows, long c
  *     tau[i][j] = Gamma(K') (sum_k |A[i][k]| |w[j][k]| + |bias[j]|),     K' = K + 1, or K + 2 with a bias:
  * a product, at most K - 1 additions, the bias, and one rounding more where (q - z) scale is formed first or the scale is applied to a group's sum.
  * q - z is a whole number and exact; executions that round q scale and z scale apart are not covered.
- * y is the formula with an error of at most 15 u (sum_k |A||w| + |bias|), the last rounding among it (K <= 32: the formula in binary64, rounded once), which tau covers itself, so that alpha = 2 admits every execution that
- * tau covers.  exact <= tau <= exact (1 + 1e-6), or the next step where it is subnormal; tau is NaN where an operand is not finite, +inf beyond the binary32 range.
+ * y is the formula with an error of at most 15 2^-24 (sum_k |A||w| + |bias|), and of at most Gamma(K') of that sum where this is less, the last rounding among it (K <= 32, and models that leave no more than
+ * 3 2^-24: the formula in binary64, rounded once).  So tau covers y itself and alpha = 2 admits every execution that tau covers, under any model with Gamma(K') >= 2^-24 (below that even the formula's value
+ * rounded once lies outside).  exact <= tau <= exact (1 + 1e-6), or the next step where it is subnormal; tau is NaN where an operand is not finite, +inf beyond the binary32 range.
  * TAO_FLAG_UNDERFLOW_TERMS adds (K' + sum_k |A[i][k]| + sum_k |scale[j][k / group]|) 2^-149 (and takes the slower kernel of short reductions).
  * A: [M][K], row stride lda.  W: [N][(K + 1) / 2] bytes, row stride ldw bytes: column 2i in the low four bits of byte i, 2i + 1 in the high ones (those behind an odd K
  * are ignored).  scale: [N][G], zero: [N][G] whole numbers from 0 to 255 or NULL (8: the signed values -8 .. 7), contiguous, G = ceil(K / group).  group: a multiple of 32, or

@@ -15,7 +15,9 @@ struct Int4Sums { double sum, size, err; };
 // Tiles of columns and of tokens, whole blocks of the reduction and those of a group of wavefronts, and the last part if a block that is not whole follows (else -1), first workgroup
 // of the launch (a grid has fewer than 2^32 threads).
 struct Int4Grid { unsigned tiles, token_blocks; int blocks, share, tail; unsigned from; };
-constexpr double kInt4Spare = 14.0 * 0x1p-24;                // ... relative to the size, for the output to be taken
+// ... relative to the size, for the output to be taken: 14u at most, so that bounds stay within 1e-6; and never so much that the output, rounded, could lie farther off than tau (probabilistic
+// models of small lambda, and those of small u).  Models that leave less than kInt4Least, which ordinary tokens' err may reach, take the kernel of any size.
+constexpr double kInt4Spare = 14.0 * 0x1p-24, kInt4Least = 2.0 * 0x1p-24;
 
 struct Int4Args {
     const float* A; const unsigned char* W;
@@ -29,6 +31,7 @@ struct Int4Args {
     unsigned long per_group;                                 // column / 32 times this over 2^32 is its group (0 for one group; exact up to 2^20 columns)
     double gamma;                    // Gamma(K'), with the margins of the sums' roundings
     double uflow, terms;             // 2^-149 over Gamma(K') or 0, K'
+    double spare;                    // how much of its size an output of the tiles may be off before it is rounded
 };
 // The bound from the sum of magnitudes, rounded up.  NaN where an operand is not finite, as an infinite bound would admit every finite claim (sums of finite operands
 // stay inside the binary64 range).
@@ -92,11 +95,11 @@ __global__ __launch_bounds__(256) void int4_any(Int4Args p) {
     }
 }
 // Whether a tile's sums are not exact enough, or no numbers.  (A size of 0 is exact: blocks of zeros and scales of 0 add nothing to either, all others add to both.)
-__device__ __forceinline__ bool int4_open(const Int4Sums& v) { return !(v.size < INFINITY) || (v.size > 0.0 && v.err > kInt4Spare * v.size); }
+__device__ __forceinline__ bool int4_open(const Int4Args& p, const Int4Sums& v) { return !(v.size < INFINITY) || (v.size > 0.0 && v.err > p.spare * v.size); }
 // The wavefront forms those anew, one lane's after the other's.
 __device__ __forceinline__ void int4_settle(const Int4Args& p, bool mine, int i, int j, Int4Sums& v) {
     const int lane = threadIdx.x & (kWave - 1);
-    unsigned long long open = __ballot(mine && int4_open(v));
+    unsigned long long open = __ballot(mine && int4_open(p, v));
     while (open) {
         const int l = __builtin_ctzll(open);
         open &= open - 1;
@@ -112,8 +115,8 @@ __device__ __forceinline__ void int4_settle(const Int4Args& p, bool mine, int i,
 // products of a digit stay below 2^21; the digits are put together and scaled in binary64.
 // What truncation leaves off: at most one unit of every X, so with dmax >= |q - z| the sum of |X||q - z| lies within [exact - 128 dmax, exact] units: the bound takes the upper end, and
 //     err = sum over the blocks of |s| 2^(E - 29) 128 dmax
-// is how far it may lie above, and how far y may be off.  An output with err <= 14u size has exact <= size <= exact (1 + 14u), so tau, rounded up, is within 16.1u < 1e-6 of its formula, and
-// y, rounded once, within 15u of the sum of magnitudes; others (blocks whose largest activation is hundreds of times the usual one, while its weight is 0) are formed in binary64.
+// is how far it may lie above, and how far y may be off.  An output with err <= spare size <= 14u size has exact <= size <= exact (1 + 14u), so tau, rounded up, is within 16.1u < 1e-6 of its formula, and
+// y, rounded once, within 15u, and Gamma(K'), of the sum of magnitudes; others (blocks whose largest activation is hundreds of times the usual one, while its weight is 0) are formed in binary64.
 // For ordinary tokens err is about 0.5u size (largest activation of 128 about 3.5 times the mean, dmax twice the mean of |q - z|).
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 typedef int intx4 __attribute__((ext_vector_type(4)));
@@ -654,15 +657,16 @@ static int int4_setup(const float* A, const uint8_t* W, const float* scale, cons
     p.gamma = g * (1.0 + ((double)K + 64.0) * 0x1p-52) * kGuard;
     p.uflow = (md->flags & TAO_FLAG_UNDERFLOW_TERMS) ? 0x1p-149 * kGuard / p.gamma : 0.0;
     p.terms = (double)steps;
+    p.spare = std::min(kInt4Spare, g * (1.0 - 0x1p-20) - 0x1p-24 * (1.0 + 0x1p-20));
     return TAO_OK;
 }
 // What a call launches: tiles of up to `tokens` tokens in `parts` parts of the reduction (tokens 0: the kernel of any size), with digits formed beforehand for `slab` tokens at a time
 // (0: by the tiles themselves), and of those whether a workgroup has one wavefront's columns or two.
 struct Int4Plan { int tokens, parts; long slab; int nw, kw; };
 constexpr long kInt4Slab = 64L << 20;                        // bytes of digits that are kept at a time (a few tokens', where those are more)
-static Int4Plan int4_plan(long M, long N, long K, bool terms) {
+static Int4Plan int4_plan(long M, long N, long K, bool exact) {
     // (short reductions: a wavefront's lanes are hardly used, and what truncation leaves off would show next to the few roundings that the bound holds)
-    if (K <= 32 || K > (1L << 20) || terms) return {0, 1, 0, 1, 1};
+    if (K <= 32 || K > (1L << 20) || exact) return {0, 1, 0, 1, 1};
     // (Digits formed anew by every tile of 16 columns and eight tokens, or once, by a launch of their own.  us: 8 x 1024 over 8192 7.7 and 8.7, 8 x 4096 over 4096 10.5 and 14.9, 16 x 1024 over 2048 4.8 and 8.7,
     // 16 x 512 over 4096 6.9 and 8.8; where there are more than two tiles a compute unit, 8 x 512 over 16384 10.9 and 7.3; more than one of long reductions, 8 x 4096 over 6144 19.2 and 15.6,
     // 16 x 4096 over 4096 19.3 and 16.4; in long enough ones, 5 x 12288 over 4096 25.5 and 20.5.  Four tokens and fewer by tiles of theirs: 4096 over 12288 15.5 and 18.3.)
@@ -681,6 +685,8 @@ static Int4Plan int4_plan(long M, long N, long K, bool terms) {
     const long fit = kInt4Slab / ((K + kInt4Block - 1) / kInt4Block * kInt4Block * 8) / tokens;
     return {tokens, (int)parts, rows ? tokens * std::min(std::max(fit, 1L), token_blocks) : 0, nw, kw};
 }
+// Models whose bounds the tiles do not form, or whose tau does not cover what they may be off.
+static bool int4_exact(const Int4Args& p) { return p.uflow != 0.0 || p.spare < kInt4Least; }
 static size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 static size_t part_bytes(long M, long N, const Int4Plan& plan) { return plan.parts > 1 ? padded((size_t)plan.parts * (size_t)(M * N) * sizeof(Int4Sums)) : 0; }
 // Digits, then units.
@@ -795,7 +801,7 @@ int tao_bound_linear_int4(const float* A, const uint8_t* W, const float* scale, 
     if (!aligned(y, 4) || !aligned(tau, 4)) return TAO_ERR_ALIGN;
     const size_t need = tao_linear_int4_workspace_bytes(M, N, K);
     if (need > 0 && (!ws || !aligned(ws, 256) || ws_bytes < need)) return TAO_ERR_WORKSPACE;
-    const Int4Plan plan = int4_plan(M, N, K, p.uflow != 0.0);
+    const Int4Plan plan = int4_plan(M, N, K, int4_exact(p));
     hipStream_t st = (hipStream_t)stream;
     p.y = y; p.tau = tau;
     char* rest = (char*)ws + part_bytes(M, N, plan);
@@ -825,7 +831,7 @@ int tao_bound_check_linear_int4(const float* A, const uint8_t* W, const float* s
     if (!aligned(ws, 256) || ws_bytes < tao_bound_check_linear_int4_workspace_bytes(M, N, K)) return TAO_ERR_WORKSPACE;
     const CheckWorkspace w = carve_check_workspace(ws);
     hipStream_t st = (hipStream_t)stream;
-    const Int4Plan plan = int4_plan(M, N, K, p.uflow != 0.0);
+    const Int4Plan plan = int4_plan(M, N, K, int4_exact(p));
     p.part = (Int4Sums*)((char*)ws + padded(check_workspace_bytes()));
     if (n > 0) {
         const int rc2 = int4_launch(p, plan, (char*)p.part + std::max(part_bytes(M, N, plan), padded((size_t)n * sizeof(Int4Sums))), st);

@@ -177,6 +177,33 @@ def test_models(tao, model, K, group):
     assert_bound(tau.cpu().numpy(), int4.linear_int4(*o, model=m)[1])
 
 
+@pytest.mark.parametrize("lam", [0.2, 0.4, 0.5, 1.0, 2.0, 4.0])
+@pytest.mark.parametrize("M,N,K,group", [(3, 40, 33, 32), (8, 40, 128, 128), (8, 100, 224, 32), (3, 60, 1024, 128), (8, 8209, 200, 128), (2, 96, 12288, 128)])
+def test_outputs_are_covered_by_the_bound_of_any_lambda(tao, lam, M, N, K, group):
+    """Probabilistic bounds far below 15 u of the magnitudes, and tokens whose low bits all point the same way next to an activation, with a weight of 0, that makes a tile's whole numbers coarse: by 1 to 32 u of the
+    sum.  The output stays inside the bound, and alpha = 2 admits claims at either end of it.  (A bound of the formula is at least one rounding: Gamma(K') >= 2^-24.)"""
+    m = tao.FpModel(mode=1, lam=lam)
+    G, big = -(-K // group), 5
+    q, z = np.full((N, K), 15, np.uint8), np.zeros((N, G), np.uint8)
+    q[:, big::max(group, 128)] = 0
+    s = np.full((N, G), 0.37, F) * (1 + np.arange(N, dtype=F)[:, None] / N)
+    if K == 33:
+        s[:, 1] = 1e-20                                      # (one column: next to nothing)
+    for octave in (5, 6, 7, 8, 9, 10):
+        A = np.tile((1 + np.array([3, 1, 7, 3, 11], F) * F(2.0 ** -23))[np.arange(M) % 5, None], (1, K)).astype(F)
+        A[:, big::max(group, 128)] = 1.5 * 2.0 ** octave
+        y, tau = run(tao, A, q, s, group, z, None, model=m)
+        ye, te, size = int4.linear_int4(A, q, s, group, z, None, model=m)
+        assert_bound(tau.cpu().numpy(), te)
+        assert (np.abs(y.cpu().numpy().astype(L) - ye) <= np.maximum(te, np.abs(ye) * L(U)) * (1 + L(2) ** -20)).all(), "%d: %g u" % (octave, float((np.abs(y.cpu().numpy() - ye) / size).max() / U))
+        if te.min() < 2 * np.abs(ye).max() * U:
+            continue                                         # (claims of binary32 inside the bound: only its rounding would fit)
+        for end in (-1, 1):
+            claimed = (ye + end * (te - np.abs(ye) * L(U) * 1.01)).astype(F)       # rounded, they are inside
+            pf = tao.tao_bound_check_linear_int4(*cuda(A, int4.pack(q), s), group, cuda(claimed)[0], zero=cuda(z)[0], alpha=2.0, model=m)
+            assert pf["accept"] == 1, octave
+
+
 @pytest.mark.parametrize("M,N,K,group", [(3, 50, 96, 32), (9, 70, 257, 64), (20, 40, 512, 128)])
 @pytest.mark.parametrize("pad,at,pada,ata", [(0, 0, 0, 0), (1, 0, 3, 1), (3, 5, 0, 2), (16, 0, 4, 0), (16, 16, 4, 4), (7, 1, 1, 3), (4, 4, 2, 0)])
 def test_strides_and_addresses(tao, M, N, K, group, pad, at, pada, ata):

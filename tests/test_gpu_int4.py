@@ -447,3 +447,72 @@ def test_calls_on_two_streams(tao):
     torch.cuda.synchronize()
     for (y2, t2), pf in results:
         assert torch.equal(y, y2) and torch.equal(tau, t2) and tao.read_profile(pf)["accept"] == 1
+
+
+# ------------------------------------------------------------------ workspaces: digits (16 tokens, 64 columns), parts of the reduction, both
+
+WORKSPACES = [(16, 10300, 200, 128), (2, 96, 12288, 128), (5, 4200, 6200, 160)]
+
+
+@pytest.mark.parametrize("M,N,K,group", WORKSPACES)
+def test_two_streams_have_workspaces_of_their_own(tao, M, N, K, group):
+    """Products and checks of different operands enqueued in turn on two streams, each with the workspace that the binding keeps for its stream."""
+    assert tao.tao_linear_int4_workspace_bytes(M, N, K) > 0
+    streams, data, expect, got = [torch.cuda.Stream() for _ in range(2)], [], [], []
+    for n in range(2):
+        A, q, s, _, z, _ = operands(M, N, K, group, 40 + n, True)
+        data.append(cuda(A, int4.pack(q), s, z))
+        own = torch.empty(tao.tao_linear_int4_workspace_bytes(M, N, K), dtype=torch.uint8, device="cuda")
+        expect.append(tao.tao_bound_linear_int4(data[n][0], data[n][1], data[n][2], group, zero=data[n][3], ws=own))
+        assert_product(expect[n], A, q, s, group, z, None)
+    torch.cuda.synchronize()
+    for i in range(12):
+        n = i % 2
+        A, W, s, z = data[n]
+        with torch.cuda.stream(streams[n]):
+            got.append((n, tao.tao_bound_linear_int4(A, W, s, group, zero=z), tao.tao_bound_check_linear_int4(A, W, s, group, expect[n][0], zero=z, readback=False)))
+    torch.cuda.synchronize()
+    kept = [tao._ws_cache[(torch.cuda.current_device(), stream.cuda_stream)] for stream in streams]
+    assert min(k.numel() for k in kept) >= tao.tao_bound_check_linear_int4_workspace_bytes(M, N, K) and kept[0].data_ptr() != kept[1].data_ptr()
+    for n, (y, tau), pf in got:
+        assert torch.equal(y, expect[n][0]) and torch.equal(tau, expect[n][1])
+        pf = tao.read_profile(pf)
+        assert pf["accept"] == 1 and pf["max_rel"] == 0.0 and pf["n"] == M * N
+
+
+@pytest.mark.parametrize("M,N,K,group", WORKSPACES)
+def test_captured_products_keep_their_workspaces(tao, M, N, K, group):
+    """Two graphs of a product and its check on one stream, replayed in turn on new inputs, with eager products between the replays that use the shared workspace and make it grow."""
+    A, q, s, _, z, _ = operands(M, N, K, group, 50, True)
+    W, sd, zd = cuda(int4.pack(q), s, z)
+    inputs = [torch.from_numpy((A * F(f)).astype(F)).cuda() for f in (1.0, -0.75, 3.1)]
+    expect = [tao.tao_bound_linear_int4(a, W, sd, group, zero=zd) for a in inputs]
+    assert_product(expect[1], (A * F(-0.75)).astype(F), q, s, group, z, None)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graphs = []
+    with torch.cuda.stream(stream):
+        for n in range(2):
+            a, claim = inputs[0].clone(), expect[0][0].clone()
+            tao.tao_bound_check_linear_int4(a, W, sd, group, claim, zero=zd, readback=False)
+            stream.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                out = tao.tao_bound_linear_int4(a, W, sd, group, zero=zd)
+                pf = tao.tao_bound_check_linear_int4(a, W, sd, group, claim, zero=zd, readback=False)
+            graphs.append((graph, a, claim, out, pf))
+    torch.cuda.current_stream().wait_stream(stream)
+    for i in range(6):
+        for n, (graph, a, claim, out, pf) in enumerate(graphs):
+            k = (i + n) % 3
+            a.copy_(inputs[k])
+            claim.copy_(expect[k][0])
+            if i == 4:
+                claim[M - 1, N - 1] = float("nan")
+            graph.replay()
+            between = tao.tao_bound_linear_int4(inputs[(k + 1) % 3].repeat(1 + i, 1), W, sd, group, zero=zd)       # eager, on the same stream, of more tokens each time
+            torch.cuda.synchronize()
+            assert torch.equal(out[0], expect[k][0]) and torch.equal(out[1], expect[k][1])
+            assert tao.read_profile(pf)["violations"] == (1 if i == 4 else 0)
+            if i == 0:
+                assert torch.equal(between[0], expect[(k + 1) % 3][0])

@@ -142,3 +142,15 @@ def test_int4_check_refusals(tao):
     assert call(claimed=NUL) == call(out=NUL) == tao.ERR_NULL
     assert call(claimed=ODD) == call(y_ref=ODD) == call(out=FOUR) == tao.ERR_ALIGN
     assert call(ws=NUL) == call(bytes=need - 1) == call(ws=ctypes.c_void_p(0x100080)) == tao.ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("M,N,K", [(16, 10300, 200), (2, 96, 12288), (5, 4200, 6200)])
+def test_int4_workspace_refusals(tao, M, N, K):
+    """Products that take digits, parts of the reduction, or both: their workspace missing, short and off its alignment."""
+    L = tao.lib()
+    need, check = L.tao_linear_int4_workspace_bytes(M, N, K), L.tao_bound_check_linear_int4_workspace_bytes(M, N, K)
+    assert 0 < need < check
+    for ws, size in ((NUL, need), (NUL, 0), (P, need - 1), (P, 0), (ctypes.c_void_p(0x100080), need)):
+        assert L.tao_bound_linear_int4(P, P, P, NUL, 128, NUL, P, P, M, N, K, K, K // 2, N, None, ws, size, None) == tao.ERR_WORKSPACE
+    for ws, size in ((NUL, check), (P, check - 1), (P, need), (ctypes.c_void_p(0x100080), check)):
+        assert L.tao_bound_check_linear_int4(P, P, P, NUL, 128, NUL, NUL, P, M, N, K, K, K // 2, N, 1.0, 1e-12, None, P, ws, size, None) == tao.ERR_WORKSPACE

@@ -516,3 +516,82 @@ def test_captured_products_keep_their_workspaces(tao, M, N, K, group):
             assert tao.read_profile(pf)["violations"] == (1 if i == 4 else 0)
             if i == 0:
                 assert torch.equal(between[0], expect[(k + 1) % 3][0])
+
+
+# ------------------------------------------------------------------ the borders of digits that are formed once (and of joined parts): every shape of tile
+
+ROWS = [(8, 8209, 130, 32), (16, 10300, 200, 128), (40, 11000, 130, 64), (100, 10000, 129, 128), (5, 4200, 6200, 160)]
+JOINED = [(2, 96, 12288, 128), (24, 2100, 8300, 128)]
+
+
+@pytest.mark.parametrize("M,N,K,group", ROWS + JOINED)
+@pytest.mark.parametrize("zero", [False, True])
+def test_larger_products_whose_operands_end_where_their_memory_ends(tao, M, N, K, group, zero):
+    assert tao.tao_linear_int4_workspace_bytes(M, N, K) > 0
+    A, q, s, _, z, b = o = operands(M, N, K, group, 3, zero, True)
+    expect = run(tao, *o)
+    assert_product(expect, *o)
+    got = tao.tao_bound_linear_int4(at_the_end(A), at_the_end(int4.pack(q)), at_the_end(s), group, zero=None if z is None else at_the_end(z), bias=at_the_end(b))
+    assert torch.equal(got[0], expect[0]) and torch.equal(got[1], expect[1])
+
+
+def strided_rows(t, step, at=0):
+    """A copy of t whose rows lie `step` elements apart; what lies between is not touched."""
+    return torch.empty(at + len(t) * step, dtype=t.dtype, device="cuda").as_strided(t.shape, (step, 1), at).copy_(t)
+
+
+@pytest.mark.parametrize("M,N,K,group", ROWS[:3] + ROWS[4:] + JOINED[:1])
+def test_larger_products_beyond_32_bits(tao, M, N, K, group):
+    """Rows of A, of W, and of the outputs and claims so far apart that the last ones lie more than 2^31 elements on."""
+    assert tao.tao_linear_int4_workspace_bytes(M, N, K) > 0
+    A, q, s, _, z, b = operands(M, N, K, group, 4, True, True)
+    Ad, Wd, sd, zd, bd = cuda(A, int4.pack(q), s, z, b)
+    expect = tao.tao_bound_linear_int4(Ad, Wd, sd, group, zero=zd, bias=bd)
+    for a, w in ((strided_rows(Ad, 2 ** 31 // M + 2 ** 20), Wd), (Ad, strided_rows(Wd, 2 ** 31 // N + 2 ** 18, 16))):
+        got = tao.tao_bound_linear_int4(a, w, sd, group, zero=zd, bias=bd)
+        assert torch.equal(got[0], expect[0]) and torch.equal(got[1], expect[1])
+        del a, w
+    step = 2 ** 31 // M + 2 ** 20
+    assert (M - 1) * step > 2 ** 31 - 2 ** 31 // M
+    y, tau = strided_rows(0 * expect[0], step), strided_rows(0 * expect[0], step)
+    product, check = outputs_through_the_c_abi(tao, Ad, Wd, sd, zd, bd, group, y, tau, step)
+    assert product() == 0 and torch.equal(y, expect[0]) and torch.equal(tau, expect[1])
+    y[M - 1, N - 1] += 2 * tau[M - 1, N - 1]
+    pf = check(y)
+    assert pf["n"] == M * N and pf["violations"] == 1
+
+
+def outputs_through_the_c_abi(tao, A, W, s, z, b, group, y, tau, ldy):
+    """The product into rows ldy apart, and the check of claims laid out like that."""
+    (M, K), N = A.shape, len(W)
+    ws = torch.empty(max(256, tao.tao_bound_check_linear_int4_workspace_bytes(M, N, K)), dtype=torch.uint8, device="cuda")
+    front = [t.data_ptr() if t is not None else None for t in (A, W, s, z)] + [group, None if b is None else b.data_ptr()]
+    dims = (M, N, K, K, (K + 1) // 2, ldy)
+    L = tao.lib()
+
+    def product():
+        return L.tao_bound_linear_int4(*front, y.data_ptr(), tau.data_ptr(), *dims, None, ws.data_ptr(), ws.numel(), tao._stream())
+
+    def check(claimed):
+        out = tao.new_profile_buffer(A.device)
+        assert L.tao_bound_check_linear_int4(*front, None, claimed.data_ptr(), *dims, 1.0, 1e-12, None, out.data_ptr(), ws.data_ptr(), ws.numel(), tao._stream()) == 0
+        return tao.read_profile(out)
+    return product, check
+
+
+@pytest.mark.parametrize("M,N,K,group", ROWS + JOINED + [(20000, 48, 1000, 64)])
+def test_larger_products_into_wide_rows(tao, M, N, K, group):
+    """Outputs in rows of N + 9 elements, claims checked there too; what lies between stays as it was.  The last size goes through in slabs of tokens."""
+    assert tao.tao_linear_int4_workspace_bytes(M, N, K) > 0
+    A, q, s, _, z, b = operands(M, N, K, group, 5, True, True)
+    Ad, Wd, sd, zd, bd = cuda(A, int4.pack(q), s, z, b)
+    expect = tao.tao_bound_linear_int4(Ad, Wd, sd, group, zero=zd, bias=bd)
+    y, tau = torch.full((M, N + 9), 7.0, device="cuda"), torch.full((M, N + 9), 7.0, device="cuda")
+    product, check = outputs_through_the_c_abi(tao, Ad, Wd, sd, zd, bd, group, y, tau, N + 9)
+    assert product() == 0 and torch.equal(y[:, :N], expect[0]) and torch.equal(tau[:, :N], expect[1])
+    assert bool((y[:, N:] == 7).all()) and bool((tau[:, N:] == 7).all())
+    at = (0, M // 2, M - 1)
+    for i in at:
+        y[i, N - 1] += 2 * tau[i, N - 1]
+    pf = check(y)
+    assert pf["n"] == M * N and pf["violations"] == len(set(at))

@@ -595,3 +595,21 @@ def test_larger_products_into_wide_rows(tao, M, N, K, group):
         y[i, N - 1] += 2 * tau[i, N - 1]
     pf = check(y)
     assert pf["n"] == M * N and pf["violations"] == len(set(at))
+
+
+def test_more_outputs_than_a_launch_has_wavefronts_for(tao):
+    """The kernel of any size and the check that joins: their wavefronts and lanes take a second output, in a last trip that is not whole."""
+    M, N, K, seam = 7, 42859, 8, 262144
+    assert seam < M * N < 2 * seam
+    A, q, s, _, z, b = operands(M, N, K, K, 6, True, True)
+    got = run(tao, A, q, s, K, z, b)
+    cols = np.concatenate([np.arange(40), np.arange(seam // M - 40, seam // M + 40), np.arange(N - 40, N)])       # (outputs go out column by column)
+    assert_product([t[:, torch.from_numpy(cols).cuda()] for t in got], A, q[cols], s[cols], K, z[cols], b[cols])
+    y, tau = got
+    claimed = y.clone().view(-1)
+    at = torch.tensor([0, seam - 1, seam, M * N - 1], device="cuda")
+    claimed[at] += 3 * tau.view(-1)[at]
+    claimed = claimed.view(M, N)
+    pf = tao.tao_bound_check_linear_int4(*cuda(A, int4.pack(q), s), K, claimed, zero=cuda(z)[0], bias=cuda(b)[0])
+    assert pf["violations"] == 4
+    assert_profile_equal(pf, oracle.check_and_profile(claimed.cpu().numpy(), y.cpu().numpy(), tau.cpu().numpy()))

@@ -462,3 +462,49 @@ def test_refusals_of_the_binding(tao):
                 lambda: tables(gamma, npos=-1), lambda: check(xd, cd, sd, xd, alpha=-1.0), lambda: call(xd, cd, sd, eps=-1.0)):
         with pytest.raises((tao.TaoError, RuntimeError)):
             bad()
+
+
+# ------------------------------------------------------------------ more heads, and longer tables, than a launch has lanes for at once
+
+@pytest.mark.parametrize("T,d,rot,interleaved", [(70001, 264, 264, False), (70001, 264, 136, True), (131201, 136, 128, False), (262301, 128, 128, False), (524401, 64, 32, False), (1048701, 32, 32, True), (70001, 258, 258, False),
+                                                 (70001, 130, 66, False), (1048701, 14, 6, True), (66001, 520, 512, False)])
+def test_more_heads_than_a_launch_has_lanes_for(tao, T, d, rot, interleaved):
+    """Every kernel's lanes take a second head, in a last trip that is not whole: the first heads, those next to the seam and the last ones against the oracle; then the check of claims that leave their bounds here and there."""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    npos = 501
+    x = torch.randn((T, 1, d), generator=g, device="cuda")
+    c, s = (torch.rand((npos, rot // 2), generator=g, device="cuda") * 2 - 1 for _ in range(2))
+    gamma = 1 + 0.1 * torch.randn(d, generator=g, device="cuda")
+    positions = torch.randint(0, npos, (T,), generator=g, device="cuda")
+    k = dict(gamma=gamma, positions=positions, interleaved=interleaved)
+    y, tau = tao.tao_bound_norm_rope(x, c, s, **k)
+    lanes = next(n for n in (4, 8, 16, 32, 64) if d <= 8 * n or n == 64) if d % 8 == 0 and d <= 512 else next(n for n in (4, 8, 16, 32, 64) if d <= 4 * n or n == 64)
+    seam = 16384 * (256 // lanes)
+    assert seam < T < 2 * seam
+    rows = torch.cat([torch.arange(40), torch.arange(seam - 40, seam + 40), torch.arange(T - 40, T), torch.randint(0, T, (100,))])
+    assert int(rows.max()) < T
+    rows = rows.cuda()
+    e = rotary.norm_rope(x[rows].cpu().numpy(), c.cpu().numpy(), s.cpu().numpy(), rot, gamma_q=gamma.cpu().numpy(), positions=positions[rows].cpu().numpy(), interleaved=interleaved)
+    assert_heads((y[rows], tau[rows]), e, None, rot)
+    f = torch.tensor([0.0, 0.0, 0.5, -0.9, 0.0], device="cuda")[torch.arange(y.numel(), device="cuda") % 5].view(y.shape)
+    claimed = (y.double() + f.double() * tau.double()).float()
+    claimed[[0, seam - 1, seam, T - 1], 0, 1] += 3 * tau[[0, seam - 1, seam, T - 1], 0, 1]
+    pf = tao.tao_bound_check_norm_rope(x, c, s, claimed, **k)
+    assert pf["violations"] == 4
+    assert_profile_equal(pf, oracle.check_and_profile(claimed.cpu().numpy(), y.cpu().numpy(), tau.cpu().numpy(), 1.0, 1e-12))
+
+
+@pytest.mark.parametrize("npos,half,at", [(262209, 64, 0), (270001, 63, 0), (70001, 63, 1)])
+def test_longer_tables_than_a_launch_has_lanes_for(tao, npos, half, at):
+    """Vectors of whole rows, vectors over the ends of rows, and elements from an address that fits no vector."""
+    f, n = frequencies(half), npos * half
+    whole = [torch.full((n + 8,), 7.0, device="cuda") for _ in range(4)]
+    views = [w[at:at + n].view(npos, half) for w in whole]
+    got = tao.tao_bound_rope_tables(cuda(f)[0], npos=npos, cos=views[0], sin=views[1], tau_cos=views[2], tau_sin=views[3])
+    seam = 16384 * 256 * (1 if at else 4) // half
+    assert seam < npos < 2 * seam
+    rows = np.concatenate([np.arange(20), np.arange(seam - 20, seam + 20), np.arange(npos - 20, npos), np.random.default_rng(1).integers(0, npos, 60)])
+    assert rows.max() < npos
+    assert_tables([t[torch.from_numpy(rows).cuda()] for t in got], rows, f)
+    for w in whole:
+        assert bool((w[:at] == 7).all()) and bool((w[at + n:] == 7).all())

@@ -698,7 +698,7 @@ static int int4_launch_shape(void (*whole)(Int4Args, Int4Grid, Rest...), void (*
                              const Int4Args& p, int parts, hipStream_t st, Rest... rest) {
     const long tiles = (p.N + SH::COLUMNS - 1) / SH::COLUMNS, token_blocks = (p.M + SH::TOKENS - 1) / SH::TOKENS;
     const __int128 grid = (__int128)((tiles + 7) / 8 * 8) * token_blocks;
-    if (grid >= (1L << 31)) return TAO_ERR_SHAPE;
+    if (grid >= (1L << 32)) return TAO_ERR_SHAPE;            // (none that the arguments' checks let through: 2^31 at most, of one tile of columns)
     static OncePerDevice once;
     const hipError_t e = once.run([&] {
         for (const auto kernel : {whole, halves, quarters}) {

@@ -1,6 +1,9 @@
 """Refusals of the rotary tables, the norm and rotation of heads and the product with 4-bit weights: status codes returned before anything is
 enqueued (no GPU), and their workspace queries."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 
@@ -154,3 +157,21 @@ def test_int4_workspace_refusals(tao, M, N, K):
         assert L.tao_bound_linear_int4(P, P, P, NUL, 128, NUL, P, P, M, N, K, K, K // 2, N, None, ws, size, None) == tao.ERR_WORKSPACE
     for ws, size in ((NUL, check), (P, check - 1), (P, need), (ctypes.c_void_p(0x100080), check)):
         assert L.tao_bound_check_linear_int4(P, P, P, NUL, 128, NUL, NUL, P, M, N, K, K, K // 2, N, 1.0, 1e-12, None, P, ws, size, None) == tao.ERR_WORKSPACE
+
+
+def test_int4_takes_every_number_of_tokens_that_it_says():
+    """2^31 - 1 tokens by one column are no bad shape.  (Their operands fit no card: in a process without devices, where the call ends before its launch.)"""
+    code = """
+import ctypes, torch
+import paper_2510_16028_amd as t
+assert torch.cuda.device_count() == 0
+P = ctypes.c_void_p(0x100000)
+for M, N, K in ((2 ** 31 - 1, 1, 33), (2 ** 31 - 1, 31, 127), (2 ** 31 - 8, 1, 64), (1, 2 ** 31 - 1, 64)):
+    assert t.lib().tao_linear_int4_workspace_bytes(M, N, K) == 0
+    print(t.lib().tao_bound_linear_int4(P, P, P, None, K, None, P, P, M, N, K, K, (K + 1) // 2, N, None, None, 0, None))
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, env=dict(os.environ, HIP_VISIBLE_DEVICES="-1", ROCR_VISIBLE_DEVICES="-1"), capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    import paper_2510_16028_amd as tao
+    assert r.stdout.split() == [str(tao.ERR_LAUNCH)] * 4

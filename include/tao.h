@@ -299,7 +299,8 @@ int tao_quantize_rows(const float *x, int8_t *q, float *scale, long rows, long c
  * y is the formula with an error of at most 15 2^-24 (sum_k |A||w| + |bias|), and of at most Gamma(K') of that sum where this is less, the last rounding among it (K <= 32, and models that leave no more than
  * 3 2^-24: the formula in binary64, rounded once).  So tau covers y itself and alpha = 2 admits every execution that tau covers, under any model with Gamma(K') >= 2^-24 (below that even the formula's value
  * rounded once lies outside).  exact <= tau <= exact (1 + 1e-6), or the next step where it is subnormal; tau is NaN where an operand is not finite, +inf beyond the binary32 range.
- * TAO_FLAG_UNDERFLOW_TERMS adds (K' + sum_k |A[i][k]| + sum_k |scale[j][k / group]|) 2^-149 (and takes the slower kernel of short reductions).
+ * TAO_FLAG_UNDERFLOW_TERMS adds (K' + sum_k |A[i][k]| + sum_k |scale[j][k / group]|) 2^-149 (and takes the slower kernel of short reductions).  Outputs of columns whose codes all equal their zero points
+ * are formed one after the other: leave padding out of N.
  * A: [M][K], row stride lda.  W: [N][(K + 1) / 2] bytes, row stride ldw bytes: column 2i in the low four bits of byte i, 2i + 1 in the high ones (those behind an odd K
  * are ignored).  scale: [N][G], zero: [N][G] whole numbers from 0 to 255 or NULL (8: the signed values -8 .. 7), contiguous, G = ceil(K / group).  group: a multiple of 32, or
  * any number from K on (one scale a row).  bias: [N] or NULL.  y, tau: [M][N], row stride ldy; either may be NULL (not stored).  Any strides and addresses; rows of W
@@ -529,7 +530,7 @@ int tao_bound_rope_tables(const int64_t *positions, const float *inv_freq, doubl
  *     tau_a = |x_a g_a| (k C + r tau_cos) + |x_b g_b| (k S + r tau_sin),  k = Gamma(2) (r + F) + F,  C = |cos| + tau_cos,  S = |sin| + tau_sin
  *     (tau_b with a and b exchanged),  tau = F |x g|  on the others.
  * Without a norm and without the tables' bounds this is tao_bound_rope's bound.  y is the formula in binary64, rounded once, so no re-executed output is needed, and
- * alpha = 2 admits every execution that tau covers.  tau is at or above its formula's value and within 1e-6 of it; a head whose bound is not finite, an element whose
+ * alpha = 2 admits every execution that tau covers (under models whose u, or without a norm Gamma(2), is at least 2^-24).  tau is at or above its formula's value and within 1e-6 of it; a head whose bound is not finite, an element whose
  * operands are not, and the rotated elements of a token whose position lies outside the tables (y too) get NaN.  TAO_FLAG_UNDERFLOW_TERMS adds 2 2^-149 to rotated elements.
  * x: head h of token t at x + t ldt + h ldh; heads_q heads with gain gamma_q, then heads_k with gamma_k (d elements each, or NULL: 1), as a fused projection leaves queries and keys.
  * y, tau: at t ldyt + h ldyh, without overlap; either may be NULL (not stored).  cos_table, sin_table: [npos][rot/2] contiguous; tau_cos, tau_sin: their bounds, both or neither (NULL: 0).

@@ -94,7 +94,8 @@ __global__ __launch_bounds__(256) void int4_any(Int4Args p) {
         }
     }
 }
-// Whether a tile's sums are not exact enough, or no numbers.  (A size of 0 is exact: blocks of zeros and scales of 0 add nothing to either, all others add to both.)
+// Whether a tile's sums are not exact enough, or no numbers.  (A size of 0 is exact: blocks of zeros and scales of 0 add nothing to either, all others add to both; so a column
+// whose codes all equal their zero points has a size of err alone, and is open: 16 x 4096 over 12288 with 64 such columns together 552 us, 26 without, with every sixteenth 61.)
 __device__ __forceinline__ bool int4_open(const Int4Args& p, const Int4Sums& v) { return !(v.size < INFINITY) || (v.size > 0.0 && v.err > p.spare * v.size); }
 // The wavefront forms those anew, one lane's after the other's.
 __device__ __forceinline__ void int4_settle(const Int4Args& p, bool mine, int i, int j, Int4Sums& v) {

@@ -24,7 +24,7 @@ struct TableArgs {
 // cos and sin of t + lost, |t| < 2^50, lost what t's own rounding left off: t less the nearest multiple k of pi/2 (two parts of pi/2 in fused steps: the first difference is exact, as t
 // and k times the first part are multiples of 2^-52 where k is not 0), then lost, which next to a multiple of pi/2 may be most of what remains; then polynomials on |r| <= pi/4 of degree 11 and 12,
 // for (sin r / r - 1) / r^2 and (cos r - 1 + r^2/2) / r^4 fitted in extended precision at 400 Chebyshev points of r^2 with weights that even out the largest errors: 2^-45 relatively
-// (Taylor's of that degree 2^-37; two terms more take 28.7 us for 27.7 at 131072 x 64).  k is the nearest to t (1 + 2^-53.8) / (pi/2), and lost lies outside: |r| <= pi/4 + 2^-53.8 |t| + |lost|, below 0.8
+// (Taylor's of that degree 2^-37; two terms more took 1 us of 28 at 131072 x 64).  k is the nearest to t (1 + 2^-53.8) / (pi/2), and lost lies outside: |r| <= pi/4 + 2^-53.8 |t| + |lost|, below 0.8
 // up to angles of 2^45 (2^-43.7 there) and 1.05 at 2^50 (2^-34).
 __device__ __forceinline__ void cos_sin(double t, double lost, double& c, double& s) {
     const double at = fma(t, 0x1.45f306dc9c883p-1, 0x1.8p52), k = at - 0x1.8p52;         // (k in the last bits of the sum)
@@ -72,7 +72,7 @@ __device__ __forceinline__ void table_element(const TableArgs& a, int64_t n, dou
     v[2] = up32g(fma(a.k1[0], bc, a.k2[0] * ac)); v[3] = up32g(fma(a.k1[1], bs, a.k2[1] * as));
     if (!(fabs(t) < 0x1p50)) { v[0] = v[1] = v[2] = v[3] = NAN; }
 }
-// The elements whose bits are set in `left` of VEC, one after the other (in line for each, they cost the common way registers: 2^20 x 16 48.6 us, 42.3 so); at(e, n, f): element e's position and frequency.
+// The elements whose bits are set in `left` of VEC, one after the other (in line for each, they cost the common way registers: 2^20 x 16 48.6 us, 42.7 so); at(e, n, f): element e's position and frequency.
 template <int VEC, class At>
 __device__ __forceinline__ void table_elements_left(const TableArgs& a, unsigned left, float (&v)[VEC][4], At&& at) {
 #pragma unroll 1
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void rope_tables(TableArgs a) {
         }
     }
 }
-// Rows of other lengths: four neighbouring elements of the whole table a thread, over the ends of rows (131072 x 63 29.0 us, one element a thread 35.7; 2^23 x 1 34.4, 39.2).
+// Rows of other lengths: four neighbouring elements of the whole table a thread, over the ends of rows (131072 x 63 25.3 us; one element a thread 35.7 where this took 29.0, 2^23 x 1 39.2 and 34.4).
 __global__ __launch_bounds__(256) void rope_tables_flat(TableArgs a) {
     const long n = a.npos * a.half, stride = (long)gridDim.x * 1024;
     for (long i = ((long)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += stride) {

@@ -516,8 +516,8 @@ int tao_bound_check_rope(const float *x, const float *cos_table, const float *si
  *     cos_table[r][j] = m cos(p_r f_j),  sin_table[r][j] = m sin(p_r f_j),
  *     E = Gamma(d) |p f|, d = 1, or 2 where |p| > 1/u (p is rounded too);
  *     tau_cos = |m| B' [+ u |m| (|cos| + B') for m != 1],  B' = B + c_cos u (|cos| + B),  B = min(|sin| E + E^2/2, E, 1 + |cos|),   tau_sin likewise with c_sin.
- * tau covers programs that form the angle in binary32, whose error grows with it, and those that form it in more bits.  The tables are the formula in binary64 (to |m| (2^-44 + 2^-53 |p f|), and to
- * |m| 2^-34 for angles from 2^24 on), rounded once; tau is at or above its formula's value and within 1e-6 of it.  m is rounded to binary32 first, as the operator does.  Angles from 2^50 on, and frequencies that are no numbers, give NaN.
+ * tau covers programs that form the angle in binary32, whose error grows with it, and those that form it in more bits.  The tables are the formula in binary64 (to |m| 2^-44, for angles from 2^45 on
+ * to |m| 2^-34), rounded once; tau is at or above its formula's value and within 1e-6 of it.  m is rounded to binary32 first, as the operator does.  Angles from 2^50 on, and frequencies that are no numbers, give NaN.
  * positions: [npos] or NULL (0, 1, 2, ...).  inv_freq: [half].  Outputs: [npos][half] contiguous; any of the four may be NULL (not stored).
  * TAO_ERR_SHAPE for a scale that is not finite, half or npos >= 2^31 and npos half >= 2^40; TAO_ERR_ALIGN also for positions off 8 bytes. */
 int tao_bound_rope_tables(const int64_t *positions, const float *inv_freq, double scale, float *cos_table, float *sin_table,

@@ -18,7 +18,7 @@ struct TableArgs {
     double m, e1, e2, whole;         // Gamma(1), Gamma(2); positions up to `whole` are not rounded
     double k1[2], k2[2];             // of cos, of sin
     float q1[2], q2[2];              // the same in binary32
-    float near;                      // E up to which bounds are formed from those: Gamma(1) 2^24, or 0
+    float near;                      // E up to which bounds are formed from those: Gamma(1) 2^45, or 0
 };
 
 // cos and sin of t + lost, |t| < 2^50, lost what t's own rounding left off: t less the nearest multiple k of pi/2 (two parts of pi/2 in fused steps: the first difference is exact, as t
@@ -41,12 +41,12 @@ __device__ __forceinline__ void cos_sin(double t, double lost, double& c, double
     if (q & 2) s = -s;
     if ((q + 1) & 2) c = -c;
 }
-// An element from the rounded angle t = p f, with bounds in binary32, whose operations take half the time of binary64's: from E, c and s, an u each off, the sums of positive terms are 6u off at most; (1 + 8u)
+// An element from the angle t = p f, with bounds in binary32, whose operations take half the time of binary64's: from E, c and s, an u each off, the sums of positive terms are 6u off at most; (1 + 8u)
 // above them they are at or above their formulas and less than 16u < 1e-6 from them (131072 x 64: 26 us, 32.6 in binary64 with the argument's multiple of pi/2 converted to a whole number).
 // False where that does not hold, and table_element has to form the element:
 //  - bounds below 2^-60 (angles next to 0 where c_cos or c_sin is 0 or u or m small): what is lost below 2^-126 on the way is less than 2^-28 of the others (factors up to 2^60);
-//  - angles from about 2^24 on (2^23 of positions that are rounded): what the product left off, 2^-53 |t|, moves a table by as much, and a bound by as much of 1 + |cos| or 1 + |sin| (2^-29);
-//  - Gamma(1) below 2^-27: it moves a bound by 2 2^-53 |t| of E next to a multiple of pi/2 (2^-25 of E otherwise).
+//  - positions from 2^29 on: below, p f has 53 bits at most and is exact; there what the product leaves off, 2^-53 |t|, moves tables, bounds of 1 + |cos| or 1 + |sin|, and those next to a multiple of pi/2;
+//  - angles from about 2^45 on, which may be none (2^50).
 __device__ __forceinline__ bool table_element_near(const TableArgs& a, int64_t n, double f, float (&v)[4]) {
     const double p = (double)n, t = p * f, e = (fabs(p) > a.whole ? a.e2 : a.e1) * fabs(t);
     double c, s;
@@ -55,7 +55,7 @@ __device__ __forceinline__ bool table_element_near(const TableArgs& a, int64_t n
     const float ac = fabsf((float)c), as = fabsf((float)s), E = (float)e, e2 = 0.5f * E * E;
     const float bc = fminf(fminf(fmaf(as, E, e2), E), 1.f + ac), bs = fminf(fminf(fmaf(ac, E, e2), E), 1.f + as);
     v[2] = fmaf(a.q1[0], bc, a.q2[0] * ac) * (1.f + 0x1p-21f); v[3] = fmaf(a.q1[1], bs, a.q2[1] * as) * (1.f + 0x1p-21f);
-    return fminf(v[2], v[3]) >= 0x1p-60f && E < a.near;
+    return fminf(v[2], v[3]) >= 0x1p-60f && E < a.near && fabs(p) < 0x1p29;
 }
 __device__ __forceinline__ void table_element(const TableArgs& a, int64_t n, double f, float (&v)[4]) {
     double p = (double)n, low = 0.0;                         // the position is p + low exactly
@@ -692,12 +692,12 @@ int tao_bound_rope_tables(const int64_t* positions, const float* inv_freq, doubl
         a.k1[i] = widen(m * (a.m == 1.0 ? 1.0 + cu : (1.0 + u) * (1.0 + cu)));
         a.k2[i] = widen(m * (a.m == 1.0 ? cu : (1.0 + u) * cu + u));
     }
-    bool quick = a.e1 >= 0x1p-27;
+    bool quick = true;
     for (int i = 0; i < 2; ++i) {
         a.q1[i] = (float)a.k1[i]; a.q2[i] = (float)a.k2[i];
         quick = quick && a.k1[i] <= 0x1p60 && a.k2[i] <= 0x1p60;
     }
-    a.near = quick ? (float)a.e1 * 0x1p24f : 0.f;
+    a.near = quick ? (float)a.e1 * 0x1p45f : 0.f;
     // (tables of less than one element for each of the chip's threads: one a thread; 16640 x 63 8.9 us, four a thread 8.4, 2080 x 63 3.5 and 4.7)
     const bool vec = (half % 4 == 0 || npos * half >= 1L << 19) && aligned(cos_table, 16) && aligned(sin_table, 16) && aligned(tau_cos, 16) && aligned(tau_sin, 16);
     const long blocks = ((vec ? (npos * half + 3) / 4 : npos * half) + 255) / 256;
